@@ -1,0 +1,69 @@
+/*
+ * mp_layers.h -- C ABI of the operators around the aggregation: what a sparse
+ * expert layer over node features needs next to message passing (mp.h) and
+ * its typed products.  Part of libmp.so.
+ *
+ *   mp_group_norm       group norm with an activation over the nodes of each
+ *                       graph of a batch (channels last), and its gradients
+ *   mp_dropout          dropout from a counter-based generator; no mask is
+ *                       stored, the gradient draws it again
+ *   mp_route            softmax router: k experts a row, per-expert counts,
+ *                       balance and z losses, and its gradient
+ *   mp_mx_*             microscaled 4-bit floating point: quantisation, and
+ *                       the product of row segments with 4-bit weights
+ *
+ * The dispatch between them is mp.h's: mp_coo_to_csr of (row, expert) pairs
+ * sorts rows by expert and its rowptr is the segments of the products;
+ * mp_message_gather copies the rows; mp_spmm with the router's weights adds
+ * the experts' results up.
+ *
+ * Conventions are mp.h's: device arrays owned by the caller, host argument
+ * checks before anything is enqueued, no allocation, no floating-point
+ * atomics, every call asynchronous on `stream` and deterministic.  Sums,
+ * statistics and normalisers are held in fp32; a bf16 output is rounded to
+ * nearest even once.
+ */
+#ifndef MP_LAYERS_H_
+#define MP_LAYERS_H_
+
+#include "mp.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* ---------------------------------------------------------------------------
+ * Dropout from a counter-based generator.  Element f of row r has the number
+ * e = id(r) * F + f (or, with whole_rows, e = id(r) for the whole row), where
+ * id(r) = ids[r], or r without ids.  Its random word is the (e % 8)-th 16-bit
+ * word of Philox4x32-10 (Salmon, Moraes, Dror and Shaw, "Parallel random
+ * numbers: as easy as 1, 2, 3", 2011) with key (seed low, seed high) and
+ * counter (e / 8 low, e / 8 high, t low, t high), t = offset + *step.
+ * With limit = round(65536 p) the element stays iff word >= limit, multiplied
+ * by 65536 / (65536 - limit): the expectation is kept exactly, at a
+ * probability that is a multiple of 2^-16.  A dropped element is +0 whatever
+ * it held (infinities and NaN included).
+ * The mask is a function of (seed, offset, step, id, f) alone: the gradient
+ * with respect to x is the same call on the output's gradient without a
+ * residual, and with ids the edges of a CSR and of its transpose (ids = the
+ * COO numbers of either order) are dropped alike.
+ *   x         [N, F] of dtype, row r at element r * ldx.
+ *   residual  [N, F] of dtype, row stride ldr, added to what stays, or NULL.
+ *   ids       [N] int32, >= 0, or NULL.
+ *   p         in [0, 1] (1 drops everything).
+ *   step      [1] int64 on the device, or NULL (0): read when the call runs,
+ *             so that a captured graph draws anew on each replay.
+ *   out       [N, F] of dtype, row stride ldo; may be x or residual itself
+ *             (same address and stride), must not overlap them otherwise.
+ * Sizes: 0 <= N <= INT32_MAX, 1 <= F <= 65536, strides >= F.
+ * ------------------------------------------------------------------------- */
+int mp_dropout(const void* x, int dtype, int64_t N, int64_t F, int64_t ldx,
+               const void* residual, int64_t ldr, const int32_t* ids, int whole_rows, double p,
+               uint64_t seed, uint64_t offset, const int64_t* step, void* out, int64_t ldo,
+               void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* MP_LAYERS_H_ */

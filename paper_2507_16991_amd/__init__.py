@@ -1021,3 +1021,11 @@ def edge_dot(a, b, *, bidx=None, oidx=None, out=None, stream=None):
     mp_edge_dot(a, _dtype_code(a.dtype), b, _dtype_code(b.dtype), bidx, int(b.shape[0]), oidx, E,
                 F, out, stream)
     return out
+
+
+# ---- the operators around the aggregation (include/mp_layers.h) ------------------------
+
+from . import layers as _layers_module  # noqa: E402  (it uses the helpers above)
+from .layers import *  # noqa: E402,F401,F403
+
+__all__ += _layers_module.__all__

@@ -1,0 +1,116 @@
+// Internal declarations shared by the operators of include/mp_layers.h.
+#pragma once
+
+#include "mp_internal.hpp"
+#include "mp_layers.h"
+
+namespace mp {
+
+// ---- element types -----------------------------------------------------------
+// V consecutive elements at the alignment of one (gfx950 takes unaligned
+// global accesses) as floats.  bf16 is the upper half of a float; rounding back
+// is the hardware's, to nearest even.
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+struct F32 {
+    typedef float raw;
+};
+struct BF16 {
+    typedef uint16_t raw;
+};
+
+__device__ inline uint32_t pack_bf16(float a, float b) {
+    const f32x2 v = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+}
+
+template <int BYTES>
+struct Raw {
+    uint32_t w[BYTES / 4];
+};
+template <>
+struct Raw<2> {
+    uint16_t w[1];
+};
+
+// The raw bits of V elements of type T.
+template <typename T, int V>
+using RawOf = Raw<(int)sizeof(typename T::raw) * V>;
+
+template <typename T, int V>
+__device__ inline RawOf<T, V> load_raw(const typename T::raw* p) {
+    RawOf<T, V> r;
+    __builtin_memcpy(&r, p, sizeof(r));
+    return r;
+}
+
+template <typename T, int V>
+__device__ inline void to_floats(const RawOf<T, V>& r, float (&v)[V]) {
+    if constexpr (sizeof(typename T::raw) == 4) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = __uint_as_float(r.w[i]);
+    } else if constexpr (V == 1) {
+        v[0] = __uint_as_float((uint32_t)r.w[0] << 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+            v[2 * i] = __uint_as_float(r.w[i] << 16);
+            v[2 * i + 1] = __uint_as_float(r.w[i] & 0xFFFF0000u);
+        }
+    }
+}
+
+template <typename T, int V>
+__device__ inline RawOf<T, V> from_floats(const float (&v)[V]) {
+    RawOf<T, V> r;
+    if constexpr (sizeof(typename T::raw) == 4) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) r.w[i] = __float_as_uint(v[i]);
+    } else if constexpr (V == 1) {
+        r.w[0] = (uint16_t)pack_bf16(v[0], 0.f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) r.w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+    }
+    return r;
+}
+
+template <typename T, int V>
+__device__ inline void load_floats(const typename T::raw* p, float (&v)[V]) {
+    to_floats<T, V>(load_raw<T, V>(p), v);
+}
+
+template <typename T, int V>
+__device__ inline void store_floats(typename T::raw* p, const float (&v)[V]) {
+    const RawOf<T, V> r = from_floats<T, V>(v);
+    __builtin_memcpy(p, &r, sizeof(r));
+}
+
+template <typename T>
+__device__ inline float load_one(const typename T::raw* p) {
+    if constexpr (sizeof(typename T::raw) == 4) return *p;
+    else return __uint_as_float((uint32_t)*p << 16);
+}
+
+template <typename T>
+__device__ inline void store_one(typename T::raw* p, float v) {
+    if constexpr (sizeof(typename T::raw) == 4) *p = v;
+    else *p = (uint16_t)pack_bf16(v, 0.f);
+}
+
+// ---- dropout (dropout.hip) -----------------------------------------------------
+struct DropoutParams {
+    const void* x;
+    const void* residual;  // nullptr: none
+    const int32_t* ids;    // nullptr: the row's number
+    const int64_t* step;   // nullptr: 0
+    void* out;
+    int64_t N, F, ldx, ldr, ldo;
+    uint32_t limit;        // an element stays iff its 16-bit word is at least this
+    float scale;
+    uint64_t seed, offset;
+};
+hipError_t launch_dropout(const DropoutParams& p, int dtype, int whole_rows, hipStream_t s);
+
+}  // namespace mp

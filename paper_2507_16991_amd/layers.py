@@ -1,0 +1,112 @@
+"""Python binding of the operators around the aggregation (``include/mp_layers.h``): group norm with
+an activation, dropout, the softmax router and microscaled 4-bit floating point.
+
+As in the package's root, ``mp_*`` functions carry the names of the C ABI and take tensors or None for
+pointers; the others size and allocate outputs and workspaces with torch.  The root re-exports all of
+them.
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes
+
+import torch
+
+from . import (MP_F32, _bytes, _check, _dtype_code, _itype_code, _ptr, _rows_ptr, _stream, _workspace,
+               lib as _root_lib)
+
+__all__ = ["mp_dropout", "dropout", "dropout_backward"]
+
+_lib = None
+
+
+def _layers():
+    """The library with this header's functions declared."""
+    global _lib
+    if _lib is None:
+        L = _root_lib()
+        i32, i64, p, u64 = ctypes.c_int, ctypes.c_int64, ctypes.c_void_p, ctypes.c_uint64
+        L.mp_dropout.argtypes = [p, i32, i64, i64, i64, p, i64, p, i32, ctypes.c_double, u64, u64, p,
+                                 p, i64, p]
+        for name in ("mp_dropout",):
+            getattr(L, name).restype = i32
+        _lib = L
+    return _lib
+
+
+def _on(stream):
+    """What the wrappers allocate and free while they enqueue on `stream` belongs to that stream, so
+    that memory is not given away while its kernels run."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(_stream(stream))
+    return torch.cuda.stream(stream)
+
+
+def _on_gpu(*tensors):
+    """Kernels run on the current GPU: an operand elsewhere is refused."""
+    dev = torch.cuda.current_device() if torch.cuda.is_available() else None
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != dev):
+            raise ValueError(f"operands must be on the current GPU, got one on {t.device}")
+
+
+def _table(t):
+    """_rows_ptr, also for one value a row ([N] as a table of one column)."""
+    return _rows_ptr(t[:, None] if t.dim() == 1 else t)
+
+
+def _like(t, ref, name):
+    if t is not None and (t.shape != ref.shape or t.dtype != ref.dtype):
+        raise ValueError(f"{name} must have the shape and dtype of x")
+    return t
+
+
+def _vector(t, n, dtype, name):
+    """Checks a small contiguous operand of n values."""
+    if t is not None and (t.numel() != n or t.dtype != dtype):
+        raise ValueError(f"{name} must hold {n} values of {dtype}")
+    return t
+
+
+# ---- dropout ------------------------------------------------------------------------------
+
+def mp_dropout(x, dtype, N, F, ldx, residual, ldr, ids, whole_rows, p, seed, offset, step, out, ldo,
+               stream=None):
+    """x, residual and out: tensors (rows may be strided) or raw addresses."""
+    xp, rp, op = (_table(t)[0] if isinstance(t, torch.Tensor) else t for t in (x, residual, out))
+    _check("mp_dropout", _layers().mp_dropout(
+        xp, dtype, N, F, ldx, rp, ldr, _ptr(ids), whole_rows, p, seed, offset, _ptr(step), op, ldo,
+        _stream(stream)))
+
+
+def dropout(x, p, seed, *, offset=0, step=None, ids=None, rows=False, residual=None, out=None,
+            stream=None):
+    """x [N, F] or [N] with each element (rows: each row) dropped with probability p and the others
+    scaled by 1 / (1 - p), plus residual.
+
+    The mask is a function of seed, offset + step (step: an int64 tensor on the device) and the
+    element's number ids[r] * F + f (ids: int32 [N], default r; rows: ids[r]), and is stored nowhere:
+    dropout_backward draws it again."""
+    N, F = int(x.shape[0]), int(x.shape[1]) if x.dim() == 2 else 1
+    _like(residual, x, "residual")
+    _vector(ids, N, torch.int32, "ids")
+    _vector(step, 1, torch.int64, "step")
+    _like(out, x, "out")
+    _on_gpu(x, residual, ids, step, out)
+    if out is None:
+        with _on(stream):
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    xp, ldx = _table(x)
+    rp, ldr = _table(residual) if residual is not None else (None, F)
+    op, ldo = _table(out)
+    mp_dropout(xp, _dtype_code(x.dtype), N, F, ldx, rp, ldr, ids, int(rows), p, seed, offset, step, op,
+               ldo, stream)
+    return out
+
+
+def dropout_backward(dout, p, seed, *, offset=0, step=None, ids=None, rows=False, out=None,
+                     stream=None):
+    """dL/dx of dropout given dL/dout: the same mask and scale (the residual's gradient is dout)."""
+    return dropout(dout, p, seed, offset=offset, step=step, ids=ids, rows=rows, out=out, stream=stream)

@@ -1,0 +1,65 @@
+"""CPU checks of include/mp_layers.h: every function is exported, and bad arguments are refused on
+the host, before anything is enqueued (the pointers are fake and never followed)."""
+import os
+import re
+
+import numpy as np
+import pytest
+import torch
+
+import layer_refs as ref
+import paper_2507_16991_amd as mp
+from paper_2507_16991_amd import layers
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+FAKE = 0x10000
+
+
+def test_exports_every_declared_function():
+    text = open(os.path.join(ROOT, "include", "mp_layers.h")).read()
+    text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
+    names = set(re.findall(r"\bint (mp_[a-z0-9_]+)\s*\(", text))
+    assert "mp_dropout" in names
+    for n in names:
+        assert hasattr(mp.lib(), n), f"{n} declared but not exported"
+        assert getattr(mp, n), f"{n} has no binding"
+
+
+def refused(fn, base, status, **change):
+    args = dict(base, **change)
+    assert getattr(layers._layers(), fn)(*args.values()) == status, change
+
+
+DROPOUT = dict(x=FAKE, dtype=0, N=10, F=8, ldx=8, residual=None, ldr=8, ids=None, whole_rows=0, p=0.5,
+               seed=1, offset=0, step=None, out=FAKE, ldo=8, stream=None)
+
+
+@pytest.mark.parametrize("status,change", [
+    (-3, dict(dtype=2)), (-2, dict(N=-1)), (-2, dict(N=2 ** 31)), (-2, dict(F=0)),
+    (-2, dict(F=65537, ldx=65537, ldo=65537)), (-2, dict(ldx=7)), (-2, dict(ldo=7)),
+    (-2, dict(residual=FAKE, ldr=7)), (-2, dict(p=-0.1)), (-2, dict(p=1.1)),
+    (-2, dict(p=float("nan"))), (-1, dict(x=None)), (-1, dict(out=None)), (-8, dict(x=FAKE + 2)),
+    (-8, dict(out=FAKE + 1)), (-8, dict(residual=FAKE + 2)), (-8, dict(ids=FAKE + 2)),
+    (-8, dict(step=FAKE + 4))])
+def test_dropout_refusals(status, change):
+    refused("mp_dropout", DROPOUT, status, **change)
+
+
+def test_nothing_to_do_is_accepted():
+    assert layers._layers().mp_dropout(*dict(DROPOUT, N=0, x=None, out=None).values()) == 0
+
+
+def test_operands_elsewhere_are_refused():
+    with pytest.raises(ValueError):
+        mp.dropout(torch.zeros(4, 4), 0.5, 1)
+
+
+def test_philox_published_outputs():
+    """The known answers that its authors publish for Philox4x32-10."""
+    ones = 0xFFFFFFFF
+    cases = [([0] * 4, [0] * 2, [0x6627E8D5, 0xE169C58D, 0xBC57AC4C, 0x9B00DBD8]),
+             ([ones] * 4, [ones] * 2, [0x408F276D, 0x41C83B0E, 0xA20BC7C6, 0x6D5451FD]),
+             ([0x243F6A88, 0x85A308D3, 0x13198A2E, 0x03707344], [0xA4093822, 0x299F31D0],
+              [0xD16CFE09, 0x94FDCCEB, 0x5001E420, 0x24126EA1])]
+    for counter, key, out in cases:
+        assert ref.philox(np.array([counter]), key).tolist() == [out]
