@@ -139,15 +139,70 @@ __global__ __launch_bounds__(kBlock) void dropout_rows(DropoutParams P, uint32_t
     }
 }
 
+// One element a row, as edge weights have, without a stride: every row has a
+// Philox block of its own, so the generator's products bound it; a thread
+// takes four rows with 16-byte loads.
+template <typename T, bool RES>
+__global__ __launch_bounds__(kBlock) void dropout_scalars(DropoutParams P) {
+    typedef typename T::raw raw;
+    const uint64_t t = draw_of(P);
+    const raw* x = static_cast<const raw*>(P.x);
+    const raw* res = static_cast<const raw*>(P.residual);
+    raw* out = static_cast<raw*>(P.out);
+    const int64_t groups = (P.N + 3) / 4;
+    for (int64_t g = (int64_t)blockIdx.x * kBlock + threadIdx.x; g < groups;
+         g += (int64_t)gridDim.x * kBlock) {
+        const int64_t r0 = 4 * g;
+        const bool whole = r0 + 4 <= P.N;
+        int32_t id[4] = {0, 0, 0, 0};
+        float v[4] = {}, r[4] = {};
+        if (whole) {
+            __builtin_memcpy(id, P.ids + r0, sizeof(id));
+            load_floats<T, 4>(x + r0, v);
+            if (RES) load_floats<T, 4>(res + r0, r);
+        } else {
+            for (int i = 0; i < 4; ++i)
+                if (r0 + i < P.N) {
+                    id[i] = P.ids[r0 + i];
+                    v[i] = load_one<T>(x + r0 + i);
+                    if (RES) r[i] = load_one<T>(res + r0 + i);
+                }
+        }
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t e = (uint32_t)id[i];
+            uint32_t w[4];
+            philox(e >> 3, P.seed, t, w);
+            const uint32_t a = e & 2 ? w[1] : w[0], b = e & 2 ? w[3] : w[2];
+            const uint32_t word = ((e & 4 ? b : a) >> (16 * (e & 1))) & 0xFFFFu;
+            m |= (uint32_t)(word >= P.limit) << i;
+        }
+        apply<RES>(v, r, m, P.scale);
+        if (whole) {
+            store_floats<T, 4>(out + r0, v);
+        } else {
+            for (int i = 0; i < 4; ++i)
+                if (r0 + i < P.N) store_one<T>(out + r0 + i, v[i]);
+        }
+    }
+}
+
 template <typename T, bool RES>
 void launch(const DropoutParams& p, int whole_rows, hipStream_t s) {
     const int64_t F = p.F;
     const bool dense = p.N <= 1 || (p.ldx == F && p.ldo == F && (!RES || p.ldr == F));
-    if (dense && !p.ids && !whole_rows) {
+    if (dense && !p.ids && (!whole_rows || F == 1)) {  // (of one element a row is an element)
         const int64_t blocks = ceil_div(p.N * F, (int64_t)kWords * kBlock);
         hipLaunchKernelGGL((dropout_flat<T, RES>),
                            dim3((unsigned)(blocks < kMaxGrid ? blocks : kMaxGrid)), dim3(kBlock),
                            0, s, p);
+        return;
+    }
+    if (F == 1 && dense && p.ids) {
+        const int64_t blocks = ceil_div(p.N, (int64_t)4 * kBlock);
+        hipLaunchKernelGGL((dropout_scalars<T, RES>), dim3((unsigned)blocks), dim3(kBlock), 0, s,
+                           p);
         return;
     }
     const int64_t cpr = whole_rows || F % kWords == 0 ? ceil_div(F, kWords) : (F + 14) / kWords;
