@@ -62,6 +62,48 @@ int mp_dropout(const void* x, int dtype, int64_t N, int64_t F, int64_t ldx,
                uint64_t seed, uint64_t offset, const int64_t* step, void* out, int64_t ldo,
                void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Softmax router with per-expert counts, a balance loss and a z loss.  A row
+ * takes part iff its mask is nonzero (no mask: every row) and it has a logit
+ * above -inf; an expert whose logit is -inf is never chosen.  Of a row that
+ * takes part:
+ *   idx[r, j]    the expert of the j-th largest logit (equal logits: the
+ *                lower number first), or -1 where fewer than j+1 are above
+ *                -inf
+ *   weight[r, j] exp(logit) over the sum of exp of the row's chosen logits
+ *                (renorm = 1) or of all its logits (renorm = 0); 0 where
+ *                idx is -1
+ * All rows that take part, R of them, give
+ *   counts[e]    how often expert e was chosen; counts[E] = R
+ *   loss[0]      E * sum_e (counts[e] / sum of counts) * P_e, P_e = the mean
+ *                softmax probability of expert e (the balance loss: 1 where
+ *                all experts are chosen alike)
+ *   loss[1]      the mean of logsumexp(row)^2 (the z loss)
+ * both 0 if R = 0.  Other rows have idx -1, weight 0, and whatever they hold
+ * (NaN included) reaches no output.  NaN in a row that takes part makes its
+ * weights and the losses NaN (idx stays in range).
+ *   logits  [N, E] of dtype, row stride ldl;  mask [N] bytes or NULL.
+ * Sizes: 0 <= N <= INT32_MAX, 1 <= E <= 1024, 1 <= k <= min(E, 64),
+ * N * k <= INT32_MAX (the counts).
+ * ------------------------------------------------------------------------- */
+
+/* Workspace bytes of mp_route (partial sums of the losses). */
+int mp_route_workspace(int64_t N, int64_t E, size_t* bytes);
+
+int mp_route(const void* logits, int dtype, int64_t N, int64_t E, int64_t ldl, int64_t k,
+             const uint8_t* mask, int renorm, int32_t* idx, float* weight, int32_t* counts,
+             float* loss, void* ws, size_t ws_bytes, void* stream);
+
+/* dL/dlogits, given dweight = dL/dweight [N, k] fp32 (or NULL: 0) and dloss =
+ * dL/dloss [2] fp32 on the device (or NULL: 0), with the forward's idx,
+ * weight and counts (the choice itself and the counts have no gradient):
+ *   dlogits  [N, E] contiguous of dtype, written in full (0 for rows that take
+ *            no part); must not overlap logits. */
+int mp_route_backward(const void* logits, int dtype, int64_t N, int64_t E, int64_t ldl,
+                      int64_t k, const uint8_t* mask, int renorm, const int32_t* idx,
+                      const float* weight, const int32_t* counts, const float* dweight,
+                      const float* dloss, void* dlogits, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -113,4 +113,23 @@ struct DropoutParams {
 };
 hipError_t launch_dropout(const DropoutParams& p, int dtype, int whole_rows, hipStream_t s);
 
+// ---- router (route.hip) ----------------------------------------------------------
+struct RouteParams {
+    const void* logits;
+    const uint8_t* mask;  // nullptr: every row
+    int64_t N, E, ldl, k;
+    int renorm;
+    int32_t* idx;         // forward: out; backward: in
+    float* weight;
+    int32_t* counts;      // [E + 1]
+    float* loss;          // [2]
+    float* part;          // [route_blocks][2 E + 2] partial sums
+    const float* dweight; // nullptr: 0
+    const float* dloss;   // nullptr: 0
+    void* dlogits;
+};
+int route_blocks(int64_t N, int64_t E);
+hipError_t launch_route(const RouteParams& p, int dtype, hipStream_t s);
+hipError_t launch_route_backward(const RouteParams& p, int dtype, hipStream_t s);
+
 }  // namespace mp

@@ -15,7 +15,8 @@ import torch
 from . import (MP_F32, _bytes, _check, _dtype_code, _itype_code, _ptr, _rows_ptr, _stream, _workspace,
                lib as _root_lib)
 
-__all__ = ["mp_dropout", "dropout", "dropout_backward"]
+__all__ = ["mp_dropout", "dropout", "dropout_backward", "mp_route_workspace", "mp_route",
+           "mp_route_backward", "route", "route_backward"]
 
 _lib = None
 
@@ -28,7 +29,11 @@ def _layers():
         i32, i64, p, u64 = ctypes.c_int, ctypes.c_int64, ctypes.c_void_p, ctypes.c_uint64
         L.mp_dropout.argtypes = [p, i32, i64, i64, i64, p, i64, p, i32, ctypes.c_double, u64, u64, p,
                                  p, i64, p]
-        for name in ("mp_dropout",):
+        psz = ctypes.POINTER(ctypes.c_size_t)
+        L.mp_route_workspace.argtypes = [i64, i64, psz]
+        L.mp_route.argtypes = [p, i32, i64, i64, i64, i64, p, i32, p, p, p, p, p, ctypes.c_size_t, p]
+        L.mp_route_backward.argtypes = [p, i32, i64, i64, i64, i64, p, i32, p, p, p, p, p, p, p]
+        for name in ("mp_dropout", "mp_route_workspace", "mp_route", "mp_route_backward"):
             getattr(L, name).restype = i32
         _lib = L
     return _lib
@@ -110,3 +115,83 @@ def dropout_backward(dout, p, seed, *, offset=0, step=None, ids=None, rows=False
                      stream=None):
     """dL/dx of dropout given dL/dout: the same mask and scale (the residual's gradient is dout)."""
     return dropout(dout, p, seed, offset=offset, step=step, ids=ids, rows=rows, out=out, stream=stream)
+
+
+# ---- router -------------------------------------------------------------------------------
+
+def mp_route_workspace(N, E) -> int:
+    _layers()
+    return _bytes("mp_route_workspace", N, E)
+
+
+def mp_route(logits, dtype, N, E, ldl, k, mask, renorm, idx, weight, counts, loss, ws, ws_bytes,
+             stream=None):
+    """logits: a tensor (rows may be strided) or a raw address."""
+    lp = _rows_ptr(logits)[0] if isinstance(logits, torch.Tensor) else logits
+    _check("mp_route", _layers().mp_route(
+        lp, dtype, N, E, ldl, k, _ptr(mask), renorm, _ptr(idx), _ptr(weight), _ptr(counts),
+        _ptr(loss), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def mp_route_backward(logits, dtype, N, E, ldl, k, mask, renorm, idx, weight, counts, dweight, dloss,
+                      dlogits, stream=None):
+    lp = _rows_ptr(logits)[0] if isinstance(logits, torch.Tensor) else logits
+    _check("mp_route_backward", _layers().mp_route_backward(
+        lp, dtype, N, E, ldl, k, _ptr(mask), renorm, _ptr(idx), _ptr(weight), _ptr(counts),
+        _ptr(dweight), _ptr(dloss), _ptr(dlogits), _stream(stream)))
+
+
+def _mask(mask, N):
+    if mask is None:
+        return None
+    if mask.numel() != N or mask.dtype not in (torch.bool, torch.uint8):
+        raise ValueError(f"mask must hold {N} truth values")
+    return mask
+
+
+def route(logits, k, *, mask=None, renorm=True, stream=None):
+    """The k experts of every row of logits [N, E] and what the batch makes of them:
+    (idx [N, k] int32, weight [N, k] fp32, counts [E + 1] int32: choices of each expert and the rows
+    that took part, loss [2] fp32: balance and z).
+
+    Rows whose mask ([N] bool) is false, or whose logits are all -inf, take no part: idx -1, weight 0.
+    renorm: the weights of a row add up to 1 (else they are softmax probabilities over all experts)."""
+    N, E = int(logits.shape[0]), int(logits.shape[1])
+    k = int(k)
+    _mask(mask, N)
+    _on_gpu(logits, mask)
+    dev = logits.device
+    dt = _dtype_code(logits.dtype)
+    lp, ldl = _rows_ptr(logits)
+    nb = mp_route_workspace(N, E)
+    with _on(stream):
+        idx = torch.empty(N, max(k, 0), dtype=torch.int32, device=dev)
+        weight = torch.empty(N, max(k, 0), dtype=torch.float32, device=dev)
+        counts = torch.empty(E + 1, dtype=torch.int32, device=dev)
+        loss = torch.empty(2, dtype=torch.float32, device=dev)
+        ws = _workspace(nb, dev) if nb else None
+        mp_route(lp, dt, N, E, ldl, k, mask, int(renorm), idx, weight, counts, loss, ws, nb, stream)
+    return idx, weight, counts, loss
+
+
+def route_backward(logits, idx, weight, counts, *, dweight=None, dloss=None, mask=None, renorm=True,
+                   out=None, stream=None):
+    """dL/dlogits [N, E] (dtype of logits) given dweight = dL/dweight [N, k] fp32 and dloss = dL/dloss
+    [2] fp32 on the GPU (None: 0), and what route returned."""
+    N, E = int(logits.shape[0]), int(logits.shape[1])
+    k = int(idx.shape[1])
+    _mask(mask, N)
+    _vector(idx, N * k, torch.int32, "idx")
+    _vector(weight, N * k, torch.float32, "weight")
+    _vector(counts, E + 1, torch.int32, "counts")
+    _vector(dweight, N * k, torch.float32, "dweight")
+    _vector(dloss, 2, torch.float32, "dloss")
+    _like(out, logits, "out")
+    _on_gpu(logits, idx, weight, counts, dweight, dloss, mask, out)
+    lp, ldl = _rows_ptr(logits)
+    if out is None:
+        with _on(stream):
+            out = torch.empty(N, E, dtype=logits.dtype, device=logits.device)
+    mp_route_backward(lp, _dtype_code(logits.dtype), N, E, ldl, k, mask, int(renorm), idx, weight,
+                      counts, dweight, dloss, out, stream)
+    return out

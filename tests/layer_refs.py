@@ -47,3 +47,59 @@ def dropout(x, p, seed, t=0, ids=None, rows=False, residual=None):
     keep = np.broadcast_to((words(e, seed, t) >= limit).reshape(e.shape), (n, f))
     out = np.where(keep, x * (65536 / max(1, 65536 - limit)), 0.0)
     return out if residual is None else out + residual, keep
+
+
+# ---- router -------------------------------------------------------------------------------
+
+def choose(l, k, mask=None):
+    """idx [N, k] of logits l [N, E] float64 (equal logits: lower number first; -inf never), and which
+    rows take part."""
+    n, e = l.shape
+    part = np.ones(n, bool) if mask is None else mask.astype(bool)
+    part = part & (np.where(part[:, None], l, -np.inf) > -np.inf).any(1)
+    idx = np.full((n, k), -1, np.int64)
+    for r in np.nonzero(part)[0]:
+        order = sorted(range(e), key=lambda i: (-l[r, i], i))
+        for j in range(k):
+            if l[r, order[j]] > -np.inf:
+                idx[r, j] = order[j]
+    return idx, part
+
+
+def route(l, idx, part, renorm=True):
+    """weight, counts, loss [balance, z], and what the gradient needs, for given choices."""
+    n, e = l.shape
+    safe = np.where(part[:, None], l, 0.0)
+    big = safe.max(1, keepdims=True)
+    p = np.where(part[:, None], np.exp(safe - big), 0.0)
+    tot = np.where(part, p.sum(1), 1.0)
+    p = p / tot[:, None]
+    real = idx >= 0
+    w = np.where(real, np.take_along_axis(p, np.maximum(idx, 0), 1), 0.0)
+    if renorm:
+        w = w / np.where(part, w.sum(1), 1.0)[:, None]
+    counts = np.bincount(idx[real], minlength=e)
+    rows = int(part.sum())
+    lse = np.where(part, np.log(tot) + big[:, 0], 0.0)
+    balance = e * float((counts / max(1, counts.sum()) * p.sum(0) / max(1, rows)).sum())
+    return w, counts, rows, np.array([balance, float((lse ** 2).sum()) / max(1, rows)]), p, lse
+
+
+def route_backward(l, idx, part, dweight, dloss, renorm=True):
+    """dL/dl and, element by element, the size of the terms that make it up."""
+    n, e = l.shape
+    w, counts, rows, _, p, lse = route(l, idx, part, renorm)
+    real = idx >= 0
+    dw = np.where(real, dweight, 0.0)
+    S = (w * dw).sum(1, keepdims=True)
+    d = dloss[0] * e * counts / max(1, counts.sum()) / max(1, rows)
+    z = 2 * dloss[1] * lse[:, None] / max(1, rows)
+    pd = (p * d).sum(1, keepdims=True)
+    g = p * (d - pd + z - (0 if renorm else S))
+    size = p * (np.abs(d) + np.abs(pd) + np.abs(z) + (0 if renorm else np.abs(w * dw).sum(1, keepdims=True)))
+    for r in range(n):
+        for j in range(idx.shape[1]):
+            if real[r, j]:
+                g[r, idx[r, j]] += w[r, j] * (dw[r, j] - (S[r, 0] if renorm else 0))
+                size[r, idx[r, j]] += w[r, j] * (abs(dw[r, j]) + np.abs(w[r] * dw[r]).sum())
+    return np.where(part[:, None], g, 0.0), size

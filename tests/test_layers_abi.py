@@ -63,3 +63,37 @@ def test_philox_published_outputs():
               [0xD16CFE09, 0x94FDCCEB, 0x5001E420, 0x24126EA1])]
     for counter, key, out in cases:
         assert ref.philox(np.array([counter]), key).tolist() == [out]
+
+
+ROUTE = dict(logits=FAKE, dtype=0, N=10, E=8, ldl=8, k=2, mask=None, renorm=1, idx=FAKE, weight=FAKE,
+             counts=FAKE, loss=FAKE, ws=None, ws_bytes=0, stream=None)
+
+
+@pytest.mark.parametrize("status,change", [
+    (-3, dict(dtype=7)), (-2, dict(N=-1)), (-2, dict(N=2 ** 31)), (-2, dict(E=0)),
+    (-2, dict(E=1025, ldl=1025)), (-2, dict(ldl=7)), (-2, dict(k=0)), (-2, dict(k=9)),
+    (-2, dict(N=2 ** 30, k=2)), (-2, dict(E=100, ldl=100, k=65)), (-1, dict(logits=None)),
+    (-1, dict(idx=None)), (-1, dict(weight=None)), (-1, dict(counts=None)), (-1, dict(loss=None)),
+    (-8, dict(logits=FAKE + 2)), (-8, dict(idx=FAKE + 2)), (-8, dict(counts=FAKE + 1)),
+    (-1, dict(N=100000)), (-5, dict(N=100000, ws=FAKE, ws_bytes=64))])
+def test_route_refusals(status, change):
+    refused("mp_route", ROUTE, status, **change)
+
+
+ROUTE_BACKWARD = dict(logits=FAKE, dtype=1, N=10, E=8, ldl=8, k=2, mask=None, renorm=1, idx=FAKE,
+                      weight=FAKE, counts=FAKE, dweight=None, dloss=None, dlogits=FAKE, stream=None)
+
+
+@pytest.mark.parametrize("status,change", [
+    (-3, dict(dtype=7)), (-2, dict(k=9)), (-1, dict(dlogits=None)), (-1, dict(counts=None)),
+    (-8, dict(dweight=FAKE + 2)), (-8, dict(dloss=FAKE + 2)), (-8, dict(dlogits=FAKE + 1))])
+def test_route_backward_refusals(status, change):
+    refused("mp_route_backward", ROUTE_BACKWARD, status, **change)
+
+
+def test_route_workspace():
+    assert mp.mp_route_workspace(0, 64) == 0 and mp.mp_route_workspace(16, 64) == 0
+    assert mp.mp_route_workspace(10 ** 6, 64) > 0
+    for bad in ((-1, 8), (2 ** 31, 8), (8, 0), (8, 1025)):
+        with pytest.raises(mp.MPError):
+            mp.mp_route_workspace(*bad)
