@@ -33,6 +33,59 @@ extern "C" {
 #endif
 
 /* ---------------------------------------------------------------------------
+ * Group norm with an activation, over segments of consecutive rows.
+ * Segment s holds rows ptr[s] <= r < ptr[s+1] (the graphs of a batch; ptr as
+ * for mp_readout_multi), group g the channels g * F/G <= c < (g+1) * F/G.
+ *   mean[s, g], var[s, g]  over the segment's rows and the group's channels
+ *                          (population variance);  rstd = 1/sqrt(var + eps)
+ *   xhat = (x - mean) * rstd,  z = xhat * gamma[c] + beta[c],  out = act(z)
+ * The variance is taken about the mean (no difference of large squares).  An
+ * empty segment has mean = rstd = 0.
+ * ------------------------------------------------------------------------- */
+
+typedef enum mp_act {
+    MP_ACT_NONE = 0,
+    MP_ACT_RELU = 1, /* max(z, 0), derivative 0 at z = 0 */
+    MP_ACT_SILU = 2, /* z / (1 + exp(-z)) */
+    MP_ACT_GELU = 3  /* z * (1 + erf(z / sqrt 2)) / 2 */
+} mp_act;
+
+/* Workspace bytes of mp_group_norm (backward = 0) or mp_group_norm_backward
+ * (backward = 1) for N rows, S segments, F channels of x_dtype and G groups. */
+int mp_group_norm_workspace(int64_t N, int64_t S, int64_t F, int64_t G, int x_dtype,
+                            int backward, size_t* bytes);
+
+/* Forward.
+ *   ptr          [S+1] of ptr_itype: ptr[0] = 0, non-decreasing, ptr[S] = N
+ *                (offsets outside [0, N] are taken as the nearest in it).
+ *   x            [N, F] of x_dtype, row r at element r * ldx (ldx >= F).
+ *   gamma, beta  [F] fp32 or NULL (1 and 0).
+ *   eps          added to the variance, >= 0 and finite.
+ *   out          [N, F] contiguous, of out_dtype; must not overlap x.
+ *   mean, rstd   [S, G] fp32, written (the gradient takes them).
+ * Sizes: 0 <= N, 1 <= S, both <= INT32_MAX, 1 <= F <= 65536, 1 <= G <= F and
+ * F % G = 0. */
+int mp_group_norm(const void* ptr, int ptr_itype, const void* x, int x_dtype, int64_t N,
+                  int64_t S, int64_t F, int64_t ldx, int64_t G, const float* gamma,
+                  const float* beta, float eps, int act, void* out, int out_dtype, float* mean,
+                  float* rstd, void* ws, size_t ws_bytes, void* stream);
+
+/* Gradients given dout = dL/dout [N, F] of x_dtype (contiguous) and the
+ * forward's mean and rstd; ptr, x, gamma, beta and act as in the forward.
+ *   da = dout * act'(z)
+ *   dx[r, c]  = rstd * (gamma da - mean(gamma da) - xhat mean(gamma da xhat)),
+ *               the means over the segment's rows and the group's channels
+ *   dgamma[c] = sum over all rows of da * xhat,  dbeta[c] = sum of da
+ *   dx           [N, F] contiguous of dx_dtype, or NULL; must not overlap x
+ *                or dout.
+ *   dgamma, dbeta  [F] fp32, both or neither; not all three outputs NULL. */
+int mp_group_norm_backward(const void* ptr, int ptr_itype, const void* x, int x_dtype,
+                           const void* dout, int64_t N, int64_t S, int64_t F, int64_t ldx,
+                           int64_t G, const float* gamma, const float* beta, const float* mean,
+                           const float* rstd, int act, void* dx, int dx_dtype, float* dgamma,
+                           float* dbeta, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
  * Dropout from a counter-based generator.  Element f of row r has the number
  * e = id(r) * F + f (or, with whole_rows, e = id(r) for the whole row), where
  * id(r) = ids[r], or r without ids.  Its random word is the (e % 8)-th 16-bit

@@ -21,6 +21,44 @@ size_t elem(int dtype) { return dtype == MP_BF16 ? 2 : 4; }
 constexpr int64_t kMaxF = 65536;
 
 
+// Workspace of the group norm, in pieces that start on 256 bytes.
+struct NormSpace {
+    size_t stats = 0, ca = 0, cb = 0, part = 0, bytes = 0;
+};
+NormSpace norm_space(const NormShape& h, int64_t S, int64_t F, int64_t G, int backward) {
+    NormSpace n;
+    const auto take = [&](int64_t floats) {
+        const size_t at = n.bytes;
+        n.bytes = align_up(at + (size_t)floats * 4, 256);
+        return at;
+    };
+    if (h.long_tiles) {
+        n.stats = take(h.long_tiles * 2 * h.stat_line * 2);
+        if (backward) {
+            n.ca = take(S * G);
+            n.cb = take(S * G);
+        }
+    }
+    if (backward) n.part = take(((h.unit ? h.short_blocks : 0) + h.long_tiles) * 2 * F);
+    return n;
+}
+
+int norm_dims(int64_t N, int64_t S, int64_t F, int64_t G, int x_dtype) {
+    if (!valid_dtype(x_dtype)) return MP_ERR_DTYPE;
+    if (N < 0 || N > INT32_MAX || S < 1 || S > INT32_MAX || F < 1 || F > kMaxF || G < 1 ||
+        F % G != 0)
+        return MP_ERR_SIZE;
+    return MP_OK;
+}
+
+int norm_call(const void* ptr, int ptr_itype, int64_t ldx, int64_t F, int act, int out_dtype) {
+    if (!valid_itype(ptr_itype) || !valid_dtype(out_dtype)) return MP_ERR_DTYPE;
+    if (ldx < F || act < MP_ACT_NONE || act > MP_ACT_GELU) return MP_ERR_SIZE;
+    if (!ptr) return MP_ERR_NULL;
+    if (!aligned(ptr, ptr_itype == MP_I64 ? 8 : 4)) return MP_ERR_ALIGN;
+    return MP_OK;
+}
+
 int route_dims(int dtype, int64_t N, int64_t E, int64_t ldl, int64_t k) {
     if (!valid_dtype(dtype)) return MP_ERR_DTYPE;
     if (N < 0 || N > INT32_MAX || E < 1 || E > 1024 || ldl < E || k < 1 || k > 64 || k > E ||
@@ -66,6 +104,97 @@ int mp_dropout(const void* x, int dtype, int64_t N, int64_t F, int64_t ldx, cons
     P.seed = seed;
     P.offset = offset;
     return hip_status(launch_dropout(P, dtype, whole_rows != 0, as_stream(stream)));
+}
+
+int mp_group_norm_workspace(int64_t N, int64_t S, int64_t F, int64_t G, int x_dtype,
+                            int backward, size_t* bytes) {
+    if (!bytes) return MP_ERR_NULL;
+    const int st = norm_dims(N, S, F, G, x_dtype);
+    if (st != MP_OK) return st;
+    *bytes = norm_space(norm_shape(N, S, F, G, x_dtype, backward), S, F, G, backward).bytes;
+    return MP_OK;
+}
+
+int mp_group_norm(const void* ptr, int ptr_itype, const void* x, int x_dtype, int64_t N,
+                  int64_t S, int64_t F, int64_t ldx, int64_t G, const float* gamma,
+                  const float* beta, float eps, int act, void* out, int out_dtype, float* mean,
+                  float* rstd, void* ws, size_t ws_bytes, void* stream) {
+    int st = norm_dims(N, S, F, G, x_dtype);
+    if (st == MP_OK) st = norm_call(ptr, ptr_itype, ldx, F, act, out_dtype);
+    if (st != MP_OK) return st;
+    if (!(eps >= 0.f && eps <= FLT_MAX)) return MP_ERR_SIZE;
+    const NormShape h = norm_shape(N, S, F, G, x_dtype, 0);
+    const NormSpace n = norm_space(h, S, F, G, 0);
+    if ((N > 0 && (!x || !out)) || !mean || !rstd || (n.bytes && !ws)) return MP_ERR_NULL;
+    if (!aligned(x, elem(x_dtype)) || !aligned(out, elem(out_dtype)) || !aligned(gamma, 4) ||
+        !aligned(beta, 4) || !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(ws, 16))
+        return MP_ERR_ALIGN;
+    if (ws_bytes < n.bytes) return MP_ERR_WORKSPACE;
+    NormParams P{};
+    P.ptr = ptr;
+    P.rp64 = ptr_itype == MP_I64;
+    P.x = x;
+    P.N = N;
+    P.S = S;
+    P.F = F;
+    P.ldx = ldx;
+    P.G = G;
+    P.cg = (int)(F / G);
+    P.gamma = gamma;
+    P.beta = beta;
+    P.eps = eps;
+    P.act = act;
+    P.out = out;
+    P.out_bf16 = out_dtype == MP_BF16;
+    P.mean = mean;
+    P.rstd = rstd;
+    P.stats = reinterpret_cast<float*>(static_cast<char*>(ws) + n.stats);
+    return hip_status(launch_norm(P, h, x_dtype, false, nullptr, nullptr, as_stream(stream)));
+}
+
+int mp_group_norm_backward(const void* ptr, int ptr_itype, const void* x, int x_dtype,
+                           const void* dout, int64_t N, int64_t S, int64_t F, int64_t ldx,
+                           int64_t G, const float* gamma, const float* beta, const float* mean,
+                           const float* rstd, int act, void* dx, int dx_dtype, float* dgamma,
+                           float* dbeta, void* ws, size_t ws_bytes, void* stream) {
+    int st = norm_dims(N, S, F, G, x_dtype);
+    if (st == MP_OK) st = norm_call(ptr, ptr_itype, ldx, F, act, dx_dtype);
+    if (st != MP_OK) return st;
+    const NormShape h = norm_shape(N, S, F, G, x_dtype, 1);
+    const NormSpace n = norm_space(h, S, F, G, 1);
+    if ((N > 0 && (!x || !dout)) || !mean || !rstd || !dgamma != !dbeta || (!dx && !dgamma) ||
+        (n.bytes && !ws))
+        return MP_ERR_NULL;
+    if (!aligned(x, elem(x_dtype)) || !aligned(dout, elem(x_dtype)) ||
+        !aligned(dx, elem(dx_dtype)) || !aligned(gamma, 4) || !aligned(beta, 4) ||
+        !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(dgamma, 4) || !aligned(dbeta, 4) ||
+        !aligned(ws, 16))
+        return MP_ERR_ALIGN;
+    if (ws_bytes < n.bytes) return MP_ERR_WORKSPACE;
+    char* w = static_cast<char*>(ws);
+    NormParams P{};
+    P.ptr = ptr;
+    P.rp64 = ptr_itype == MP_I64;
+    P.x = x;
+    P.dout = dout;
+    P.N = N;
+    P.S = S;
+    P.F = F;
+    P.ldx = ldx;
+    P.G = G;
+    P.cg = (int)(F / G);
+    P.gamma = gamma;
+    P.beta = beta;
+    P.act = act;
+    P.out = dx;
+    P.out_bf16 = dx_dtype == MP_BF16;
+    P.mean = const_cast<float*>(mean);
+    P.rstd = const_cast<float*>(rstd);
+    P.stats = reinterpret_cast<float*>(w + n.stats);
+    P.ca = reinterpret_cast<float*>(w + n.ca);
+    P.cb = reinterpret_cast<float*>(w + n.cb);
+    P.part = dgamma ? reinterpret_cast<float*>(w + n.part) : nullptr;
+    return hip_status(launch_norm(P, h, x_dtype, true, dgamma, dbeta, as_stream(stream)));
 }
 
 int mp_route_workspace(int64_t N, int64_t E, size_t* bytes) {

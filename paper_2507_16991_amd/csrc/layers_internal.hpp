@@ -113,6 +113,49 @@ struct DropoutParams {
 };
 hipError_t launch_dropout(const DropoutParams& p, int dtype, int whole_rows, hipStream_t s);
 
+// ---- group norm (norm.hip) -------------------------------------------------------
+// How a call of these sizes is cut up.
+struct NormShape {
+    int V;                  // channels of a thread's chunk
+    // short segments (unit = 0: groups too wide, every segment is a long one)
+    int unit, tile_groups, tiles, cpr, slots, lpg, short_blocks;
+    int64_t lmax;           // rows of the longest short segment
+    size_t lds;
+    // long segments (long_tiles = 0: there can be none)
+    int64_t tile_rows, long_tiles, col_tile, stat_line;
+    int col_tiles, long_lpg;
+    size_t long_lds;
+};
+NormShape norm_shape(int64_t N, int64_t S, int64_t F, int64_t G, int dtype, int backward);
+
+struct NormParams {
+    const void* ptr;
+    int rp64;
+    const void* x;
+    const void* dout;    // backward
+    int64_t N, S, F, ldx, G;
+    int cg;              // channels of a group
+    const float* gamma;  // nullptr: 1
+    const float* beta;   // nullptr: 0
+    float eps;
+    int act;
+    void* out;           // or dx (nullptr: not wanted)
+    int out_bf16;
+    float* mean;
+    float* rstd;
+    // workspace: partial statistics of the tiles, the segments' mean gradients,
+    // lines of dgamma and dbeta (nullptr: not wanted)
+    float* stats;
+    float* ca;
+    float* cb;
+    float* part;
+    // of the NormShape, filled by the launch
+    int64_t lmax, tile_rows, stat_line;
+    int tile_groups, cpr, slots, lpg, short_blocks;
+};
+hipError_t launch_norm(NormParams p, const NormShape& h, int dtype, bool backward, float* dgamma,
+                       float* dbeta, hipStream_t s);
+
 // ---- router (route.hip) ----------------------------------------------------------
 struct RouteParams {
     const void* logits;

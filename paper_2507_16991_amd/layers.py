@@ -15,8 +15,11 @@ import torch
 from . import (MP_F32, _bytes, _check, _dtype_code, _itype_code, _ptr, _rows_ptr, _stream, _workspace,
                lib as _root_lib)
 
-__all__ = ["mp_dropout", "dropout", "dropout_backward", "mp_route_workspace", "mp_route",
+__all__ = ["MP_ACT", "mp_group_norm_workspace", "mp_group_norm", "mp_group_norm_backward",
+           "group_norm", "group_norm_backward", "mp_dropout", "dropout", "dropout_backward", "mp_route_workspace", "mp_route",
            "mp_route_backward", "route", "route_backward"]
+
+MP_ACT = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 
 _lib = None
 
@@ -29,11 +32,17 @@ def _layers():
         i32, i64, p, u64 = ctypes.c_int, ctypes.c_int64, ctypes.c_void_p, ctypes.c_uint64
         L.mp_dropout.argtypes = [p, i32, i64, i64, i64, p, i64, p, i32, ctypes.c_double, u64, u64, p,
                                  p, i64, p]
-        psz = ctypes.POINTER(ctypes.c_size_t)
+        psz, sz, f32 = ctypes.POINTER(ctypes.c_size_t), ctypes.c_size_t, ctypes.c_float
+        L.mp_group_norm_workspace.argtypes = [i64, i64, i64, i64, i32, i32, psz]
+        L.mp_group_norm.argtypes = [p, i32, p, i32, i64, i64, i64, i64, i64, p, p, f32, i32, p, i32,
+                                    p, p, p, sz, p]
+        L.mp_group_norm_backward.argtypes = [p, i32, p, i32, p, i64, i64, i64, i64, i64, p, p, p, p,
+                                             i32, p, i32, p, p, p, sz, p]
         L.mp_route_workspace.argtypes = [i64, i64, psz]
-        L.mp_route.argtypes = [p, i32, i64, i64, i64, i64, p, i32, p, p, p, p, p, ctypes.c_size_t, p]
+        L.mp_route.argtypes = [p, i32, i64, i64, i64, i64, p, i32, p, p, p, p, p, sz, p]
         L.mp_route_backward.argtypes = [p, i32, i64, i64, i64, i64, p, i32, p, p, p, p, p, p, p]
-        for name in ("mp_dropout", "mp_route_workspace", "mp_route", "mp_route_backward"):
+        for name in ("mp_group_norm_workspace", "mp_group_norm", "mp_group_norm_backward",
+                     "mp_dropout", "mp_route_workspace", "mp_route", "mp_route_backward"):
             getattr(L, name).restype = i32
         _lib = L
     return _lib
@@ -73,6 +82,94 @@ def _vector(t, n, dtype, name):
     if t is not None and (t.numel() != n or t.dtype != dtype):
         raise ValueError(f"{name} must hold {n} values of {dtype}")
     return t
+
+
+# ---- group norm ---------------------------------------------------------------------------
+
+def mp_group_norm_workspace(N, S, F, G, x_dtype, backward) -> int:
+    _layers()
+    return _bytes("mp_group_norm_workspace", N, S, F, G, x_dtype, int(backward))
+
+
+def mp_group_norm(ptr, ptr_itype, x, x_dtype, N, S, F, ldx, G, gamma, beta, eps, act, out, out_dtype,
+                  mean, rstd, ws, ws_bytes, stream=None):
+    """x: a tensor (rows may be strided) or a raw address."""
+    xp = _rows_ptr(x)[0] if isinstance(x, torch.Tensor) else x
+    _check("mp_group_norm", _layers().mp_group_norm(
+        _ptr(ptr), ptr_itype, xp, x_dtype, N, S, F, ldx, G, _ptr(gamma), _ptr(beta), eps, act,
+        _ptr(out), out_dtype, _ptr(mean), _ptr(rstd), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def mp_group_norm_backward(ptr, ptr_itype, x, x_dtype, dout, N, S, F, ldx, G, gamma, beta, mean, rstd,
+                           act, dx, dx_dtype, dgamma, dbeta, ws, ws_bytes, stream=None):
+    xp = _rows_ptr(x)[0] if isinstance(x, torch.Tensor) else x
+    _check("mp_group_norm_backward", _layers().mp_group_norm_backward(
+        _ptr(ptr), ptr_itype, xp, x_dtype, _ptr(dout), N, S, F, ldx, G, _ptr(gamma), _ptr(beta),
+        _ptr(mean), _ptr(rstd), act, _ptr(dx), dx_dtype, _ptr(dgamma), _ptr(dbeta), _ptr(ws),
+        ws_bytes, _stream(stream)))
+
+
+def _act(act):
+    if act not in MP_ACT:
+        raise ValueError(f"act must be one of {', '.join(MP_ACT)}")
+    return MP_ACT[act]
+
+
+def group_norm(ptr, x, groups, *, weight=None, bias=None, eps=1e-5, act="none", out_dtype=None,
+               out=None, stream=None):
+    """act(group norm of x [N, F]) over the segments of consecutive rows that ptr [S + 1] gives (the
+    graphs of a batch) and `groups` groups of consecutive channels; weight and bias [F] fp32.
+
+    Returns (out [N, F] of out_dtype (default x's), mean [S, groups], rstd [S, groups]); the latter two
+    go to group_norm_backward."""
+    N, F = int(x.shape[0]), int(x.shape[1])
+    S, G = int(ptr.numel()) - 1, int(groups)
+    a = _act(act)
+    _vector(weight, F, torch.float32, "weight")
+    _vector(bias, F, torch.float32, "bias")
+    if out is not None and out.shape != x.shape:
+        raise ValueError("out must have the shape of x")
+    _on_gpu(ptr, x, weight, bias, out)
+    dt, it = _dtype_code(x.dtype), _itype_code(ptr.dtype)
+    xp, ldx = _rows_ptr(x)
+    nb = mp_group_norm_workspace(N, S, F, G, dt, 0)
+    dev = x.device
+    with _on(stream):
+        if out is None:
+            out = torch.empty(N, F, dtype=out_dtype or x.dtype, device=dev)
+        mean = torch.empty(S, G, dtype=torch.float32, device=dev)
+        rstd = torch.empty(S, G, dtype=torch.float32, device=dev)
+        ws = _workspace(nb, dev) if nb else None
+        mp_group_norm(ptr, it, xp, dt, N, S, F, ldx, G, weight, bias, eps, a, out,
+                      _dtype_code(out.dtype), mean, rstd, ws, nb, stream)
+    return out, mean, rstd
+
+
+def group_norm_backward(ptr, x, dout, groups, mean, rstd, *, weight=None, bias=None, act="none",
+                        dx_dtype=None, want_dx=True, want_dw=True, stream=None):
+    """Gradients of group_norm given dout [N, F] (dtype of x): (dx [N, F] of dx_dtype (default x's) or
+    None, dweight [F] fp32 or None, dbias [F] fp32 or None)."""
+    N, F = int(x.shape[0]), int(x.shape[1])
+    S, G = int(ptr.numel()) - 1, int(groups)
+    a = _act(act)
+    _like(dout, x, "dout")
+    _vector(mean, S * G, torch.float32, "mean")
+    _vector(rstd, S * G, torch.float32, "rstd")
+    _vector(weight, F, torch.float32, "weight")
+    _vector(bias, F, torch.float32, "bias")
+    _on_gpu(ptr, x, dout, mean, rstd, weight, bias)
+    dt, it = _dtype_code(x.dtype), _itype_code(ptr.dtype)
+    xp, ldx = _rows_ptr(x)
+    nb = mp_group_norm_workspace(N, S, F, G, dt, 1)
+    dev = x.device
+    with _on(stream):
+        dx = torch.empty(N, F, dtype=dx_dtype or x.dtype, device=dev) if want_dx else None
+        dw = torch.empty(F, dtype=torch.float32, device=dev) if want_dw else None
+        db = torch.empty(F, dtype=torch.float32, device=dev) if want_dw else None
+        ws = _workspace(nb, dev) if nb else None
+        mp_group_norm_backward(ptr, it, xp, dt, dout, N, S, F, ldx, G, weight, bias, mean, rstd, a, dx,
+                               _dtype_code(dx.dtype) if want_dx else MP_F32, dw, db, ws, nb, stream)
+    return dx, dw, db
 
 
 # ---- dropout ------------------------------------------------------------------------------

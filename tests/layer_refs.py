@@ -103,3 +103,58 @@ def route_backward(l, idx, part, dweight, dloss, renorm=True):
                 g[r, idx[r, j]] += w[r, j] * (dw[r, j] - (S[r, 0] if renorm else 0))
                 size[r, idx[r, j]] += w[r, j] * (abs(dw[r, j]) + np.abs(w[r] * dw[r]).sum())
     return np.where(part[:, None], g, 0.0), size
+
+
+# ---- group norm ---------------------------------------------------------------------------
+
+def _erf(v):
+    return torch.erf(torch.from_numpy(np.ascontiguousarray(v))).numpy()
+
+
+def act(z, name):
+    """act(z) and its derivative."""
+    if name == "relu":
+        return np.maximum(z, 0), (z > 0).astype(np.float64)
+    if name == "silu":
+        g = 1 / (1 + np.exp(-z))
+        return z * g, g + z * g * (1 - g)
+    if name == "gelu":
+        g = 0.5 * (1 + _erf(z / math.sqrt(2)))
+        return z * g, g + z * np.exp(-z * z / 2) / math.sqrt(2 * math.pi)
+    return z, np.ones_like(z)
+
+
+def group_norm(ptr, x, groups, weight, bias, eps, name):
+    """A dict of out, mean, rstd, xhat and z for x [N, F] float64."""
+    n, f = x.shape
+    s, w = len(ptr) - 1, f // groups
+    mean, rstd = np.zeros((s, groups)), np.zeros((s, groups))
+    xhat = np.zeros((n, groups, w))
+    for i in range(s):
+        v = x[ptr[i]:ptr[i + 1]].reshape(-1, groups, w)
+        if not v.shape[0]:
+            continue
+        mean[i] = v.mean((0, 2))
+        rstd[i] = 1 / np.sqrt(((v - mean[i][:, None]) ** 2).mean((0, 2)) + eps)
+        xhat[ptr[i]:ptr[i + 1]] = (v - mean[i][:, None]) * rstd[i][:, None]
+    xhat = xhat.reshape(n, f)
+    z = xhat * weight + bias
+    return dict(out=act(z, name)[0], mean=mean, rstd=rstd, xhat=xhat, z=z)
+
+
+def group_norm_backward(ptr, r, dout, groups, weight, name):
+    """dx, dweight, dbias from what group_norm returned."""
+    n, f = dout.shape
+    w = f // groups
+    da = dout * act(r["z"], name)[1]
+    dweight, dbias = (da * r["xhat"]).sum(0), da.sum(0)
+    g = (da * weight).reshape(n, groups, w)
+    xh = r["xhat"].reshape(n, groups, w)
+    dx = np.zeros((n, groups, w))
+    for i in range(len(ptr) - 1):
+        a, b = ptr[i], ptr[i + 1]
+        if a == b:
+            continue
+        m1, m2 = g[a:b].mean((0, 2))[:, None], (g[a:b] * xh[a:b]).mean((0, 2))[:, None]
+        dx[a:b] = r["rstd"][i][:, None] * (g[a:b] - m1 - xh[a:b] * m2)
+    return dx.reshape(n, f), dweight, dbias

@@ -97,3 +97,41 @@ def test_route_workspace():
     for bad in ((-1, 8), (2 ** 31, 8), (8, 0), (8, 1025)):
         with pytest.raises(mp.MPError):
             mp.mp_route_workspace(*bad)
+
+
+NORM = dict(ptr=FAKE, ptr_itype=0, x=FAKE, x_dtype=0, N=10, S=2, F=8, ldx=8, G=2, gamma=None, beta=None,
+            eps=1e-5, act=0, out=FAKE, out_dtype=0, mean=FAKE, rstd=FAKE, ws=None, ws_bytes=0,
+            stream=None)
+NORM_BACKWARD = dict(ptr=FAKE, ptr_itype=0, x=FAKE, x_dtype=0, dout=FAKE, N=10, S=2, F=8, ldx=8, G=2,
+                     gamma=None, beta=None, mean=FAKE, rstd=FAKE, act=0, dx=FAKE, dx_dtype=0,
+                     dgamma=FAKE, dbeta=FAKE, ws=FAKE, ws_bytes=1 << 30, stream=None)
+SHARED = [(-3, dict(ptr_itype=2)), (-3, dict(x_dtype=2)), (-2, dict(N=-1)), (-2, dict(S=0)),
+          (-2, dict(F=0)), (-2, dict(F=65537, ldx=65537)), (-2, dict(G=0)), (-2, dict(G=3)),
+          (-2, dict(G=16)), (-2, dict(ldx=7)), (-2, dict(act=4)), (-2, dict(act=-1)),
+          (-1, dict(ptr=None)), (-1, dict(x=None)), (-1, dict(mean=None)), (-1, dict(rstd=None)),
+          (-8, dict(ptr=FAKE + 4, ptr_itype=1)), (-8, dict(x=FAKE + 2)), (-8, dict(gamma=FAKE + 2)),
+          (-8, dict(beta=FAKE + 1)), (-8, dict(mean=FAKE + 2)), (-8, dict(ws=FAKE + 8))]
+
+
+@pytest.mark.parametrize("status,change", SHARED + [
+    (-3, dict(out_dtype=5)), (-2, dict(eps=-1.0)), (-2, dict(eps=float("nan"))),
+    (-2, dict(eps=float("inf"))), (-1, dict(out=None)), (-8, dict(out=FAKE + 2)),
+    (-1, dict(N=10 ** 6)), (-5, dict(N=10 ** 6, ws=FAKE, ws_bytes=64))])
+def test_group_norm_refusals(status, change):
+    refused("mp_group_norm", NORM, status, **change)
+
+
+@pytest.mark.parametrize("status,change", SHARED + [
+    (-3, dict(dx_dtype=5)), (-1, dict(dout=None)), (-1, dict(dgamma=None)), (-1, dict(dbeta=None)),
+    (-1, dict(dx=None, dgamma=None, dbeta=None)), (-8, dict(dout=FAKE + 2)), (-8, dict(dx=FAKE + 2)),
+    (-1, dict(ws=None)), (-5, dict(ws_bytes=16))])
+def test_group_norm_backward_refusals(status, change):
+    refused("mp_group_norm_backward", NORM_BACKWARD, status, **change)
+
+
+def test_group_norm_workspace():
+    assert mp.mp_group_norm_workspace(100, 5, 64, 8, 0, False) == 0
+    assert mp.mp_group_norm_workspace(10 ** 6, 5, 64, 8, 0, False) > 0
+    assert mp.mp_group_norm_workspace(100, 5, 64, 8, 1, True) > 0
+    with pytest.raises(mp.MPError):
+        mp.mp_group_norm_workspace(100, 5, 64, 7, 0, False)
