@@ -157,6 +157,51 @@ int mp_route_backward(const void* logits, int dtype, int64_t N, int64_t E, int64
                       const float* weight, const int32_t* counts, const float* dweight,
                       const float* dloss, void* dlogits, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Microscaled 4-bit floating point (OCP Microscaling Formats, 2023: MXFP4).
+ * A row of K values is cut into blocks of 32, KB = ceil(K / 32) of them.  A
+ * block has one scale byte s (E8M0: 2^(s - 127); 255: every value is NaN)
+ * and 32 four-bit codes (E2M1: sign, and 0, 0.5, 1, 1.5, 2, 3, 4 or 6).
+ * Layout of a table of N rows: codes [N, KB * 16] bytes, element i of a row in
+ * byte i / 2, the lower nibble first; scales [N, KB] bytes.  The places past
+ * K of a last block hold code 0.
+ * Quantisation: the scale of a block is 2^(floor(log2 max|x|) - 2), no less
+ * than 2^-127 (a block of zeros has s = 0); values are divided by it, rounded
+ * to nearest with ties to the even code, and saturate at 6.  A block that
+ * holds an infinity or NaN gets s = 255.
+ * ------------------------------------------------------------------------- */
+
+/* x [N, K] of dtype, row stride ldx -> codes and scales (both or neither), and
+ * the values that they stand for, [N, K] contiguous of dtype, or NULL (for
+ * training with quantised values; exact in either type).  0 <= N <=
+ * INT32_MAX, 1 <= K <= 65536.  codes 16-byte aligned. */
+int mp_mx_quantize(const void* x, int dtype, int64_t N, int64_t K, int64_t ldx, uint8_t* codes,
+                   uint8_t* scales, void* values, void* stream);
+
+/* The values that codes and scales stand for: out [N, K] contiguous of dtype. */
+int mp_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t N, int64_t K,
+                     void* out, int dtype, void* stream);
+
+/* Workspace bytes of mp_mx_segment_matmul (the rows' codes and scales). */
+int mp_mx_segment_matmul_workspace(int64_t N, int64_t K, size_t* bytes);
+
+/* out[r, o] = sum over k of q(x)[r, k] * W[t][o, k] for the rows r of segment t:
+ * mp_segment_matmul for serving, on 4-bit matrix cores, with W quantised
+ * along its input channels ([Fo, K] a type: transposed against mp.h) and
+ * the rows of x quantised (as mp_mx_quantize does) on the way.
+ *   seg     [T+1] of seg_itype on the DEVICE (the rowptr of a dispatch):
+ *           seg[0] = 0, non-decreasing, seg[T] = N (offsets outside [0, N]
+ *           are taken as the nearest in it; rows of no segment are not written).
+ *   x       [N, K] of x_dtype, row stride ldx.
+ *   w_codes [T, Fo, KB * 16], w_scales [T, Fo, KB].
+ *   out     [N, Fo] contiguous of out_dtype, from fp32 sums.
+ * Sizes: 0 <= N <= INT32_MAX, 1 <= T <= 4096, 1 <= K, Fo <= 65536; w_codes and
+ * ws 16-byte aligned. */
+int mp_mx_segment_matmul(const void* seg, int seg_itype, int64_t T, const void* x, int x_dtype,
+                         int64_t N, int64_t K, int64_t ldx, const uint8_t* w_codes,
+                         const uint8_t* w_scales, int64_t Fo, void* out, int out_dtype, void* ws,
+                         size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

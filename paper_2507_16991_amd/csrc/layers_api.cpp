@@ -260,4 +260,66 @@ int mp_route_backward(const void* logits, int dtype, int64_t N, int64_t E, int64
     return hip_status(launch_route_backward(P, dtype, as_stream(stream)));
 }
 
+int mp_mx_quantize(const void* x, int dtype, int64_t N, int64_t K, int64_t ldx, uint8_t* codes,
+                   uint8_t* scales, void* values, void* stream) {
+    if (!valid_dtype(dtype)) return MP_ERR_DTYPE;
+    if (N < 0 || N > INT32_MAX || K < 1 || K > kMaxF || ldx < K) return MP_ERR_SIZE;
+    if ((N > 0 && !x) || !codes != !scales || (N > 0 && !codes && !values)) return MP_ERR_NULL;
+    if (!aligned(x, elem(dtype)) || !aligned(codes, 16) || !aligned(values, elem(dtype)))
+        return MP_ERR_ALIGN;
+    return hip_status(
+        launch_mx_quantize(x, dtype, N, K, ldx, codes, scales, values, as_stream(stream)));
+}
+
+int mp_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t N, int64_t K, void* out,
+                     int dtype, void* stream) {
+    if (!valid_dtype(dtype)) return MP_ERR_DTYPE;
+    if (N < 0 || N > INT32_MAX || K < 1 || K > kMaxF) return MP_ERR_SIZE;
+    if (N > 0 && (!codes || !scales || !out)) return MP_ERR_NULL;
+    if (!aligned(codes, 16) || !aligned(out, elem(dtype))) return MP_ERR_ALIGN;
+    return hip_status(launch_mx_dequantize(codes, scales, N, K, out, dtype, as_stream(stream)));
+}
+
+int mp_mx_segment_matmul_workspace(int64_t N, int64_t K, size_t* bytes) {
+    if (!bytes) return MP_ERR_NULL;
+    if (N < 0 || N > INT32_MAX || K < 1 || K > kMaxF) return MP_ERR_SIZE;
+    const size_t blocks = (size_t)N * (size_t)ceil_div(K, 32);
+    *bytes = align_up(blocks * 16, 256) + align_up(blocks, 256);
+    return MP_OK;
+}
+
+int mp_mx_segment_matmul(const void* seg, int seg_itype, int64_t T, const void* x, int x_dtype,
+                         int64_t N, int64_t K, int64_t ldx, const uint8_t* w_codes,
+                         const uint8_t* w_scales, int64_t Fo, void* out, int out_dtype, void* ws,
+                         size_t ws_bytes, void* stream) {
+    if (!valid_itype(seg_itype) || !valid_dtype(x_dtype) || !valid_dtype(out_dtype))
+        return MP_ERR_DTYPE;
+    if (N < 0 || N > INT32_MAX || T < 1 || T > 4096 || K < 1 || K > kMaxF || ldx < K || Fo < 1 ||
+        Fo > kMaxF)
+        return MP_ERR_SIZE;
+    if (!seg || !w_codes || !w_scales || (N > 0 && (!x || !out || !ws))) return MP_ERR_NULL;
+    if (!aligned(seg, seg_itype == MP_I64 ? 8 : 4) || !aligned(x, elem(x_dtype)) ||
+        !aligned(w_codes, 16) || !aligned(out, elem(out_dtype)) || !aligned(ws, 16))
+        return MP_ERR_ALIGN;
+    size_t need = 0;
+    mp_mx_segment_matmul_workspace(N, K, &need);
+    if (ws_bytes < need) return MP_ERR_WORKSPACE;
+    MxParams P{};
+    P.seg = seg;
+    P.seg64 = seg_itype == MP_I64;
+    P.T = T;
+    P.N = N;
+    P.x = x;
+    P.ldx = ldx;
+    P.K = (int)K;
+    P.KB = (int)ceil_div(K, 32);
+    P.Fo = (int)Fo;
+    P.w_codes = w_codes;
+    P.w_scales = w_scales;
+    P.x_codes = static_cast<uint8_t*>(ws);
+    P.x_scales = P.x_codes + align_up((size_t)N * (size_t)P.KB * 16, 256);
+    P.out = out;
+    return hip_status(launch_mx_product(P, x_dtype, out_dtype, as_stream(stream)));
+}
+
 }  // extern "C"

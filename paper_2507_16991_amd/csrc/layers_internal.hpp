@@ -175,4 +175,24 @@ int route_blocks(int64_t N, int64_t E);
 hipError_t launch_route(const RouteParams& p, int dtype, hipStream_t s);
 hipError_t launch_route_backward(const RouteParams& p, int dtype, hipStream_t s);
 
+// ---- microscaled 4-bit floating point (mx.hip) -------------------------------------
+struct MxParams {
+    const void* seg;
+    int seg64;
+    int64_t T, N;
+    const void* x;
+    int64_t ldx;
+    int K, KB, Fo;
+    const uint8_t* w_codes;   // [T, Fo, KB * 16]
+    const uint8_t* w_scales;  // [T, Fo, KB]
+    uint8_t* x_codes;         // workspace [N, KB * 16]
+    uint8_t* x_scales;        // workspace [N, KB]
+    void* out;
+};
+hipError_t launch_mx_quantize(const void* x, int dtype, int64_t N, int64_t K, int64_t ldx,
+                              uint8_t* codes, uint8_t* scales, void* values, hipStream_t s);
+hipError_t launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t N, int64_t K,
+                                void* out, int dtype, hipStream_t s);
+hipError_t launch_mx_product(const MxParams& p, int x_dtype, int out_dtype, hipStream_t s);
+
 }  // namespace mp

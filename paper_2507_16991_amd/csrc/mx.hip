@@ -1,0 +1,580 @@
+// Microscaled 4-bit floating point (MXFP4): quantisation, and the product of row
+// segments with 4-bit weights (include/mp_layers.h states format and layout).
+//
+// Products run on v_mfma_scale_f32_*_f8f6f4, whose operands are 32 codes (16
+// bytes, along k) and their block's scale exponent from each lane: lane l of
+// the 32x32x64 form holds row l % 32 and block l / 32, of the 16x16x128 form
+// row l % 16 and block l / 16; the accumulators are those of the bf16 forms.
+// Weights are the first operand and rows of x the second, so that a lane's
+// accumulators are neighbouring output columns of one row.
+//
+// x is quantised first (a quarter of its bytes); two kernels share the products out:
+//   * mx_thin: segments of few rows: bound by reading the weights, which go
+//     straight to registers, k split over the wavefronts of a workgroup;
+//   * mx_tiles: tiles staged through LDS by asynchronous loads.
+#include "layers_internal.hpp"
+
+namespace mp {
+namespace {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kBlock = 256;
+constexpr int kMxBlock = 32;      // values under one scale
+constexpr int kFp4 = 4;           // operand format of the MFMA: E2M1
+constexpr uint32_t kNanScale = 255;
+
+// ---- quantisation ------------------------------------------------------------------
+// Four neighbouring lanes have the 32 values of a block, eight each.
+
+// Largest over the four lanes of a quad.
+__device__ inline uint32_t quad_max(uint32_t x) {
+    uint32_t y = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, true);
+    x = x > y ? x : y;
+    y = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, true);
+    return x > y ? x : y;
+}
+
+// The scale byte for a block whose largest magnitude has these float bits:
+// floor(log2) - 2 with E8M0's bias is the exponent field less two.
+__device__ inline uint32_t scale_of(uint32_t bits) {
+    const uint32_t e = bits >> 23;
+    return e == 255 ? kNanScale : (e > 2 ? e - 2 : 0);
+}
+// 2^(s - 127) (s = 0 is subnormal); NaN for 255.
+__device__ inline float scale_value(uint32_t s) {
+    return __uint_as_float(s == kNanScale ? 0x7FC00000u : (s ? s << 23 : 0x00400000u));
+}
+
+// Eight values -> their block's scale and eight codes.  The conversion divides by the
+// scale, rounds to nearest even and saturates.
+template <typename T>
+__device__ inline uint32_t quantize8(const RawOf<T, 8>& r, uint32_t& s) {
+    uint32_t m = 0, c = 0;
+    if constexpr (sizeof(typename T::raw) == 2) {
+        u16x2 h = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            h = __builtin_elementwise_max(h, __builtin_bit_cast(u16x2, r.w[i] & 0x7FFF7FFFu));
+        m = (uint32_t)(h.x > h.y ? h.x : h.y) << 16;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t a = r.w[i] & 0x7FFFFFFFu;
+            m = m > a ? m : a;
+        }
+    }
+    s = scale_of(quad_max(m));
+    const float f = scale_value(s == kNanScale ? 127u : s);
+    if constexpr (sizeof(typename T::raw) == 2) {
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, r.w[0]), f, 0);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, r.w[1]), f, 1);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, r.w[2]), f, 2);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, r.w[3]), f, 3);
+    } else {
+        float v[8];
+        to_floats<T, 8>(r, v);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0], v[1], f, 0);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], f, 1);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], f, 2);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], f, 3);
+    }
+    return c;
+}
+
+// The value of a code under a scale: magnitude bits e1 e0 m are 0 or 0.5 (e = 0), or
+// (1 + m / 2) 2^(e - 1); exact, and exact in bf16.
+__device__ inline float value_of(uint32_t code, float scale) {
+    const uint32_t e = (code >> 1) & 3, m = code & 1;
+    const float a = e ? __uint_as_float(((126 + e) << 23) | (m << 22)) : (m ? 0.5f : 0.f);
+    return (code & 8 ? -a : a) * scale;
+}
+
+// Values k0 .. k0+7 of a row of K, zero past its end.
+template <typename T>
+__device__ inline RawOf<T, 8> load8(const typename T::raw* p, int k0, int K) {
+    if (k0 + 8 <= K) return load_raw<T, 8>(p + k0);
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = k0 + i < K ? load_one<T>(p + k0 + i) : 0.f;
+    return from_floats<T, 8>(v);
+}
+
+template <typename T>
+__device__ inline void store8(typename T::raw* p, int k0, int K, const float (&v)[8]) {
+    if (k0 + 8 <= K) {
+        store_floats<T, 8>(p + k0, v);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (k0 + i < K) store_one<T>(p + k0 + i, v[i]);
+}
+
+// A workgroup takes rows_per_block rows, a thread eight values of one.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void mx_quantize(const typename T::raw* x, int64_t N, int K,
+                                                      int64_t ldx, int rows_per_block,
+                                                      uint32_t* codes, uint8_t* scales,
+                                                      typename T::raw* values) {
+    const int per = 4 * ((K + kMxBlock - 1) / kMxBlock);
+    const int64_t groups = (N + rows_per_block - 1) / rows_per_block;
+    for (int64_t g = blockIdx.x; g < groups; g += gridDim.x) {
+        const int64_t r0 = g * rows_per_block;
+        const uint32_t n = (uint32_t)(N - r0 < rows_per_block ? N - r0 : rows_per_block) * per;
+        for (uint32_t l = threadIdx.x; l < n; l += kBlock) {  // (n is a multiple of 4: whole quads)
+            const uint32_t dr = l / (uint32_t)per, j = l - dr * per;
+            const int64_t r = r0 + dr;
+            uint32_t s;
+            const uint32_t c = quantize8<T>(load8<T>(x + r * ldx, 8 * j, K), s);
+            if (codes) {
+                codes[r * per + j] = c;
+                if ((j & 3) == 0) scales[r * (per / 4) + j / 4] = (uint8_t)s;
+            }
+            if (values && 8 * (int)j < K) {
+                const float f = scale_value(s);
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = value_of(c >> (4 * i), f);
+                store8<T>(values + r * K, 8 * j, K, v);
+            }
+        }
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kBlock) void mx_dequantize(const uint32_t* codes,
+                                                        const uint8_t* scales, int64_t N, int K,
+                                                        int rows_per_block,
+                                                        typename T::raw* out) {
+    const int per = 4 * ((K + kMxBlock - 1) / kMxBlock);
+    const int64_t groups = (N + rows_per_block - 1) / rows_per_block;
+    for (int64_t g = blockIdx.x; g < groups; g += gridDim.x) {
+        const int64_t r0 = g * rows_per_block;
+        const uint32_t n = (uint32_t)(N - r0 < rows_per_block ? N - r0 : rows_per_block) * per;
+        for (uint32_t l = threadIdx.x; l < n; l += kBlock) {
+            const uint32_t dr = l / (uint32_t)per, j = l - dr * per;
+            if (8 * (int)j >= K) continue;
+            const int64_t r = r0 + dr;
+            const uint32_t c = codes[r * per + j];
+            const float f = scale_value(scales[r * (per / 4) + j / 4]);
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = value_of(c >> (4 * i), f);
+            store8<T>(out + r * K, 8 * j, K, v);
+        }
+    }
+}
+
+// ---- segments -------------------------------------------------------------------------
+__device__ inline int64_t seg_at(const MxParams& P, int64_t t) {
+    const int64_t v = P.seg64 ? static_cast<const int64_t*>(P.seg)[t]
+                              : (int64_t)static_cast<const int32_t*>(P.seg)[t];
+    return v < 0 ? 0 : (v > P.N ? P.N : v);
+}
+
+// Tile `tile` of the segments' rows in tiles of BM (no tile has rows of two):
+// its segment and rows, or t = -1 past the last.  64 segments a step.
+struct RowTile {
+    int64_t t, r0, r1;
+};
+__device__ inline RowTile row_tile(const MxParams& P, int64_t tile, int BM) {
+    const int lane = threadIdx.x & 63;
+    int64_t before = 0;
+    for (int64_t t0 = 0; t0 < P.T; t0 += 64) {
+        const int64_t t = t0 + lane;
+        const int64_t b = t < P.T ? seg_at(P, t) : 0, e = t < P.T ? seg_at(P, t + 1) : 0;
+        const int n = e > b ? (int)((e - b + BM - 1) / BM) : 0;
+        int sum = n;  // tiles up to and with this lane's segment
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int v = __shfl_up(sum, o);
+            if (lane >= o) sum += v;
+        }
+        const int64_t end = before + sum;
+        const uint64_t hit = __ballot(n > 0 && tile < end);
+        if (hit) {
+            const int i = __builtin_ctzll(hit);
+            // the lane's values, made uniform
+            const int64_t ti = t0 + i, bi = seg_at(P, ti), ei = seg_at(P, ti + 1);
+            const int ni = __shfl(n, i);
+            const int64_t first = before + __shfl(sum, i) - ni;
+            const int64_t r0 = bi + (tile - first) * BM;
+            return RowTile{ti, r0, r0 + BM < ei ? r0 + BM : ei};
+        }
+        before += __shfl(sum, 63);
+    }
+    return RowTile{-1, 0, 0};
+}
+
+__device__ inline i32x8 operand(const uint4& c) {
+    return i32x8{(int)c.x, (int)c.y, (int)c.z, (int)c.w, 0, 0, 0, 0};
+}
+
+template <bool BF>
+__device__ inline void store4(void* out, int64_t at, const float (&v)[4]) {
+    if (BF) store_floats<BF16, 4>(static_cast<uint16_t*>(out) + at, v);
+    else store_floats<F32, 4>(static_cast<float*>(out) + at, v);
+}
+template <bool BF>
+__device__ inline void store_col(void* out, int64_t at, float v) {
+    if (BF) store_one<BF16>(static_cast<uint16_t*>(out) + at, v);
+    else store_one<F32>(static_cast<float*>(out) + at, v);
+}
+
+// ---- tiles ------------------------------------------------------------------------------
+// A workgroup of WM x WN wavefronts has 32 FM WM output columns x 32 FN WN rows, a
+// wavefront FM x FN products of 32 x 32.  k in steps of 8 blocks (128 bytes a row),
+// two buffers: while one is multiplied, asynchronous loads fill the other.
+// In LDS the 16-byte pieces of row r lie at piece ^ (r % 8), so that the
+// lanes of a fragment (32 rows, one piece) spread over the banks.
+constexpr int kStep = 8;  // blocks of a step
+constexpr int kRowBytes = kStep * 16;
+
+template <int ROWS>
+struct TileBuffer {
+    uint8_t codes[ROWS * kRowBytes];
+    uint2 scales[ROWS];
+};
+
+// A workgroup's loads of ROWS rows of codes and scales, blocks kb0 .. kb0+7 at a
+// time.  Rows past `rows` repeat the last one (their products are not stored),
+// blocks past KB the last one, under scales of 0: both factors are then 2^-127,
+// and such products vanish.
+template <int ROWS, int WAVES>
+struct TileLoader {
+    static constexpr int PER = ROWS / 8 / WAVES;  // loads of a wavefront, 8 rows each
+    const uint8_t* codes;
+    const uint8_t* scales;  // this thread's row
+    uint32_t off[PER];
+    int KB, piece;
+    uint64_t s;
+
+    // stride: bytes from one row's scales to the next
+    __device__ TileLoader(const uint8_t* c, const uint8_t* sc, int rows, int kb, int stride) {
+        const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, tid = threadIdx.x;
+        codes = c;
+        KB = kb;
+        piece = (lane & 7) ^ (lane >> 3);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int r = (w * PER + i) * 8 + (lane >> 3);
+            off[i] = (uint32_t)((r < rows ? r : rows - 1) * kb) * 16u;
+        }
+        scales = sc + (int64_t)(tid < rows ? tid : rows - 1) * stride;
+        s = 0;
+    }
+    __device__ void fetch_codes(uint8_t* lds, int kb0) const {
+        const int w = threadIdx.x >> 6;
+        const uint32_t at = (uint32_t)(kb0 + piece < KB ? kb0 + piece : KB - 1) * 16u;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            __builtin_amdgcn_global_load_lds(
+                (const __attribute__((address_space(1))) void*)(codes + (off[i] + at)),
+                (__attribute__((address_space(3))) void*)(lds + (w * PER + i) * 8 * kRowBytes), 16,
+                0, 0);
+    }
+    // KB >= 8: eight bytes that end with the row at the latest
+    __device__ void fetch_scales(int kb0) {
+        const int k = kb0 + kStep <= KB ? kb0 : KB - kStep;
+        __builtin_memcpy(&s, scales + k, 8);
+    }
+    __device__ uint64_t scales_of(int kb0) const {
+        const int past = kb0 + kStep - KB;
+        return past > 0 ? s >> (8 * past) : s;
+    }
+    __device__ void fetch_few_scales() {  // KB < 8
+        s = 0;
+        for (int i = 0; i < KB; ++i) s |= (uint64_t)scales[i] << (8 * i);
+    }
+};
+
+template <int FM, int FN, int BM, int BN>
+__device__ inline void multiply(const TileBuffer<BM>& W, const TileBuffer<BN>& X, int wm,
+                                int wn, int lane, f32x16 (&acc)[FM][FN]) {
+    const int half = lane >> 5, row = lane & 31;
+    uint2 sw[FM], sx[FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+        sw[i] = W.scales[(wm * FM + i) * 32 + row];
+        sw[i].x >>= 8 * half;  // now byte 2 (s % 2) is the scale of block 2 s + half
+        sw[i].y >>= 8 * half;
+    }
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        sx[j] = X.scales[(wn * FN + j) * 32 + row];
+        sx[j].x >>= 8 * half;
+        sx[j].y >>= 8 * half;
+    }
+    // the next fragments are read while these are multiplied; the scheduling
+    // barriers keep more of them from being read ahead, which spills
+    uint4 a[2][FM], b[2][FN];
+    const auto read = [&](int s, uint4 (&fa)[FM], uint4 (&fb)[FN]) {
+        const int at = ((2 * s + half) ^ (row & 7)) * 16;
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+            fa[i] = *reinterpret_cast<const uint4*>(
+                &W.codes[((wm * FM + i) * 32 + row) * kRowBytes + at]);
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+            fb[j] = *reinterpret_cast<const uint4*>(
+                &X.codes[((wn * FN + j) * 32 + row) * kRowBytes + at]);
+    };
+    read(0, a[0], b[0]);
+#pragma unroll
+    for (int s = 0; s < kStep / 2; ++s) {
+        if (s + 1 < kStep / 2) read(s + 1, a[(s + 1) & 1], b[(s + 1) & 1]);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                const int si = (int)(s < 2 ? sw[i].x : sw[i].y), sj = (int)(s < 2 ? sx[j].x : sx[j].y);
+                const i32x8 va = operand(a[s & 1][i]), vb = operand(b[s & 1][j]);
+                if (s & 1)
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                        va, vb, acc[i][j], kFp4, kFp4, 2, si, 2, sj);
+                else
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                        va, vb, acc[i][j], kFp4, kFp4, 0, si, 0, sj);
+            }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    // the products stay here: the compiler would sink them past the workgroup's
+    // barrier, with all fragments in registers until then
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) asm volatile("" : "+v"(acc[i][j]));
+}
+
+template <int FM, int FN, int WM, int WN, bool BF>
+__global__ __launch_bounds__(64 * WM * WN) void mx_tiles(MxParams P, int64_t row_tiles,
+                                                         int col_tiles) {
+    constexpr int BM = 32 * FM * WM, BN = 32 * FN * WN;  // output columns, rows
+    static_assert(64 * WM * WN >= BM && 64 * WM * WN >= BN, "a thread a row of scales");
+    __shared__ __attribute__((aligned(16))) TileBuffer<BM> W0, W1;
+    __shared__ __attribute__((aligned(16))) TileBuffer<BN> X0, X1;
+    // Workgroups go to the XCDs in turn; each XCD has a run of tiles, in
+    // bands of eight row tiles, so that its L2 serves rows and columns again.
+    const int64_t total = row_tiles * col_tiles, per = (total + 7) / 8;
+    const int64_t lin = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    if (lin >= total) return;
+    const int64_t band = lin / (8 * col_tiles), in = lin - band * 8 * col_tiles;
+    const int64_t high = row_tiles - band * 8 < 8 ? row_tiles - band * 8 : 8;
+    const int64_t rt = band * 8 + in % high;
+    const int ct = (int)(in / high);
+    const RowTile tile = row_tile(P, rt, BN);
+    if (tile.t < 0) return;
+    const int KB = P.KB, rows = (int)(tile.r1 - tile.r0);
+    const int c0 = ct * BM, cols = P.Fo - c0 < BM ? P.Fo - c0 : BM;
+    const uint8_t* wc = P.w_codes + (tile.t * P.Fo + c0) * KB * 16;
+    const uint8_t* ws = P.w_scales + (tile.t * P.Fo + c0) * KB;
+    const uint8_t* xc = P.x_codes + tile.r0 * KB * 16;
+    const uint8_t* xs = P.x_scales + tile.r0 * KB;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, wm = w % WM, wn = w / WM;
+
+    f32x16 acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+
+    TileLoader<BM, WM * WN> lw(wc, ws, cols, KB, KB);
+    TileLoader<BN, WM * WN> lx(xc, xs, rows, KB, KB);
+    const auto settle = [&](TileBuffer<BM>& Wb, TileBuffer<BN>& Xb, int kb0) {
+        if (tid < BM) Wb.scales[tid] = __builtin_bit_cast(uint2, lw.scales_of(kb0));
+        if (tid < BN) Xb.scales[tid] = __builtin_bit_cast(uint2, lx.scales_of(kb0));
+        __builtin_amdgcn_s_waitcnt(0);  // the asynchronous loads too
+        __syncthreads();
+    };
+    const auto fetch = [&](TileBuffer<BM>& Wb, TileBuffer<BN>& Xb, int kb0) {
+        lw.fetch_codes(Wb.codes, kb0);
+        lx.fetch_codes(Xb.codes, kb0);
+        lw.fetch_scales(kb0);
+        lx.fetch_scales(kb0);
+    };
+    const int steps = (KB + kStep - 1) / kStep;
+    if (KB >= kStep) {
+        fetch(W0, X0, 0);
+        settle(W0, X0, 0);
+    } else {
+        lw.fetch_codes(W0.codes, 0);
+        lx.fetch_codes(X0.codes, 0);
+        lw.fetch_few_scales();
+        lx.fetch_few_scales();
+        if (tid < BM) W0.scales[tid] = __builtin_bit_cast(uint2, lw.s);
+        if (tid < BN) X0.scales[tid] = __builtin_bit_cast(uint2, lx.s);
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+    }
+    int k = 0;
+    for (; k + 1 < steps; k += 2) {
+        fetch(W1, X1, (k + 1) * kStep);
+        multiply<FM, FN, BM, BN>(W0, X0, wm, wn, lane, acc);
+        settle(W1, X1, (k + 1) * kStep);
+        if (k + 2 < steps) fetch(W0, X0, (k + 2) * kStep);
+        multiply<FM, FN, BM, BN>(W1, X1, wm, wn, lane, acc);
+        if (k + 2 < steps) settle(W0, X0, (k + 2) * kStep);
+    }
+    if (k < steps) multiply<FM, FN, BM, BN>(W0, X0, wm, wn, lane, acc);
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        const int r = (wn * FN + j) * 32 + (lane & 31);
+        if (r >= rows) continue;
+        const int64_t at = (tile.r0 + r) * P.Fo + c0;
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int c = (wm * FM + i) * 32 + 8 * q + 4 * (lane >> 5);
+                const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2],
+                                    acc[i][j][4 * q + 3]};
+                if (c + 4 <= cols) {
+                    store4<BF>(P.out, at + c, v);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (c + e < cols) store_col<BF>(P.out, at + c + e, v[e]);
+                }
+            }
+    }
+}
+
+// ---- few rows ------------------------------------------------------------------------------
+// A workgroup has 16 output columns and up to 16 rows of a segment; its four
+// wavefronts take steps of four blocks (k = 128) in turn, weights straight from
+// memory, kThinDeep loads in flight, and their sums are added in LDS.
+constexpr int kThinRows = 16, kThinCols = 16, kThinDeep = 4;
+
+template <bool BF>
+__global__ __launch_bounds__(kBlock) void mx_thin(MxParams P) {
+    __shared__ f32x4 s_acc[4][kWave];
+    const RowTile tile = row_tile(P, blockIdx.y, kThinRows);
+    if (tile.t < 0) return;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int KB = P.KB, rows = (int)(tile.r1 - tile.r0);
+    const int c0 = blockIdx.x * kThinCols, cols = P.Fo - c0 < kThinCols ? P.Fo - c0 : kThinCols;
+    const int row = lane & 15, blk = lane >> 4;
+    const int64_t wr = tile.t * P.Fo + c0 + (row < cols ? row : cols - 1);
+    const int64_t xr = tile.r0 + (row < rows ? row : rows - 1);
+    const uint4* wc = reinterpret_cast<const uint4*>(P.w_codes) + wr * KB;
+    const uint4* xc = reinterpret_cast<const uint4*>(P.x_codes) + xr * KB;
+    const uint8_t* ws = P.w_scales + wr * KB;
+    const uint8_t* xs = P.x_scales + xr * KB;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int kb0 = w * 4; kb0 < KB; kb0 += 16 * kThinDeep) {
+        uint4 a[kThinDeep], b[kThinDeep];
+        int sa[kThinDeep], sb[kThinDeep];
+#pragma unroll
+        for (int i = 0; i < kThinDeep; ++i) {
+            const int kb = kb0 + 16 * i + blk;
+            const bool in = kb < KB;
+            const int k = in ? kb : KB - 1;
+            a[i] = wc[k];
+            b[i] = xc[k];
+            sa[i] = in ? ws[k] : 0;  // (2^-127 on both sides: products vanish)
+            sb[i] = in ? xs[k] : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < kThinDeep; ++i)
+            acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                operand(a[i]), operand(b[i]), acc, kFp4, kFp4, 0, sa[i], 0, sb[i]);
+    }
+    s_acc[w][lane] = acc;
+    __syncthreads();
+    if (w) return;
+    f32x4 s = s_acc[0][lane];
+#pragma unroll
+    for (int i = 1; i < 4; ++i) s += s_acc[i][lane];
+    if (row >= rows) return;
+    const int64_t at = (tile.r0 + row) * P.Fo + c0;
+    const int c = 4 * blk;
+    const float v[4] = {s[0], s[1], s[2], s[3]};
+    if (c + 4 <= cols) {
+        store4<BF>(P.out, at + c, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (c + e < cols) store_col<BF>(P.out, at + c + e, v[e]);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_mx_quantize(const void* x, int dtype, int64_t N, int64_t K, int64_t ldx,
+                              uint8_t* codes, uint8_t* scales, void* values, hipStream_t s) {
+    if (N <= 0) return hipSuccess;
+    const int64_t per = 4 * ceil_div(K, kMxBlock);
+    const int64_t rpb = per >= 4 * kBlock ? 1 : 4 * kBlock / per;
+    const int64_t groups = ceil_div(N, rpb);
+    const dim3 g((unsigned)(groups < (1 << 22) ? groups : (1 << 22))), b(kBlock);
+    if (dtype == MP_BF16)
+        hipLaunchKernelGGL(mx_quantize<BF16>, g, b, 0, s, static_cast<const uint16_t*>(x), N, (int)K,
+                           ldx, (int)rpb, reinterpret_cast<uint32_t*>(codes), scales,
+                           static_cast<uint16_t*>(values));
+    else
+        hipLaunchKernelGGL(mx_quantize<F32>, g, b, 0, s, static_cast<const float*>(x), N, (int)K,
+                           ldx, (int)rpb, reinterpret_cast<uint32_t*>(codes), scales,
+                           static_cast<float*>(values));
+    return hipGetLastError();
+}
+
+hipError_t launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t N, int64_t K,
+                                void* out, int dtype, hipStream_t s) {
+    if (N <= 0) return hipSuccess;
+    const int64_t per = 4 * ceil_div(K, kMxBlock);
+    const int64_t rpb = per >= 4 * kBlock ? 1 : 4 * kBlock / per;
+    const int64_t groups = ceil_div(N, rpb);
+    const dim3 g((unsigned)(groups < (1 << 22) ? groups : (1 << 22))), b(kBlock);
+    const uint32_t* c = reinterpret_cast<const uint32_t*>(codes);
+    if (dtype == MP_BF16)
+        hipLaunchKernelGGL(mx_dequantize<BF16>, g, b, 0, s, c, scales, N, (int)K, (int)rpb,
+                           static_cast<uint16_t*>(out));
+    else
+        hipLaunchKernelGGL(mx_dequantize<F32>, g, b, 0, s, c, scales, N, (int)K, (int)rpb,
+                           static_cast<float*>(out));
+    return hipGetLastError();
+}
+
+// Tiles of BM rows that segments of N rows can have at most: every segment that
+// has rows may end in a part of one.
+static int64_t row_tiles_bound(const MxParams& p, int64_t BM) {
+    return p.N / BM + (p.T < p.N ? p.T : p.N);
+}
+
+template <int FM, int FN, int WM, int WN>
+static hipError_t tiles(const MxParams& p, int bf, hipStream_t s) {
+    const int64_t rt = row_tiles_bound(p, 32 * FN * WN), ct = ceil_div(p.Fo, 32 * FM * WM);
+    const int64_t grid = ceil_div(rt * ct, 8) * 8;
+    if (grid > INT32_MAX) return hipErrorInvalidValue;
+    const dim3 g((unsigned)grid), b(64 * WM * WN);
+    if (bf) hipLaunchKernelGGL((mx_tiles<FM, FN, WM, WN, true>), g, b, 0, s, p, rt, (int)ct);
+    else hipLaunchKernelGGL((mx_tiles<FM, FN, WM, WN, false>), g, b, 0, s, p, rt, (int)ct);
+    return hipGetLastError();
+}
+
+hipError_t launch_mx_product(const MxParams& p, int x_dtype, int out_dtype, hipStream_t s) {
+    if (p.N <= 0) return hipSuccess;
+    const int bf = out_dtype == MP_BF16;
+    hipError_t e = launch_mx_quantize(p.x, x_dtype, p.N, p.K, p.ldx, p.x_codes, p.x_scales, nullptr,
+                                      s);
+    if (e != hipSuccess) return e;
+    // few rows a segment: the weights are what is read
+    const int64_t thin = row_tiles_bound(p, kThinRows);
+    if (p.N <= 16 * p.T + 16 && thin <= 65535) {
+        const dim3 g((unsigned)ceil_div(p.Fo, kThinCols), (unsigned)thin), b(kBlock);
+        if (bf) hipLaunchKernelGGL(mx_thin<true>, g, b, 0, s, p);
+        else hipLaunchKernelGGL(mx_thin<false>, g, b, 0, s, p);
+        return hipGetLastError();
+    }
+    const int64_t big = row_tiles_bound(p, 256) * ceil_div(p.Fo, 256);
+    return big >= 256 ? tiles<4, 2, 2, 4>(p, bf, s) : tiles<2, 2, 2, 2>(p, bf, s);
+}
+
+}  // namespace mp

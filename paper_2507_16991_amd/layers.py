@@ -17,7 +17,9 @@ from . import (MP_F32, _bytes, _check, _dtype_code, _itype_code, _ptr, _rows_ptr
 
 __all__ = ["MP_ACT", "mp_group_norm_workspace", "mp_group_norm", "mp_group_norm_backward",
            "group_norm", "group_norm_backward", "mp_dropout", "dropout", "dropout_backward", "mp_route_workspace", "mp_route",
-           "mp_route_backward", "route", "route_backward"]
+           "mp_route_backward", "route", "route_backward", "mp_mx_quantize", "mp_mx_dequantize",
+           "mp_mx_segment_matmul_workspace", "mp_mx_segment_matmul", "mx_quantize", "mx_dequantize",
+           "mx_segment_matmul"]
 
 MP_ACT = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 
@@ -41,7 +43,13 @@ def _layers():
         L.mp_route_workspace.argtypes = [i64, i64, psz]
         L.mp_route.argtypes = [p, i32, i64, i64, i64, i64, p, i32, p, p, p, p, p, sz, p]
         L.mp_route_backward.argtypes = [p, i32, i64, i64, i64, i64, p, i32, p, p, p, p, p, p, p]
-        for name in ("mp_group_norm_workspace", "mp_group_norm", "mp_group_norm_backward",
+        L.mp_mx_quantize.argtypes = [p, i32, i64, i64, i64, p, p, p, p]
+        L.mp_mx_dequantize.argtypes = [p, p, i64, i64, p, i32, p]
+        L.mp_mx_segment_matmul_workspace.argtypes = [i64, i64, psz]
+        L.mp_mx_segment_matmul.argtypes = [p, i32, i64, p, i32, i64, i64, i64, p, p, i64, p, i32, p, sz,
+                                           p]
+        for name in ("mp_mx_quantize", "mp_mx_dequantize", "mp_mx_segment_matmul_workspace",
+                     "mp_mx_segment_matmul", "mp_group_norm_workspace", "mp_group_norm", "mp_group_norm_backward",
                      "mp_dropout", "mp_route_workspace", "mp_route", "mp_route_backward"):
             getattr(L, name).restype = i32
         _lib = L
@@ -291,4 +299,101 @@ def route_backward(logits, idx, weight, counts, *, dweight=None, dloss=None, mas
             out = torch.empty(N, E, dtype=logits.dtype, device=logits.device)
     mp_route_backward(lp, _dtype_code(logits.dtype), N, E, ldl, k, mask, int(renorm), idx, weight,
                       counts, dweight, dloss, out, stream)
+    return out
+
+
+# ---- microscaled 4-bit floating point --------------------------------------------------------
+
+def mp_mx_quantize(x, dtype, N, K, ldx, codes, scales, values, stream=None):
+    """x: a tensor (rows may be strided) or a raw address."""
+    xp = _rows_ptr(x)[0] if isinstance(x, torch.Tensor) else x
+    _check("mp_mx_quantize", _layers().mp_mx_quantize(
+        xp, dtype, N, K, ldx, _ptr(codes), _ptr(scales), _ptr(values), _stream(stream)))
+
+
+def mp_mx_dequantize(codes, scales, N, K, out, dtype, stream=None):
+    _check("mp_mx_dequantize", _layers().mp_mx_dequantize(
+        _ptr(codes), _ptr(scales), N, K, _ptr(out), dtype, _stream(stream)))
+
+
+def mp_mx_segment_matmul_workspace(N, K) -> int:
+    _layers()
+    return _bytes("mp_mx_segment_matmul_workspace", N, K)
+
+
+def mp_mx_segment_matmul(seg, seg_itype, T, x, x_dtype, N, K, ldx, w_codes, w_scales, Fo, out,
+                         out_dtype, ws, ws_bytes, stream=None):
+    xp = _rows_ptr(x)[0] if isinstance(x, torch.Tensor) else x
+    _check("mp_mx_segment_matmul", _layers().mp_mx_segment_matmul(
+        _ptr(seg), seg_itype, T, xp, x_dtype, N, K, ldx, _ptr(w_codes), _ptr(w_scales), Fo, _ptr(out),
+        out_dtype, _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def _blocks(K):
+    return -(-int(K) // 32)
+
+
+def mx_quantize(x, *, want_values=False, stream=None):
+    """x [..., K] in 4 bits: (codes [..., 16 KB] uint8, scales [..., KB] uint8), KB = ceil(K / 32), and
+    with want_values also the values that they stand for, in x's shape and dtype (training with
+    quantised values: use them in the forward pass and hand their gradient to x unchanged).
+
+    The weights of mx_segment_matmul are mx_quantize(W.transpose(1, 2)) of segment_matmul's W."""
+    K = int(x.shape[-1])
+    # (of a table the rows may be strided; other shapes are made contiguous)
+    rows = x if x.dim() == 2 else x.contiguous().view(-1, K)
+    N = int(rows.shape[0])
+    _on_gpu(x)
+    xp, ldx = _rows_ptr(rows)
+    lead, kb = tuple(x.shape[:-1]), _blocks(K)
+    with _on(stream):
+        codes = torch.empty(*lead, 16 * kb, dtype=torch.uint8, device=x.device)
+        scales = torch.empty(*lead, kb, dtype=torch.uint8, device=x.device)
+        values = torch.empty(x.shape, dtype=x.dtype, device=x.device) if want_values else None
+        mp_mx_quantize(xp, _dtype_code(x.dtype), N, K, ldx, codes, scales, values, stream)
+    return (codes, scales, values) if want_values else (codes, scales)
+
+
+def _mx(codes, scales, K):
+    kb = _blocks(K)
+    if (codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.shape[-1] != 16 * kb
+            or scales.shape[-1] != kb or codes.shape[:-1] != scales.shape[:-1]):
+        raise ValueError(f"codes [..., {16 * kb}] and scales [..., {kb}] of uint8 expected for K = {K}")
+
+
+def mx_dequantize(codes, scales, K, *, dtype=torch.float32, stream=None):
+    """The values [..., K] that codes and scales stand for."""
+    _mx(codes, scales, K)
+    _on_gpu(codes, scales)
+    lead = tuple(codes.shape[:-1])
+    kb = _blocks(K)
+    with _on(stream):
+        out = torch.empty(*lead, int(K), dtype=dtype, device=codes.device)
+        mp_mx_dequantize(codes, scales, scales.numel() // kb, int(K), out, _dtype_code(dtype), stream)
+    return out
+
+
+def mx_segment_matmul(seg, x, codes, scales, *, out_dtype=torch.float32, out=None, stream=None):
+    """out[r] = q(x[r]) @ W[t]^T for the rows r of segment t: x [N, K] is quantised on the way, W is
+    given in 4 bits as codes [T, Fo, 16 KB] and scales [T, Fo, KB] (mx_quantize of [T, Fo, K]).
+
+    seg [T + 1] (int32 or int64) lies on the GPU, as the rowptr of a dispatch does; rows of no segment
+    are not written."""
+    N, K = int(x.shape[0]), int(x.shape[1])
+    _mx(codes, scales, K)
+    if codes.dim() != 3 or int(seg.numel()) != codes.shape[0] + 1:
+        raise ValueError("codes [T, Fo, ...] and seg [T + 1] expected")
+    T, Fo = int(codes.shape[0]), int(codes.shape[1])
+    if out is not None and tuple(out.shape) != (N, Fo):
+        raise ValueError("out must be [N, Fo]")
+    _on_gpu(seg, x, codes, scales, out)
+    dt, it = _dtype_code(x.dtype), _itype_code(seg.dtype)
+    xp, ldx = _rows_ptr(x)
+    nb = mp_mx_segment_matmul_workspace(N, K)
+    with _on(stream):
+        if out is None:
+            out = torch.empty(N, Fo, dtype=out_dtype, device=x.device)
+        ws = _workspace(nb, x.device)
+        mp_mx_segment_matmul(seg, it, T, xp, dt, N, K, ldx, codes, scales, Fo, out,
+                             _dtype_code(out.dtype), ws, nb, stream)
     return out

@@ -158,3 +158,47 @@ def group_norm_backward(ptr, r, dout, groups, weight, name):
         m1, m2 = g[a:b].mean((0, 2))[:, None], (g[a:b] * xh[a:b]).mean((0, 2))[:, None]
         dx[a:b] = r["rstd"][i][:, None] * (g[a:b] - m1 - xh[a:b] * m2)
     return dx.reshape(n, f), dweight, dbias
+
+
+# ---- microscaled 4-bit floating point --------------------------------------------------------
+
+E2M1 = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6])
+
+
+def mx_quantize(x):
+    """x [N, K] float64 (values of fp32 or bf16) -> codes [N, KB, 32], scale bytes [N, KB], values
+    [N, K]."""
+    n, k = x.shape
+    kb = -(-k // 32)
+    v = np.zeros((n, kb * 32))
+    v[:, :k] = x
+    v = v.reshape(n, kb, 32)
+    with np.errstate(all="ignore"):
+        top = np.abs(v).max(2)
+        bad = ~np.isfinite(v).all(2)
+        e = np.frexp(np.where(bad | (top == 0), 1.0, top))[1] - 1  # floor(log2)
+        s = np.clip(e - 2 + 127, 0, 254)
+        s = np.where(top == 0, 0, s)
+        s = np.where(bad, 255, s)
+        a = np.abs(np.where(bad[..., None], 0.0, v)) / np.exp2(np.where(bad, 127, s) - 127.0)[..., None]
+    # nearest of the eight magnitudes; halfway, the one with the even code
+    dist = np.abs(a[..., None] - E2M1)
+    near = dist.min(-1, keepdims=True)
+    cand = dist == near
+    code = np.where(cand[..., 0::2].any(-1) & (cand.sum(-1) > 1), 2 * cand[..., 0::2].argmax(-1),
+                    cand.argmax(-1))
+    code = code + 8 * np.signbit(v)
+    value = mx_values(code, s).reshape(n, -1)[:, :k]
+    return code, s, value
+
+
+def mx_values(code, s):
+    sign = np.where(code >= 8, -1.0, 1.0)
+    v = sign * E2M1[code & 7] * np.exp2(np.where(s == 255, 127, s) - 127.0)[..., None]
+    return np.where((s == 255)[..., None], np.nan, v)
+
+
+def mx_pack(code):
+    """[..., KB, 32] codes -> [..., KB * 16] bytes."""
+    b = code[..., 0::2] | (code[..., 1::2] << 4)
+    return b.reshape(*code.shape[:-2], -1).astype(np.uint8)

@@ -135,3 +135,46 @@ def test_group_norm_workspace():
     assert mp.mp_group_norm_workspace(100, 5, 64, 8, 1, True) > 0
     with pytest.raises(mp.MPError):
         mp.mp_group_norm_workspace(100, 5, 64, 7, 0, False)
+
+
+QUANTIZE = dict(x=FAKE, dtype=0, N=10, K=64, ldx=64, codes=FAKE, scales=FAKE, values=None, stream=None)
+
+
+@pytest.mark.parametrize("status,change", [
+    (-3, dict(dtype=2)), (-2, dict(N=-1)), (-2, dict(N=2 ** 31)), (-2, dict(K=0)), (-2, dict(ldx=63)),
+    (-2, dict(K=65537, ldx=65537)), (-1, dict(x=None)), (-1, dict(codes=None)), (-1, dict(scales=None)),
+    (-1, dict(codes=None, scales=None)), (-8, dict(x=FAKE + 2)), (-8, dict(codes=FAKE + 8)),
+    (-8, dict(values=FAKE + 2))])
+def test_quantize_refusals(status, change):
+    refused("mp_mx_quantize", QUANTIZE, status, **change)
+
+
+DEQUANTIZE = dict(codes=FAKE, scales=FAKE, N=10, K=64, out=FAKE, dtype=0, stream=None)
+
+
+@pytest.mark.parametrize("status,change", [
+    (-3, dict(dtype=2)), (-2, dict(N=-1)), (-2, dict(K=0)), (-1, dict(codes=None)),
+    (-1, dict(scales=None)), (-1, dict(out=None)), (-8, dict(codes=FAKE + 4)), (-8, dict(out=FAKE + 2))])
+def test_dequantize_refusals(status, change):
+    refused("mp_mx_dequantize", DEQUANTIZE, status, **change)
+
+
+PRODUCT = dict(seg=FAKE, seg_itype=0, T=2, x=FAKE, x_dtype=1, N=10, K=64, ldx=64, w_codes=FAKE,
+               w_scales=FAKE, Fo=32, out=FAKE, out_dtype=0, ws=FAKE, ws_bytes=1 << 20, stream=None)
+
+
+@pytest.mark.parametrize("status,change", [
+    (-3, dict(seg_itype=2)), (-3, dict(x_dtype=2)), (-3, dict(out_dtype=2)), (-2, dict(T=0)),
+    (-2, dict(T=4097)), (-2, dict(N=-1)), (-2, dict(K=0)), (-2, dict(ldx=63)), (-2, dict(Fo=0)),
+    (-2, dict(Fo=65537)), (-1, dict(seg=None)), (-1, dict(w_codes=None)), (-1, dict(w_scales=None)),
+    (-1, dict(x=None)), (-1, dict(out=None)), (-1, dict(ws=None)), (-8, dict(seg=FAKE + 4, seg_itype=1)),
+    (-8, dict(x=FAKE + 1)), (-8, dict(w_codes=FAKE + 8)), (-8, dict(out=FAKE + 2)),
+    (-8, dict(ws=FAKE + 8)), (-5, dict(ws_bytes=16))])
+def test_product_refusals(status, change):
+    refused("mp_mx_segment_matmul", PRODUCT, status, **change)
+
+
+def test_product_workspace():
+    assert mp.mp_mx_segment_matmul_workspace(100, 64) >= 100 * 34
+    with pytest.raises(mp.MPError):
+        mp.mp_mx_segment_matmul_workspace(100, 0)
