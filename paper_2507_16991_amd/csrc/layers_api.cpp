@@ -23,7 +23,7 @@ constexpr int64_t kMaxF = 65536;
 
 // Workspace of the group norm, in pieces that start on 256 bytes.
 struct NormSpace {
-    size_t stats = 0, ca = 0, cb = 0, part = 0, bytes = 0;
+    size_t flags = 0, stats = 0, ca = 0, cb = 0, part = 0, bytes = 0;
 };
 NormSpace norm_space(const NormShape& h, int64_t S, int64_t F, int64_t G, int backward) {
     NormSpace n;
@@ -33,7 +33,8 @@ NormSpace norm_space(const NormShape& h, int64_t S, int64_t F, int64_t G, int ba
         return at;
     };
     if (h.long_tiles) {
-        n.stats = take(h.long_tiles * 2 * h.stat_line * 2);
+        n.flags = take(h.short_blocks);
+        n.stats = take(h.long_tiles * h.places * h.stat_line * 2);
         if (backward) {
             n.ca = take(S * G);
             n.cb = take(S * G);
@@ -148,6 +149,7 @@ int mp_group_norm(const void* ptr, int ptr_itype, const void* x, int x_dtype, in
     P.out_bf16 = out_dtype == MP_BF16;
     P.mean = mean;
     P.rstd = rstd;
+    P.flags = reinterpret_cast<int*>(static_cast<char*>(ws) + n.flags);
     P.stats = reinterpret_cast<float*>(static_cast<char*>(ws) + n.stats);
     return hip_status(launch_norm(P, h, x_dtype, false, nullptr, nullptr, as_stream(stream)));
 }
@@ -190,6 +192,7 @@ int mp_group_norm_backward(const void* ptr, int ptr_itype, const void* x, int x_
     P.out_bf16 = dx_dtype == MP_BF16;
     P.mean = const_cast<float*>(mean);
     P.rstd = const_cast<float*>(rstd);
+    P.flags = reinterpret_cast<int*>(w + n.flags);
     P.stats = reinterpret_cast<float*>(w + n.stats);
     P.ca = reinterpret_cast<float*>(w + n.ca);
     P.cb = reinterpret_cast<float*>(w + n.cb);

@@ -5,33 +5,36 @@
 // the rows are read.  Segment lengths are on the device; two paths share them
 // out by length:
 //   * short segments: a unit (a wavefront, or a workgroup) takes a whole
-//     segment and keeps its rows in registers, raw, from the statistics to the
-//     normalisation: one read, one write.  What does not fit in the registers
-//     is read again from the caches.
+//     segment, statistics and normalisation in one launch; the second read of
+//     its rows comes from the caches.  (Rows kept in registers in between were
+//     slower: 128 registers and spills instead of 64, so half the wavefronts.)
 //   * long segments (more than lmax rows): tiles of `tile_rows` rows, whatever
 //     the segments' lengths, leave partial statistics (norm_long_stats), a
 //     workgroup joins those of a segment (norm_long_join), and the tiles
-//     are normalised by a second read (norm_long_apply).  tile_rows <= lmax, so
-//     a tile meets at most two long segments and its partials have two fixed
-//     places.
-// A thread owns a chunk of V channels (16 bytes) and every slots-th row, so
+//     are normalised by a second read (norm_long_apply).  The workgroups of the
+//     short path leave word whether they met a long segment; these return at
+//     once if none did.
+// A thread owns a chunk of V = 4 channels and every slots-th row, so
 // groups of any width cost nothing in the loops: sums are per channel, and
 // channels are added up to groups in LDS.  Rows whose width is no multiple of V
 // end with a chunk moved back to end with the row; the channels that it shares
 // with the chunk before it are left out of the sums and stored twice, equal.
-// Variances are taken about means: the short path holds the rows and
-// subtracts the mean, the long path joins (count, mean, M2) of batches of eight
-// rows by  mean = a + d nb / n,  M2 = M2a + M2b + d^2 na nb / n,  d = b - a.
+// Variances are taken about means: batches of a few rows are summed, then their
+// squares about the batch's own mean, and (count, mean, M2) of batches joined by
+// mean = a + d nb / n,  M2 = M2a + M2b + d^2 na nb / n,  d = b - a.
 #include "layers_internal.hpp"
 
 namespace mp {
 namespace {
 
 constexpr int kLong = 256;        // threads of the long path's workgroups
-constexpr int kRows = 8;          // rows that a thread has in registers
-constexpr int kPad = 8;           // LDS line of a thread's v-th channel: UNIT + 8 floats,
-                                  // so that consecutive channels lie on consecutive banks
+constexpr int kPad = 16;          // LDS line of a thread's v-th channel: UNIT + 16 floats,
+                                  // so that consecutive channels lie on different banks
 constexpr int kJoin = 256;
+
+// Rows of a batch: loads that a thread has in flight.
+constexpr int kShortRows = 8;
+constexpr int long_rows(bool bf16, bool backward) { return bf16 || !backward ? 8 : 4; }
 
 // ---- activations ----------------------------------------------------------------------
 // The standard normal distribution and density at z.  With a = |z| and t =
@@ -57,8 +60,21 @@ __device__ inline float sigmoid(float z) {
     return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * z));
 }
 
-template <int V>
-__device__ inline void activate(float (&z)[V], int act) {
+// f(Act<act>()): the loops over rows are there once for every activation.
+template <int A>
+struct Act {
+    static constexpr int value = A;
+};
+template <typename Fn>
+__device__ inline void by_act(int act, Fn f) {
+    if (act == MP_ACT_RELU) f(Act<MP_ACT_RELU>());
+    else if (act == MP_ACT_SILU) f(Act<MP_ACT_SILU>());
+    else if (act == MP_ACT_GELU) f(Act<MP_ACT_GELU>());
+    else f(Act<MP_ACT_NONE>());
+}
+
+template <int V, int act>
+__device__ inline void activate(float (&z)[V], Act<act>) {
     if (act == MP_ACT_RELU) {
 #pragma unroll
         for (int v = 0; v < V; ++v) z[v] = z[v] < 0.f ? 0.f : z[v];  // (keeps NaN)
@@ -76,8 +92,8 @@ __device__ inline void activate(float (&z)[V], int act) {
 }
 
 // d <- d * act'(z)
-template <int V>
-__device__ inline void slope(float (&d)[V], const float (&z)[V], int act) {
+template <int V, int act>
+__device__ inline void slope(float (&d)[V], const float (&z)[V], Act<act>) {
     if (act == MP_ACT_RELU) {
 #pragma unroll
         for (int v = 0; v < V; ++v) d[v] = z[v] > 0.f ? d[v] : 0.f;
@@ -118,20 +134,32 @@ __device__ inline int64_t segment_of(const NormParams& P, int64_t row) {
     return lo;
 }
 
+// The first segment s with ptr[s] + s >= key: shares of equal rows plus segments.
+__device__ inline int64_t share_begin(const NormParams& P, int64_t key) {
+    const int lane = threadIdx.x & 63;
+    int64_t lo = 0, hi = P.S;
+    while (lo < hi) {
+        const int64_t step = (hi - lo + 63) / 64, at = lo + lane * step;
+        const uint64_t below = __ballot(at < hi && offset_of(P, at) + at < key);
+        if (!below) break;
+        lo += (63 - __builtin_clzll(below)) * step + 1;
+        if (hi > lo - 1 + step) hi = lo - 1 + step;
+    }
+    return lo;
+}
+
 // ---- a thread's chunk of channels ------------------------------------------------------------
 // Columns [c0, c0 + W) are cut into cpr chunks of V; thread t of a unit has
 // chunk t % cpr and row slot t / cpr (slots of them; threads beyond are idle).
 template <int V>
 struct Chunk {
-    int k, slot, c, skip;  // c: first column within the tile; skip: columns of the chunk before
+    int slot, c;  // c: first column within the tile
     bool on;
     __device__ Chunk(int t, int cpr, int slots, int W) {
-        k = t % cpr;
         slot = t / cpr;
         on = slot < slots;
-        const int c0 = k * V;
+        const int c0 = (t - slot * cpr) * V;
         c = c0 + V <= W ? c0 : W - V;
-        skip = c0 - c;
     }
 };
 
@@ -142,6 +170,26 @@ __device__ inline int place(int slot, int c, int cpr, int W) {
     const int v = k == cpr - 1 && cpr * V > W ? c - (W - V) : c - k * V;
     return v * (UNIT + kPad) + slot * cpr + k;
 }
+
+// The groups of a chunk's channels: that of the first, and a bit for every channel
+// that begins a new one.
+template <int V>
+struct Groups {
+    int first;
+    uint32_t next;
+    __device__ Groups(int64_t c, int cg) {
+        first = (int)(c / cg);
+        next = 0;
+        int left = (int)((int64_t)(first + 1) * cg - c);  // channels to the next group
+#pragma unroll
+        for (int v = 1; v < V; ++v)
+            if (v == left) {
+                next |= 1u << v;
+                left += cg;
+            }
+    }
+    __device__ int of(int v) const { return first + __popc(next & ((2u << v) - 1)); }
+};
 
 // For each of `groups` ranges of columns (range(g, b, e): [b, e)) the sum over
 // slots and columns of get(slot, place); put(g, sum) by one thread.  lpg (a power of
@@ -190,15 +238,173 @@ __device__ inline int rows_of_slot(int64_t n, int slot, int slots) {
     return n > slot ? (int)((n - slot + slots - 1) / slots) : 0;
 }
 
+// ---- a thread's rows -------------------------------------------------------------------------
+// `mine` rows from x (and d), step_x (step_f) elements apart.
+template <typename T>
+struct Rows {
+    const typename T::raw* x;
+    const typename T::raw* d;
+    int64_t step_x, step_f;
+    int mine;
+};
+
+// A thread's parameters for its V channels; M = 1 where they lie in one group, else V.
+template <int V, int M>
+struct Param {
+    float gamma[V], beta[V], mean[M], rstd[M];
+};
+
+// xhat and da of one row.
+template <typename T, int V, int M, typename A>
+__device__ inline void grads(A act, const Param<V, M>& p, const RawOf<T, V>& a,
+                             const RawOf<T, V>& e, float (&xh)[V], float (&da)[V]) {
+    float z[V];
+    to_floats<T, V>(a, xh);
+    to_floats<T, V>(e, da);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        xh[v] = (xh[v] - p.mean[v % M]) * p.rstd[v % M];
+        z[v] = __builtin_fmaf(xh[v], p.gamma[v], p.beta[v]);
+    }
+    slope<V>(da, z, act);
+}
+
+// Statistics of the thread's rows, R loads in flight.  Forward: A and B the mean
+// and M2 of each channel; backward: the sums of da and da xhat.
+template <typename T, int V, int M, int R, bool BWD>
+__device__ inline void row_stats(const Rows<T>& rows, const Param<V, M>& p, int act, float (&A)[V],
+                                 float (&B)[V]) {
+    const auto loop = [&](auto act) {
+        const typename T::raw* px = rows.x;
+        const typename T::raw* pd = rows.d;
+        for (int i0 = 0; i0 < rows.mine; i0 += R) {
+            const int nb = rows.mine - i0 < R ? rows.mine - i0 : R;
+            RawOf<T, V> xr[R], dr[R];
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                // (past the end: the last row again, weighted by nothing)
+                xr[i] = load_raw<T, V>(px);
+                if (BWD) dr[i] = load_raw<T, V>(pd);
+                const bool on = i0 + i + 1 < rows.mine;
+                px += on ? rows.step_x : 0;
+                pd += on ? rows.step_f : 0;
+            }
+            if constexpr (!BWD) {
+                const float fn = (float)nb, f0 = (float)i0;
+                const float inb = __builtin_amdgcn_rcpf(fn);
+                const float share = fn * __builtin_amdgcn_rcpf(f0 + fn);
+                float m[V] = {}, q[V] = {};
+#pragma unroll
+                for (int i = 0; i < R; ++i) {
+                    float f[V];
+                    to_floats<T, V>(xr[i], f);
+#pragma unroll
+                    for (int v = 0; v < V; ++v) m[v] += i < nb ? f[v] : 0.f;
+                }
+#pragma unroll
+                for (int v = 0; v < V; ++v) m[v] *= inb;
+#pragma unroll
+                for (int i = 0; i < R; ++i) {
+                    float f[V];
+                    to_floats<T, V>(xr[i], f);
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        const float u = i < nb ? f[v] - m[v] : 0.f;
+                        q[v] = __builtin_fmaf(u, u, q[v]);
+                    }
+                }
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const float u = m[v] - A[v];
+                    A[v] = i0 ? __builtin_fmaf(u, share, A[v]) : m[v];
+                    B[v] += __builtin_fmaf(u * u, f0 * share, q[v]);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < R; ++i) {
+                    if (i >= nb) break;
+                    float xh[V], da[V];
+                    grads<T>(act, p, xr[i], dr[i], xh, da);
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        A[v] += da[v];
+                        B[v] = __builtin_fmaf(da[v], xh[v], B[v]);
+                    }
+                }
+            }
+        }
+    };
+    if constexpr (BWD) by_act(act, loop);
+    else loop(Act<MP_ACT_NONE>());
+}
+
+// The thread's rows of out (p.rstd times gamma in p.gamma), or of dx.  o: the first
+// one's element.
+template <typename T, int V, int M, int R, bool BWD>
+__device__ inline void row_apply(const Rows<T>& rows, const Param<V, M>& p, const float (&ca)[M],
+                                 const float (&cb)[M], int act, void* out, int out_bf16,
+                                 int64_t o) {
+    by_act(act, [&](auto act) {
+        const typename T::raw* px = rows.x;
+        const typename T::raw* pd = rows.d;
+        for (int i0 = 0; i0 < rows.mine; i0 += R) {
+            RawOf<T, V> xr[R], dr[R];
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+                if (i0 + i < rows.mine) {
+                    xr[i] = load_raw<T, V>(px);
+                    px += rows.step_x;
+                    if (BWD) {
+                        dr[i] = load_raw<T, V>(pd);
+                        pd += rows.step_f;
+                    }
+                }
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                if (i0 + i >= rows.mine) break;
+                float f[V];
+                if constexpr (!BWD) {
+                    to_floats<T, V>(xr[i], f);
+#pragma unroll
+                    for (int v = 0; v < V; ++v)
+                        f[v] = __builtin_fmaf(f[v] - p.mean[v % M], p.gamma[v], p.beta[v]);
+                    activate<V>(f, act);
+                } else {
+                    float xh[V];
+                    grads<T>(act, p, xr[i], dr[i], xh, f);
+#pragma unroll
+                    for (int v = 0; v < V; ++v)
+                        f[v] = p.rstd[v % M] *
+                               (__builtin_fmaf(p.gamma[v], f[v], -ca[v % M]) - xh[v] * cb[v % M]);
+                }
+                if (out_bf16) store_floats<BF16, V>(static_cast<uint16_t*>(out) + o, f);
+                else store_floats<F32, V>(static_cast<float*>(out) + o, f);
+                o += rows.step_f;
+            }
+        }
+    });
+}
+
+// Threads of a workgroup of the short path: four wavefronts that are units, or
+// one unit.
+constexpr int short_block(int unit) { return unit == 64 ? 256 : unit; }
+
 // ---- short segments ----------------------------------------------------------------------
 // blockIdx.y: a tile of whole groups (the last one moved back to end with the
 // last group).  BWD: workgroup blockIdx.x leaves its sums of da xhat and da in
 // line blockIdx.x of P.part.
-template <typename T, int V, int UNIT, bool BWD>
-__global__ __launch_bounds__(UNIT < 256 ? 256 : UNIT) void norm_short(NormParams P) {
+//
+// Units have shares of neighbouring segments, equal by rows and segments together
+// (in turn by number, units that met several long ones took twice the average).
+//
+// WHOLE: a chunk lies within one group (F / G a multiple of V), so a thread has one
+// mean and leaves one entry in LDS instead of V.
+template <typename T, int V, int UNIT, bool BWD, bool WHOLE>
+__global__ __launch_bounds__(short_block(UNIT), 4) void norm_short(NormParams P) {
     typedef typename T::raw raw;
-    constexpr int BLOCK = UNIT < 256 ? 256 : UNIT, UNITS = BLOCK / UNIT;
+    constexpr int BLOCK = short_block(UNIT), UNITS = BLOCK / UNIT;
     constexpr int ENT = V * (UNIT + kPad);
+    constexpr int M = WHOLE ? 1 : V;  // means of a thread
     extern __shared__ float s_mem[];
     const int t = threadIdx.x % UNIT, u = threadIdx.x / UNIT;
     const int cg = P.cg, gt = P.tile_groups;
@@ -206,31 +412,75 @@ __global__ __launch_bounds__(UNIT < 256 ? 256 : UNIT) void norm_short(NormParams
     const int own = (int)blockIdx.y * gt * cg - g0 * cg;  // columns of the tile before
     const int W = gt * cg, cpr = P.cpr, slots = P.slots;
     const int64_t c0 = (int64_t)g0 * cg;
-    float* ent = s_mem + u * ((BWD ? 2 : 1) * ENT + 2 * gt);
-    float* ent2 = ent + ENT;  // (BWD)
-    float* s_a = ent + (BWD ? 2 : 1) * ENT;
+    float* ent = s_mem + u * (2 * ENT + 2 * gt);  // means, or sums of gamma da
+    float* ent2 = ent + ENT;                      // M2, or sums of gamma da xhat
+    float* s_a = ent2 + ENT;
     float* s_b = s_a + gt;
     const Chunk<V> ck(t, cpr, slots, W);
-    const auto range = [&](int g, int& b, int& e) {
-        b = g * cg;
-        e = b + cg;
+    const Groups<V> lg(ck.c, cg);
+    // WHOLE: the entries of a group are its cpg chunks of every slot, lpg threads
+    // to them
+    const int cpg = WHOLE ? cg / V : 1, l = t & (P.lpg - 1);
+    const int e_slot = l / cpg, e_k = l - e_slot * cpg, d_slot = P.lpg / cpg, d_k = P.lpg - d_slot * cpg;
+    // f(slot, place of an entry) for the thread's share of group g's entries
+    const auto entries = [&](int g, auto f) {
+        if constexpr (WHOLE) {
+            int i = e_slot, k = e_k;
+            while (i < slots) {
+                f(i, i * cpr + g * cpg + k);
+                i += d_slot;
+                k += d_k;
+                if (k >= cpg) {
+                    k -= cpg;
+                    ++i;
+                }
+            }
+        } else {
+            int i = l / cg, c = l - i * cg;
+            const int di = P.lpg / cg, dc = P.lpg - di * cg;
+            while (i < slots) {
+                f(i, place<V, UNIT>(i, g * cg + c, cpr, W));
+                i += di;
+                c += dc;
+                if (c >= cg) {
+                    c -= cg;
+                    ++i;
+                }
+            }
+        }
+    };
+    const auto over_threads = [&](float a) {
+        for (int o = P.lpg >> 1; o > 0; o >>= 1) a += __shfl_xor(a, o);
+        return a;
     };
 
-    float gamma[V], beta[V];
-    int lg[V];
+    Param<V, M> p;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        gamma[v] = P.gamma ? P.gamma[c0 + ck.c + v] : 1.f;
-        beta[v] = P.beta ? P.beta[c0 + ck.c + v] : 0.f;
-        lg[v] = (ck.c + v) / cg;
+        p.gamma[v] = P.gamma ? P.gamma[c0 + ck.c + v] : 1.f;
+        p.beta[v] = P.beta ? P.beta[c0 + ck.c + v] : 0.f;
     }
     float sum_g[V] = {}, sum_b[V] = {};  // BWD: over all segments of the unit
+    int seen = 0;                        // a long segment
 
+    Rows<T> rows;
+    rows.step_x = (int64_t)slots * P.ldx;
+    rows.step_f = (int64_t)slots * P.F;
     const raw* x = static_cast<const raw*>(P.x) + c0 + ck.c;
-    for (int64_t s = (int64_t)blockIdx.x * UNITS + u; s < P.S; s += (int64_t)gridDim.x * UNITS) {
-        const int64_t b = offset_of(P, s), n = offset_of(P, s + 1) - b;
-        if (n > P.lmax) continue;
-        if (n <= 0) {
+    const raw* d = static_cast<const raw*>(P.dout) + c0 + ck.c;
+    const int64_t unit = (int64_t)blockIdx.x * UNITS + u, units = (int64_t)gridDim.x * UNITS;
+    const int64_t first = share_begin(P, (P.N + P.S) * unit / units);
+    const int64_t last = unit + 1 < units ? share_begin(P, (P.N + P.S) * (unit + 1) / units) : P.S;
+    int64_t next = first < last ? offset_of(P, first) : 0;
+    for (int64_t s = first; s < last; ++s) {
+        const int64_t b = next;
+        next = offset_of(P, s + 1);
+        const int64_t n64 = next - b;
+        if (n64 > P.lmax) {
+            seen = 1;
+            continue;
+        }
+        if (n64 <= 0) {
             if (!BWD)
                 for (int g = t; g < gt; g += UNIT) {
                     P.mean[s * P.G + g0 + g] = 0.f;
@@ -238,145 +488,116 @@ __global__ __launch_bounds__(UNIT < 256 ? 256 : UNIT) void norm_short(NormParams
                 }
             continue;
         }
+        const int n = (int)n64;
         const float inv = 1.f / ((float)n * (float)cg);
-        const int mine = ck.on ? rows_of_slot(n, ck.slot, slots) : 0;
-        const int64_t r0 = b + ck.slot;
-        RawOf<T, V> xr[kRows], dr[kRows];
-        const raw* d = static_cast<const raw*>(P.dout) + c0 + ck.c;
+        rows.mine = ck.on ? rows_of_slot(n, ck.slot, slots) : 0;
+        const int64_t r0 = rows.mine ? b + ck.slot : b;
+        rows.x = x + r0 * P.ldx;
+        rows.d = d + r0 * P.F;
+        const int64_t o0 = r0 * P.F + c0 + ck.c;
+        float A[V] = {}, B[V] = {};
+        if constexpr (BWD) {
 #pragma unroll
-        for (int i = 0; i < kRows; ++i)
-            if (i < mine) {
-                const int64_t r = r0 + (int64_t)i * slots;
-                xr[i] = load_raw<T, V>(x + r * P.ldx);
-                if (BWD) dr[i] = load_raw<T, V>(d + r * P.F);
-            }
-        // every row of the thread: those in registers, then the others
-        const auto each = [&](auto f) {
-#pragma unroll
-            for (int i = 0; i < kRows; ++i)
-                if (i < mine) f(r0 + (int64_t)i * slots, xr[i], dr[i]);
-            for (int i = kRows; i < mine; ++i) {
-                const int64_t r = r0 + (int64_t)i * slots;
-                const RawOf<T, V> a = load_raw<T, V>(x + r * P.ldx);
-                RawOf<T, V> e{};
-                if (BWD) e = load_raw<T, V>(d + r * P.F);
-                f(r, a, e);
-            }
-        };
-        const auto at = [&](int slot, int p) { return ent[p]; };
-        if constexpr (!BWD) {
-            float q[V] = {};
-            each([&](int64_t, const RawOf<T, V>& a, const RawOf<T, V>&) {
-                float f[V];
-                to_floats<T, V>(a, f);
-#pragma unroll
-                for (int v = 0; v < V; ++v) q[v] += f[v];
-            });
-#pragma unroll
-            for (int v = 0; v < V; ++v) ent[v * (UNIT + kPad) + t] = q[v];
-            unit_sync<UNIT>();
-            group_sums<V, UNIT>(t, P.lpg, gt, slots, cpr, W, range, at,
-                                [&](int g, float sum) { s_a[g] = sum * inv; });
-            unit_sync<UNIT>();
-            float mean[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                mean[v] = s_a[lg[v]];
-                q[v] = 0.f;
-            }
-            each([&](int64_t, const RawOf<T, V>& a, const RawOf<T, V>&) {
-                float f[V];
-                to_floats<T, V>(a, f);
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const float e = f[v] - mean[v];
-                    q[v] = __builtin_fmaf(e, e, q[v]);
-                }
-            });
-#pragma unroll
-            for (int v = 0; v < V; ++v) ent[v * (UNIT + kPad) + t] = q[v];
-            unit_sync<UNIT>();
-            group_sums<V, UNIT>(t, P.lpg, gt, slots, cpr, W, range, at, [&](int g, float sum) {
-                const float rs = 1.f / sqrtf(sum * inv + P.eps);
-                s_b[g] = rs;
-                P.mean[s * P.G + g0 + g] = s_a[g];
-                P.rstd[s * P.G + g0 + g] = rs;
-            });
-            unit_sync<UNIT>();
-            float scale[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) scale[v] = s_b[lg[v]] * gamma[v];
-            each([&](int64_t r, const RawOf<T, V>& a, const RawOf<T, V>&) {
-                float f[V];
-                to_floats<T, V>(a, f);
-#pragma unroll
-                for (int v = 0; v < V; ++v)
-                    f[v] = __builtin_fmaf(f[v] - mean[v], scale[v], beta[v]);
-                activate<V>(f, P.act);
-                if (P.out_bf16) store_floats<BF16, V>(static_cast<uint16_t*>(P.out) + r * P.F + c0 + ck.c, f);
-                else store_floats<F32, V>(static_cast<float*>(P.out) + r * P.F + c0 + ck.c, f);
-            });
-        } else {
-            float mean[V], rstd[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                mean[v] = P.mean[s * P.G + g0 + lg[v]];
-                rstd[v] = P.rstd[s * P.G + g0 + lg[v]];
-            }
-            float qg[V] = {}, qb[V] = {};
-            const auto grads = [&](const RawOf<T, V>& a, const RawOf<T, V>& e, float (&xh)[V],
-                                   float (&da)[V]) {
-                float z[V];
-                to_floats<T, V>(a, xh);
-                to_floats<T, V>(e, da);
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    xh[v] = (xh[v] - mean[v]) * rstd[v];
-                    z[v] = __builtin_fmaf(xh[v], gamma[v], beta[v]);
-                }
-                slope<V>(da, z, P.act);
-            };
-            each([&](int64_t, const RawOf<T, V>& a, const RawOf<T, V>& e) {
-                float xh[V], da[V];
-                grads(a, e, xh, da);
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    qb[v] += da[v];
-                    qg[v] = __builtin_fmaf(da[v], xh[v], qg[v]);
-                }
-            });
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                ent[v * (UNIT + kPad) + t] = gamma[v] * qb[v];
-                ent2[v * (UNIT + kPad) + t] = gamma[v] * qg[v];
-                sum_b[v] += qb[v];
-                sum_g[v] += qg[v];
-            }
-            if (P.out) {
-                unit_sync<UNIT>();
-                group_sums<V, UNIT>(t, P.lpg, gt, slots, cpr, W, range, at,
-                                    [&](int g, float sum) { s_a[g] = sum * inv; });
-                group_sums<V, UNIT>(t, P.lpg, gt, slots, cpr, W, range,
-                                    [&](int, int p) { return ent2[p]; },
-                                    [&](int g, float sum) { s_b[g] = sum * inv; });
-                unit_sync<UNIT>();
-                float ca[V], cb[V];
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    ca[v] = s_a[lg[v]];
-                    cb[v] = s_b[lg[v]];
-                }
-                each([&](int64_t r, const RawOf<T, V>& a, const RawOf<T, V>& e) {
-                    float xh[V], da[V];
-                    grads(a, e, xh, da);
-#pragma unroll
-                    for (int v = 0; v < V; ++v)
-                        da[v] = rstd[v] * (__builtin_fmaf(gamma[v], da[v], -ca[v]) - xh[v] * cb[v]);
-                    if (P.out_bf16) store_floats<BF16, V>(static_cast<uint16_t*>(P.out) + r * P.F + c0 + ck.c, da);
-                    else store_floats<F32, V>(static_cast<float*>(P.out) + r * P.F + c0 + ck.c, da);
-                });
+            for (int m = 0; m < M; ++m) {
+                p.mean[m] = P.mean[s * P.G + g0 + lg.of(m)];
+                p.rstd[m] = P.rstd[s * P.G + g0 + lg.of(m)];
             }
         }
+        row_stats<T, V, M, kShortRows, BWD>(rows, p, P.act, A, B);
+        if constexpr (BWD) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                sum_b[v] += A[v];
+                sum_g[v] += B[v];
+                A[v] *= p.gamma[v];
+                B[v] *= p.gamma[v];
+            }
+            if (!P.out) continue;
+        }
+        if constexpr (WHOLE) {
+            float a = A[0], e = B[0];
+#pragma unroll
+            for (int v = 1; v < V; ++v) {
+                a += A[v];
+                e += B[v];
+            }
+            if (!BWD) {  // one mean of the chunk's channels, and M2 about it
+                a *= 1.f / V;
+                float q = 0.f;
+#pragma unroll
+                for (int v = 0; v < V; ++v) q = __builtin_fmaf(A[v] - a, A[v] - a, q);
+                e = __builtin_fmaf(q, (float)rows.mine, e);
+            }
+            ent[t] = a;
+            ent2[t] = e;
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                ent[v * (UNIT + kPad) + t] = A[v];
+                ent2[v * (UNIT + kPad) + t] = B[v];
+            }
+        }
+        unit_sync<UNIT>();
+        for (int gb = 0; gb < gt; gb += UNIT / P.lpg) {
+            const int g = gb + t / P.lpg;
+            const bool on = g < gt;
+            float a = 0.f, e = 0.f;
+            if constexpr (BWD) {
+                if (on)
+                    entries(g, [&](int, int at) {
+                        a += ent[at];
+                        e += ent2[at];
+                    });
+                a = over_threads(a) * inv;
+                e = over_threads(e) * inv;
+                if (on && l == 0) {
+                    s_a[g] = a;
+                    s_b[g] = e;
+                }
+            } else {
+                constexpr float width = WHOLE ? V : 1;  // channels of an entry
+                if (on)
+                    entries(g, [&](int i, int at) {
+                        a = __builtin_fmaf(width * (float)rows_of_slot(n, i, slots), ent[at], a);
+                    });
+                a = over_threads(a) * inv;
+                if (on)
+                    entries(g, [&](int i, int at) {
+                        const int r = rows_of_slot(n, i, slots);
+                        const float q = ent[at] - a;
+                        e += r > 0 ? __builtin_fmaf(q * q, width * (float)r, ent2[at]) : 0.f;
+                    });
+                e = over_threads(e) * inv;
+                if (on && l == 0) {
+                    const float rs = 1.f / sqrtf(e + P.eps);
+                    s_a[g] = a;
+                    s_b[g] = rs;
+                    P.mean[s * P.G + g0 + g] = a;
+                    P.rstd[s * P.G + g0 + g] = rs;
+                }
+            }
+        }
+        unit_sync<UNIT>();
+        float ca[M], cb[M];
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            ca[m] = s_a[lg.of(m)];
+            cb[m] = s_b[lg.of(m)];
+        }
+        if constexpr (BWD) {
+            row_apply<T, V, M, kShortRows, true>(rows, p, ca, cb, P.act, P.out, P.out_bf16, o0);
+        } else {
+            Param<V, M> w = p;
+#pragma unroll
+            for (int m = 0; m < M; ++m) w.mean[m] = ca[m];
+#pragma unroll
+            for (int v = 0; v < V; ++v) w.gamma[v] *= cb[v % M];
+            row_apply<T, V, M, kShortRows, false>(rows, w, ca, cb, P.act, P.out, P.out_bf16, o0);
+        }
+    }
+    if (P.flags) {
+        const int any = __syncthreads_or(seen);
+        if (threadIdx.x == 0 && blockIdx.y == 0) P.flags[blockIdx.x] = any;
     }
     if constexpr (BWD) {
         if (!P.part) return;
@@ -392,9 +613,9 @@ __global__ __launch_bounds__(UNIT < 256 ? 256 : UNIT) void norm_short(NormParams
             float a = 0.f, e = 0.f;
             for (int j = 0; j < UNITS; ++j)
                 for (int i = 0; i < slots; ++i) {
-                    const float* p = s_mem + j * (2 * ENT + 2 * gt) + place<V, UNIT>(i, c, cpr, W);
-                    a += p[0];
-                    e += p[ENT];
+                    const float* q = s_mem + j * (2 * ENT + 2 * gt) + place<V, UNIT>(i, c, cpr, W);
+                    a += q[0];
+                    e += q[ENT];
                 }
             line[c] = a;
             line[P.F + c] = e;
@@ -403,8 +624,23 @@ __global__ __launch_bounds__(UNIT < 256 ? 256 : UNIT) void norm_short(NormParams
 }
 
 // ---- long segments ---------------------------------------------------------------------
+// Whether a workgroup of the short path has met a long segment; uniform.
+__device__ inline bool any_long(const NormParams& P) {
+    if (!P.flags) return true;
+    int any = 0;
+    for (int i = threadIdx.x; i < P.short_blocks; i += blockDim.x) any |= P.flags[i];
+    return __syncthreads_or(any) != 0;
+}
+
+// Where the partials of a long segment that begins at row b lie among those of
+// the tile at row0: one that has begun has the first place, and the beginnings
+// of others lie more than lmax rows apart.
+__device__ inline int64_t place_of(const NormParams& P, int64_t b, int64_t row0) {
+    return b <= row0 ? 0 : 1 + (b - row0) / (P.lmax + 1);
+}
+
 // The long segments of rows [row0, row1) in order: f(segment, first row, end,
-// whether it has begun before or at row0).  At most two, as tile_rows <= lmax.
+// place of its partials).
 template <typename Fn>
 __device__ inline void long_segments(const NormParams& P, int64_t row0, int64_t row1, Fn f) {
     const int lane = threadIdx.x & 63;
@@ -419,7 +655,7 @@ __device__ inline void long_segments(const NormParams& P, int64_t row0, int64_t 
             const int i = __builtin_ctzll(hit);
             hit &= hit - 1;
             const int64_t sb = offset_of(P, s0 + i), se = offset_of(P, s0 + i + 1);
-            f(s0 + i, sb > row0 ? sb : row0, se < row1 ? se : row1, sb <= row0);
+            f(s0 + i, sb > row0 ? sb : row0, se < row1 ? se : row1, place_of(P, sb, row0));
         }
         if (!more) break;
         s0 += 64;
@@ -444,15 +680,16 @@ struct LongTile {
     }
 };
 
-// Partials of rows [row0, row1) of a segment: place `seg_slot` (two a tile), then
+// Partials of rows [row0, row1) of a segment: its place among the tile's, then
 // blockIdx.y + group: {mean, M2} or {sum gamma da, sum gamma da xhat}.
 template <typename T, int V, bool BWD>
-__global__ __launch_bounds__(kLong) void norm_long_stats(NormParams P) {
+__global__ __launch_bounds__(kLong, 4) void norm_long_stats(NormParams P) {
     typedef typename T::raw raw;
     constexpr int UNIT = kLong, ENT = V * (UNIT + kPad);
     __shared__ float ent[ENT], ent2[ENT];
     extern __shared__ float s_a[];  // [groups of a tile]
     const int t = threadIdx.x;
+    if (!any_long(P)) return;
     const LongTile<V> lt(P);
     const Chunk<V> ck(t, lt.cpr, lt.slots, lt.W);
     const int64_t row0 = (int64_t)blockIdx.x * P.tile_rows;
@@ -463,102 +700,46 @@ __global__ __launch_bounds__(kLong) void norm_long_stats(NormParams P) {
         b = gb > lt.skip0 ? (int)gb : lt.skip0;
         e = ge < lt.W ? (int)ge : lt.W;
     };
-    float gamma[V], beta[V];
-    int lg[V];
+    Param<V, V> p;
+    const Groups<V> lg(cc, P.cg);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        gamma[v] = P.gamma ? P.gamma[cc + v] : 1.f;
-        beta[v] = P.beta ? P.beta[cc + v] : 0.f;
-        lg[v] = (int)((cc + v) / P.cg);
+        p.gamma[v] = P.gamma ? P.gamma[cc + v] : 1.f;
+        p.beta[v] = P.beta ? P.beta[cc + v] : 0.f;
     }
     float sum_g[V] = {}, sum_b[V] = {};
     const raw* x = static_cast<const raw*>(P.x) + cc;
     const raw* d = static_cast<const raw*>(P.dout) + cc;
 
-    long_segments(P, row0, row1, [&](int64_t s, int64_t b, int64_t e, bool began) {
+    long_segments(P, row0, row1, [&](int64_t s, int64_t b, int64_t e, int64_t nth) {
         const int64_t n = e - b;
-        const int mine = ck.on ? rows_of_slot(n, ck.slot, lt.slots) : 0;
-        const int64_t r0 = b + ck.slot;
-        float A[V] = {}, B[V] = {};  // mean and M2, or the sums of da and da xhat
-        float mean[V], rstd[V];
+        Rows<T> rows;
+        rows.mine = ck.on ? rows_of_slot(n, ck.slot, lt.slots) : 0;
+        const int64_t r0 = rows.mine ? b + ck.slot : b;
+        rows.x = x + r0 * P.ldx;
+        rows.d = d + r0 * P.F;
+        rows.step_x = lt.slots * P.ldx;
+        rows.step_f = lt.slots * P.F;
+        float A[V] = {}, B[V] = {};
         if (BWD) {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                mean[v] = P.mean[s * P.G + lg[v]];
-                rstd[v] = P.rstd[s * P.G + lg[v]];
+                p.mean[v] = P.mean[s * P.G + lg.of(v)];
+                p.rstd[v] = P.rstd[s * P.G + lg.of(v)];
             }
         }
-        for (int i0 = 0; i0 < mine; i0 += kRows) {
-            const int nb = mine - i0 < kRows ? mine - i0 : kRows;
-            RawOf<T, V> xr[kRows], dr[kRows];
-#pragma unroll
-            for (int i = 0; i < kRows; ++i) {
-                // (past the end: the last row again, weighted by nothing)
-                const int64_t r = r0 + (int64_t)(i0 + (i < nb ? i : nb - 1)) * lt.slots;
-                xr[i] = load_raw<T, V>(x + r * P.ldx);
-                if (BWD) dr[i] = load_raw<T, V>(d + r * P.F);
-            }
-            if constexpr (!BWD) {
-                const float fn = (float)nb, f0 = (float)i0;
-                const float inb = 1.f / fn, share = fn / (f0 + fn);
-                float m[V] = {}, q[V] = {};
-#pragma unroll
-                for (int i = 0; i < kRows; ++i) {
-                    float f[V];
-                    to_floats<T, V>(xr[i], f);
-#pragma unroll
-                    for (int v = 0; v < V; ++v) m[v] += i < nb ? f[v] : 0.f;
-                }
-#pragma unroll
-                for (int v = 0; v < V; ++v) m[v] *= inb;
-#pragma unroll
-                for (int i = 0; i < kRows; ++i) {
-                    float f[V];
-                    to_floats<T, V>(xr[i], f);
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        const float u = i < nb ? f[v] - m[v] : 0.f;
-                        q[v] = __builtin_fmaf(u, u, q[v]);
-                    }
-                }
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const float u = m[v] - A[v];
-                    A[v] = i0 ? __builtin_fmaf(u, share, A[v]) : m[v];
-                    B[v] += __builtin_fmaf(u * u, f0 * share, q[v]);
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < kRows; ++i) {
-                    if (i >= nb) break;
-                    float xh[V], da[V], z[V];
-                    to_floats<T, V>(xr[i], xh);
-                    to_floats<T, V>(dr[i], da);
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        xh[v] = (xh[v] - mean[v]) * rstd[v];
-                        z[v] = __builtin_fmaf(xh[v], gamma[v], beta[v]);
-                    }
-                    slope<V>(da, z, P.act);
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        A[v] += da[v];
-                        B[v] = __builtin_fmaf(da[v], xh[v], B[v]);
-                    }
-                }
-            }
-        }
+        row_stats<T, V, V, long_rows(sizeof(raw) == 2, BWD), BWD>(rows, p, P.act, A, B);
         __syncthreads();  // the segment before has been added up
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            ent[v * (UNIT + kPad) + t] = BWD ? gamma[v] * A[v] : A[v];
-            ent2[v * (UNIT + kPad) + t] = BWD ? gamma[v] * B[v] : B[v];
+            ent[v * (UNIT + kPad) + t] = BWD ? p.gamma[v] * A[v] : A[v];
+            ent2[v * (UNIT + kPad) + t] = BWD ? p.gamma[v] * B[v] : B[v];
             sum_b[v] += A[v];
             sum_g[v] += B[v];
         }
         __syncthreads();
         float2* out = reinterpret_cast<float2*>(P.stats) +
-                      ((int64_t)blockIdx.x * 2 + (began ? 0 : 1)) * P.stat_line + blockIdx.y + lt.ga;
+                      ((int64_t)blockIdx.x * P.places + nth) * P.stat_line + blockIdx.y + lt.ga;
         if constexpr (BWD) {
             group_sums<V, UNIT>(t, P.lpg, lt.gn, lt.slots, lt.cpr, lt.W, range,
                                 [&](int, int p) { return ent[p]; },
@@ -638,6 +819,7 @@ __global__ __launch_bounds__(kJoin) void norm_long_join(NormParams P, int gw, in
     __shared__ int64_t s_seg[kJoin];
     __shared__ int s_n;
     const int t = threadIdx.x, gi = t & (gw - 1), q = t / gw, Q = kJoin / gw;
+    if (!any_long(P)) return;
     for (int64_t base = blockIdx.x; base < P.S; base += (int64_t)gridDim.x * kJoin) {
         __syncthreads();
         if (t == 0) s_n = 0;
@@ -662,7 +844,7 @@ __global__ __launch_bounds__(kJoin) void norm_long_join(NormParams P, int gw, in
 #pragma unroll 4
                     for (int64_t i = q; i < parts; i += Q) {
                         const int64_t tile = t0 + i / ny, y = y0 + i % ny;
-                        const int64_t at = tile * 2 + (b > tile * P.tile_rows ? 1 : 0);
+                        const int64_t at = tile * P.places + place_of(P, b, tile * P.tile_rows);
                         const float2 v = reinterpret_cast<const float2*>(P.stats)[at * P.stat_line + y + g];
                         const int64_t ra = tile * P.tile_rows > b ? tile * P.tile_rows : b;
                         const int64_t rb = (tile + 1) * P.tile_rows < e ? (tile + 1) * P.tile_rows : e;
@@ -716,92 +898,76 @@ __global__ __launch_bounds__(kJoin) void norm_long_join(NormParams P, int gw, in
 // The tiles again, from the last to the first (the last are still in the caches):
 // out, or dx.
 template <typename T, int V, bool BWD>
-__global__ __launch_bounds__(kLong) void norm_long_apply(NormParams P) {
+__global__ __launch_bounds__(kLong, 4) void norm_long_apply(NormParams P) {
     typedef typename T::raw raw;
     const int t = threadIdx.x;
+    if (!any_long(P)) return;
     const LongTile<V> lt(P);
     const Chunk<V> ck(t, lt.cpr, lt.slots, lt.W);
     const int64_t tile = (int64_t)gridDim.x - 1 - blockIdx.x;
     const int64_t row0 = tile * P.tile_rows;
     const int64_t row1 = row0 + P.tile_rows < P.N ? row0 + P.tile_rows : P.N;
     const int64_t cc = lt.c0 + ck.c;
-    float gamma[V], beta[V];
-    int lg[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        gamma[v] = P.gamma ? P.gamma[cc + v] : 1.f;
-        beta[v] = P.beta ? P.beta[cc + v] : 0.f;
-        lg[v] = (int)((cc + v) / P.cg);
-    }
+    const Groups<V> lg(cc, P.cg);
     const raw* x = static_cast<const raw*>(P.x) + cc;
     const raw* d = static_cast<const raw*>(P.dout) + cc;
-    long_segments(P, row0, row1, [&](int64_t s, int64_t b, int64_t e, bool) {
-        if (!ck.on) return;
-        float mean[V], rstd[V], ca[V], cb[V];
+    long_segments(P, row0, row1, [&](int64_t s, int64_t b, int64_t e, int64_t) {
+        Rows<T> rows;
+        rows.mine = ck.on ? rows_of_slot(e - b, ck.slot, lt.slots) : 0;
+        if (!rows.mine) return;
+        const int64_t r0 = b + ck.slot;
+        rows.x = x + r0 * P.ldx;
+        rows.d = d + r0 * P.F;
+        rows.step_x = lt.slots * P.ldx;
+        rows.step_f = lt.slots * P.F;
+        Param<V, V> p;
+        float ca[V], cb[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            mean[v] = P.mean[s * P.G + lg[v]];
-            rstd[v] = P.rstd[s * P.G + lg[v]];
-            ca[v] = BWD ? P.ca[s * P.G + lg[v]] : 0.f;
-            cb[v] = BWD ? P.cb[s * P.G + lg[v]] : 0.f;
-            if (!BWD) rstd[v] *= gamma[v];
+            const int64_t g = s * P.G + lg.of(v);
+            p.gamma[v] = P.gamma ? P.gamma[cc + v] : 1.f;
+            p.beta[v] = P.beta ? P.beta[cc + v] : 0.f;
+            p.mean[v] = P.mean[g];
+            p.rstd[v] = P.rstd[g];
+            ca[v] = BWD ? P.ca[g] : 0.f;
+            cb[v] = BWD ? P.cb[g] : 0.f;
+            if (!BWD) p.gamma[v] *= p.rstd[v];
         }
-#pragma unroll 4
-        for (int64_t r = b + ck.slot; r < e; r += lt.slots) {
-            float f[V];
-            load_floats<T, V>(x + r * P.ldx, f);
-            if constexpr (!BWD) {
-#pragma unroll
-                for (int v = 0; v < V; ++v)
-                    f[v] = __builtin_fmaf(f[v] - mean[v], rstd[v], beta[v]);
-                activate<V>(f, P.act);
-            } else {
-                float da[V], z[V];
-                load_floats<T, V>(d + r * P.F, da);
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    f[v] = (f[v] - mean[v]) * rstd[v];
-                    z[v] = __builtin_fmaf(f[v], gamma[v], beta[v]);
-                }
-                slope<V>(da, z, P.act);
-#pragma unroll
-                for (int v = 0; v < V; ++v)
-                    f[v] = rstd[v] * (__builtin_fmaf(gamma[v], da[v], -ca[v]) - f[v] * cb[v]);
-            }
-            if (P.out_bf16) store_floats<BF16, V>(static_cast<uint16_t*>(P.out) + r * P.F + cc, f);
-            else store_floats<F32, V>(static_cast<float*>(P.out) + r * P.F + cc, f);
-        }
+        row_apply<T, V, V, long_rows(sizeof(raw) == 2, BWD), BWD>(rows, p, ca, cb, P.act, P.out,
+                                                                  P.out_bf16, r0 * P.F + cc);
     });
 }
 
-// dgamma and dbeta: the lines of P.part added up in order, 64 columns a workgroup,
-// a sixteenth of the lines a wavefront.
-constexpr int kGradWaves = 16;
-__global__ __launch_bounds__(kGradWaves * kWave) void norm_param_grads(NormParams P, int64_t lines,
-                                                                       float* dgamma,
-                                                                       float* dbeta) {
-    __shared__ float s_sum[kGradWaves][kWave];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * kWave + lane, n = 2 * P.F;
+// dgamma and dbeta: the lines of P.part added up in order (those of the tiles only
+// if there are long segments).  Bound by the latency of its loads: a workgroup
+// has 16 columns, a lane every 64th line of one, eight loads in flight.
+constexpr int kGradBlock = 1024, kGradCols = 16, kGradRows = kGradBlock / kGradCols;
+__global__ __launch_bounds__(kGradBlock) void norm_param_grads(NormParams P, int64_t long_tiles,
+                                                               float* dgamma, float* dbeta) {
+    __shared__ float s_sum[kGradRows][kGradCols];
+    const int64_t lines = P.short_blocks + (long_tiles && any_long(P) ? long_tiles : 0);
+    const int col = threadIdx.x % kGradCols, w = threadIdx.x / kGradCols;
+    const int64_t c = (int64_t)blockIdx.x * kGradCols + col, n = 2 * P.F;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
     if (c < n) {
-        int64_t i = w;
-        for (; i + 7 * kGradWaves < lines; i += 8 * kGradWaves) {
+        for (int64_t i = w; i < lines; i += 8 * kGradRows) {
             float v[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = P.part[(i + j * kGradWaves) * n + c];
+            for (int j = 0; j < 8; ++j)
+                v[j] = i + j * kGradRows < lines ? P.part[(i + j * kGradRows) * n + c] : 0.f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) s[j & 3] += v[j];
         }
-        for (; i < lines; i += kGradWaves) s[0] += P.part[i * n + c];
     }
-    s_sum[w][lane] = (s[0] + s[1]) + (s[2] + s[3]);
+    s_sum[w][col] = (s[0] + s[1]) + (s[2] + s[3]);
     __syncthreads();
+    for (int o = kGradRows / 2; o > 0; o >>= 1) {
+        if (w < o) s_sum[w][col] += s_sum[w + o][col];
+        __syncthreads();
+    }
     if (w == 0 && c < n) {
-        float r = s_sum[0][lane];
-        for (int j = 1; j < kGradWaves; ++j) r += s_sum[j][lane];
-        if (c < P.F) dgamma[c] = r;
-        else dbeta[c - P.F] = r;
+        if (c < P.F) dgamma[c] = s_sum[0][col];
+        else dbeta[c - P.F] = s_sum[0][col];
     }
 }
 
@@ -814,14 +980,13 @@ int pow2_below(int64_t v, int most) {
 
 }  // namespace
 
-// V: 16 bytes of a row, or single elements for rows narrower than that.  The
-// unit is the smallest that holds a row's chunks and one and a half average
-// segments in registers, else 256 threads (1024 for rows that need them).
+// V: 4 channels, or 1 for rows narrower than that.  The
+// unit is the smallest that holds a row's chunks and eight rows a
+// thread of an average segment, else 256 threads (1024 for rows that need them).
 NormShape norm_shape(int64_t N, int64_t S, int64_t F, int64_t G, int dtype, int backward) {
     NormShape h{};
     const int64_t cg = F / G;
-    const int wide = dtype == MP_BF16 ? 8 : 4;
-    h.V = F >= wide ? wide : 1;
+    h.V = F >= 4 ? 4 : 1;
     h.tile_rows = 1;
     // short path: whole groups in tiles of at most `unit` chunks
     const int64_t most = 1024 * (int64_t)h.V;
@@ -832,29 +997,35 @@ NormShape norm_shape(int64_t N, int64_t S, int64_t F, int64_t G, int dtype, int 
         const int64_t W = h.tile_groups * cg;
         h.cpr = (int)ceil_div(W, h.V);
         h.unit = 0;
-        for (int u : {64, 256}) {
+        for (int u : {64, 128, 256}) {
             if (u < h.cpr) continue;
-            if (kRows * (u / h.cpr) * S * 2 >= 3 * N) {
+            if (8 * (u / h.cpr) * S >= N) {
                 h.unit = u;
                 break;
             }
         }
         if (!h.unit) h.unit = h.cpr <= 256 ? 256 : 1024;
         h.slots = h.unit / h.cpr;
-        h.lmax = 4 * kRows * h.slots;
+        // Many segments: up to 128 KB of one are its unit's.  Few: at most eight rows of
+        // a thread, as longer ones have more of the chip in tiles.
+        h.lmax = 8 * (int64_t)h.slots;
+        if (S >= 4096) {
+            const int64_t rows = (128 << 10) / (W * (dtype == MP_BF16 ? 2 : 4));
+            h.lmax = rows > h.lmax ? rows : h.lmax;
+        }
         h.lpg = pow2_below(h.unit / h.tile_groups, 64);
-        const int64_t units = h.unit < 256 ? 256 / h.unit : 1;
-        const int64_t cap = backward ? 1024 : (int64_t(1) << 20);
+        const int64_t units = short_block(h.unit) / h.unit;
+        const int64_t cap = 2048;
         const int64_t blocks = ceil_div(S, units);
         h.short_blocks = (int)(blocks < cap ? blocks : cap);
-        h.lds = (size_t)units * ((backward ? 2 : 1) * h.V * (h.unit + kPad) + 2 * h.tile_groups) * 4;
+        h.lds = (size_t)units * (2 * h.V * (h.unit + kPad) + 2 * h.tile_groups) * 4;
     }
     h.col_tile = kLong * (int64_t)h.V;
     if (N > h.lmax) {
         int64_t r = ceil_div(N, 2048);
         if (r < 32) r = 32;
-        if (r > h.lmax) r = h.lmax > 0 ? h.lmax : 1;
         h.tile_rows = r;
+        h.places = 2 + (r - 1) / (h.lmax + 1);
         h.long_tiles = ceil_div(N, r);
         h.col_tiles = (int)ceil_div(F, h.col_tile);
         h.stat_line = h.col_tiles + G;
@@ -866,6 +1037,18 @@ NormShape norm_shape(int64_t N, int64_t S, int64_t F, int64_t G, int dtype, int 
     return h;
 }
 
+template <typename T, int V, bool BWD, bool WHOLE>
+static void short_path(const NormParams& q, const NormShape& h, dim3 g, hipStream_t s) {
+    if (h.unit == 64)
+        hipLaunchKernelGGL((norm_short<T, V, 64, BWD, WHOLE>), g, dim3(256), h.lds, s, q);
+    else if (h.unit == 128)
+        hipLaunchKernelGGL((norm_short<T, V, 128, BWD, WHOLE>), g, dim3(128), h.lds, s, q);
+    else if (h.unit == 256)
+        hipLaunchKernelGGL((norm_short<T, V, 256, BWD, WHOLE>), g, dim3(256), h.lds, s, q);
+    else
+        hipLaunchKernelGGL((norm_short<T, V, 1024, BWD, WHOLE>), g, dim3(1024), h.lds, s, q);
+}
+
 template <typename T, int V, bool BWD>
 static void run(const NormParams& p, const NormShape& h, hipStream_t s) {
     NormParams q = p;
@@ -875,12 +1058,9 @@ static void run(const NormParams& p, const NormShape& h, hipStream_t s) {
         q.slots = h.slots;
         q.lpg = h.lpg;
         const dim3 g((unsigned)h.short_blocks, (unsigned)h.tiles);
-        if (h.unit == 64)
-            hipLaunchKernelGGL((norm_short<T, V, 64, BWD>), g, dim3(256), h.lds, s, q);
-        else if (h.unit == 256)
-            hipLaunchKernelGGL((norm_short<T, V, 256, BWD>), g, dim3(256), h.lds, s, q);
-        else
-            hipLaunchKernelGGL((norm_short<T, V, 1024, BWD>), g, dim3(1024), h.lds, s, q);
+        // (of a width that is a multiple of V no chunk is moved back)
+        if (V > 1 && p.cg % V == 0) short_path<T, V, BWD, true>(q, h, g, s);
+        else short_path<T, V, BWD, false>(q, h, g, s);
     }
     if (!h.unit || h.long_tiles) {
         q.lpg = h.long_lpg;
@@ -903,12 +1083,14 @@ hipError_t launch_norm(NormParams p, const NormShape& h, int dtype, bool backwar
     p.lmax = h.lmax;
     p.tile_rows = h.tile_rows;
     p.stat_line = h.stat_line;
+    p.places = h.places;
+    if (!h.unit || !h.long_tiles) p.flags = nullptr;
     p.short_blocks = h.unit ? h.short_blocks : 0;
 #define MP_NORM(T, V)                              \
     if (backward) run<T, V, true>(p, h, s);        \
     else run<T, V, false>(p, h, s)
     if (dtype == MP_BF16) {
-        if (h.V == 8) { MP_NORM(BF16, 8); }
+        if (h.V == 4) { MP_NORM(BF16, 4); }
         else { MP_NORM(BF16, 1); }
     } else {
         if (h.V == 4) { MP_NORM(F32, 4); }
@@ -916,9 +1098,8 @@ hipError_t launch_norm(NormParams p, const NormShape& h, int dtype, bool backwar
     }
 #undef MP_NORM
     if (backward && p.part)
-        hipLaunchKernelGGL(norm_param_grads, dim3((unsigned)ceil_div(2 * p.F, kWave)),
-                           dim3(kGradWaves * kWave), 0, s, p, p.short_blocks + h.long_tiles, dgamma,
-                           dbeta);
+        hipLaunchKernelGGL(norm_param_grads, dim3((unsigned)ceil_div(2 * p.F, kGradCols)),
+                           dim3(kGradBlock), 0, s, p, h.long_tiles, dgamma, dbeta);
     return hipGetLastError();
 }
 
