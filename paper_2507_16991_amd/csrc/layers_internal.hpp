@@ -122,7 +122,7 @@ struct NormShape {
     int64_t lmax;           // rows of the longest short segment
     size_t lds;
     // long segments (long_tiles = 0: there can be none)
-    int64_t tile_rows, long_tiles, col_tile, stat_line, places;
+    int64_t tile_rows, apply_rows, long_tiles, col_tile, stat_line, places;
     int col_tiles, long_lpg;
     size_t long_lds;
 };
@@ -151,7 +151,7 @@ struct NormParams {
     float* part;
     int* flags;          // [short_blocks]: the short path's workgroups met a long segment
     // of the NormShape, filled by the launch
-    int64_t lmax, tile_rows, stat_line, places;
+    int64_t lmax, tile_rows, apply_rows, stat_line, places;
     int tile_groups, cpr, slots, lpg, short_blocks;
 };
 hipError_t launch_norm(NormParams p, const NormShape& h, int dtype, bool backward, float* dgamma,

@@ -8,7 +8,10 @@
 // Weights are the first operand and rows of x the second, so that a lane's
 // accumulators are neighbouring output columns of one row.
 //
-// x is quantised first (a quarter of its bytes); two kernels share the products out:
+// Three kernels share the products out; for the last two x is quantised first (a
+// quarter of its bytes):
+//   * mx_narrow: weights of a segment that fit into LDS, few output columns: x is
+//     quantised on the way; bound by reading x and writing out;
 //   * mx_thin: segments of few rows: bound by reading the weights, which go
 //     straight to registers, k split over the wavefronts of a workgroup;
 //   * mx_tiles: tiles staged through LDS by asynchronous loads.
@@ -177,9 +180,10 @@ __device__ inline int64_t seg_at(const MxParams& P, int64_t t) {
 }
 
 // Tile `tile` of the segments' rows in tiles of BM (no tile has rows of two):
-// its segment and rows, or t = -1 past the last.  64 segments a step.
+// its segment, rows and the segment's end, or t = -1 past the last.  64 segments a
+// step.
 struct RowTile {
-    int64_t t, r0, r1;
+    int64_t t, r0, r1, end;
 };
 __device__ inline RowTile row_tile(const MxParams& P, int64_t tile, int BM) {
     const int lane = threadIdx.x & 63;
@@ -203,11 +207,11 @@ __device__ inline RowTile row_tile(const MxParams& P, int64_t tile, int BM) {
             const int ni = __shfl(n, i);
             const int64_t first = before + __shfl(sum, i) - ni;
             const int64_t r0 = bi + (tile - first) * BM;
-            return RowTile{ti, r0, r0 + BM < ei ? r0 + BM : ei};
+            return RowTile{ti, r0, r0 + BM < ei ? r0 + BM : ei, ei};
         }
         before += __shfl(sum, 63);
     }
-    return RowTile{-1, 0, 0};
+    return RowTile{-1, 0, 0, 0};
 }
 
 __device__ inline i32x8 operand(const uint4& c) {
@@ -505,6 +509,193 @@ __global__ __launch_bounds__(kBlock) void mx_thin(MxParams P) {
     }
 }
 
+// ---- few output columns -------------------------------------------------------------------
+// The weights of a segment (CT column tiles of 32, KS steps of two blocks) stay in
+// LDS while a workgroup goes through a run of the segments' row tiles.  Each
+// wavefront has 32 rows to itself: it quantises them into its own part of LDS
+// (lanes along the row, so that loads are whole lines), multiplies, and hands the
+// results back through the same LDS, to write rows of out in whole pieces.
+// No wavefront waits for another but when the segment changes.
+constexpr int kNarrowRows = 32, kNarrowTile = 32 * 4;  // rows of a wavefront, of a workgroup
+constexpr int kNarrowCols = 4;                         // column tiles of a pass (accumulators)
+// floats to a row of results in LDS: two rows of a store lie on other banks
+constexpr int kNarrowLine = 32 * kNarrowCols + 4;
+
+// Bytes of LDS: weights, their scales, and per wavefront codes and scales of its rows or
+// its results.
+struct NarrowShape {
+    int cols, steps;  // padded: column tiles, steps of 64 along k
+    int mask, shift;  // of the order of a row's pieces
+    size_t w_codes, w_scales, wave, bytes;
+    // Place of a 16-byte piece within row r: exchanged in groups of a power of two that
+    // divides the row, so that 16 rows' pieces lie on different banks.
+    __device__ int at(int r, int piece) const { return piece ^ ((r >> shift) & mask); }
+};
+__host__ __device__ inline NarrowShape narrow_shape(int KB, int Fo) {
+    NarrowShape h;
+    h.cols = (Fo + 31) / 32;
+    h.steps = (KB + 1) / 2;
+    const int pieces = 2 * h.steps;
+    int g = 2;
+    h.shift = 3;
+    while (g < 16 && pieces % (2 * g) == 0) {
+        g *= 2;
+        --h.shift;
+    }
+    h.mask = g - 1;
+    h.w_codes = (size_t)h.cols * 32 * h.steps * 32;
+    h.w_scales = (size_t)h.cols * 32 * h.steps * 2;
+    const size_t in = (size_t)kNarrowRows * h.steps * (32 + 2);
+    const size_t out = (size_t)kNarrowRows * kNarrowLine * 4;
+    h.wave = in > out ? in : out;
+    h.wave = (h.wave + 15) & ~(size_t)15;
+    h.bytes = h.w_codes + ((h.w_scales + 15) & ~(size_t)15) + 4 * h.wave;
+    return h;
+}
+
+__device__ inline void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+template <typename T, bool BF>
+__global__ __launch_bounds__(kBlock) void mx_narrow(MxParams P, int64_t row_tiles) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t s_mem[];
+    const NarrowShape h = narrow_shape(P.KB, P.Fo);
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int pieces = 2 * h.steps;  // 16-byte pieces, blocks, of a row
+    uint8_t* s_wc = s_mem;
+    uint8_t* s_ws = s_wc + h.w_codes;
+    uint8_t* mine = s_ws + ((h.w_scales + 15) & ~(size_t)15) + w * h.wave;
+    uint8_t* s_xc = mine;
+    uint8_t* s_xs = s_xc + kNarrowRows * pieces * 16;
+    float* s_out = reinterpret_cast<float*>(mine);
+    const int row = lane & 31, half = lane >> 5;
+    const int64_t first = row_tiles * blockIdx.x / gridDim.x;
+    const int64_t last = row_tiles * (blockIdx.x + 1) / gridDim.x;
+    int64_t have = -1;  // the segment whose weights are in LDS
+    RowTile tile{-1, 0, 0, 0};
+    for (int64_t rt = first; rt < last; ++rt) {
+        if (tile.r1 < tile.end) {  // (the next of the same segment)
+            tile.r0 = tile.r1;
+            tile.r1 = tile.r0 + kNarrowTile < tile.end ? tile.r0 + kNarrowTile : tile.end;
+        } else {
+            tile = row_tile(P, rt, kNarrowTile);
+        }
+        if (tile.t < 0) return;  // (the same for the whole workgroup: no tile follows)
+        if (tile.t != have) {
+            __syncthreads();  // the others are done with the old weights
+            const uint8_t* wc = P.w_codes + tile.t * P.Fo * P.KB * 16;
+            const uint8_t* ws = P.w_scales + tile.t * P.Fo * P.KB;
+            for (int i = tid; i < h.cols * 32 * pieces; i += kBlock) {
+                const int c = i / pieces, k = i - c * pieces;
+                const bool in = c < P.Fo && k < P.KB;
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (in) v = reinterpret_cast<const uint4*>(wc)[(int64_t)c * P.KB + k];
+                reinterpret_cast<uint4*>(s_wc)[c * pieces + h.at(c, k)] = v;
+                s_ws[c * pieces + k] = in ? ws[(int64_t)c * P.KB + k] : 0;
+            }
+            __syncthreads();
+            have = tile.t;
+        }
+        const int64_t r0 = tile.r0 + w * kNarrowRows;
+        const int rows = tile.r1 - r0 < kNarrowRows ? (int)(tile.r1 - r0) : kNarrowRows;
+        if (rows <= 0) continue;
+        // eight values a lane: four lanes a block, `per` lanes a row
+        const int per = 4 * pieces, units = kNarrowRows * per;
+        const typename T::raw* x = static_cast<const typename T::raw*>(P.x) + r0 * P.ldx;
+        for (int i0 = 0; i0 < units; i0 += 4 * kWave) {
+            RawOf<T, 8> v[4];
+            int r[4], j[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int i = i0 + u * kWave + lane;
+                r[u] = i / per;
+                j[u] = i - r[u] * per;
+                const int rc = r[u] < rows ? r[u] : rows - 1;  // (rows past the end are not stored)
+                v[u] = load8<T>(x + rc * P.ldx, 8 * j[u], P.K);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                uint32_t sc;
+                const uint32_t c = quantize8<T>(v[u], sc);
+                if (i0 + u * kWave + lane < units) {
+                    const int k = j[u] >> 2;
+                    reinterpret_cast<uint32_t*>(s_xc)[(r[u] * pieces + h.at(r[u], k)) * 4 + (j[u] & 3)] = c;
+                    if ((j[u] & 3) == 0) s_xs[r[u] * pieces + k] = (uint8_t)sc;
+                }
+            }
+        }
+        wave_sync();
+        for (int ct0 = 0; ct0 < h.cols; ct0 += kNarrowCols) {
+            f32x16 acc[kNarrowCols];
+#pragma unroll
+            for (int i = 0; i < kNarrowCols; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[i][v] = 0.f;
+            for (int st = 0; st < h.steps; ++st) {
+                const int k = 2 * st + half;
+                const i32x8 b = operand(
+                    reinterpret_cast<const uint4*>(s_xc)[row * pieces + h.at(row, k)]);
+                const int sb = s_xs[row * pieces + k];
+#pragma unroll
+                for (int i = 0; i < kNarrowCols; ++i) {
+                    if (ct0 + i < h.cols) {
+                        const int c = (ct0 + i) * 32 + row;
+                        const i32x8 a = operand(
+                            reinterpret_cast<const uint4*>(s_wc)[c * pieces + h.at(c, k)]);
+                        acc[i] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                            a, b, acc[i], kFp4, kFp4, 0, (int)s_ws[c * pieces + k], 0, sb);
+                    }
+                }
+            }
+            const int cols = P.Fo - ct0 * 32 < 32 * kNarrowCols ? P.Fo - ct0 * 32 : 32 * kNarrowCols;
+            if (ct0 + kNarrowCols >= h.cols) {
+                // the last columns: the rows' codes make room for the results
+                wave_sync();
+#pragma unroll
+                for (int i = 0; i < kNarrowCols; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float4 v = make_float4(acc[i][4 * q], acc[i][4 * q + 1],
+                                                     acc[i][4 * q + 2], acc[i][4 * q + 3]);
+                        *reinterpret_cast<float4*>(&s_out[row * kNarrowLine + i * 32 + 8 * q + 4 * half]) = v;
+                    }
+                wave_sync();
+                constexpr int E = BF ? 8 : 4;  // columns of a 16-byte store
+                const int64_t o0 = r0 * P.Fo + ct0 * 32;
+                const int per_row = (cols + E - 1) / E;
+                for (int i = lane; i < rows * per_row; i += kWave) {
+                    const int rr = i / per_row, c = (i - rr * per_row) * E;
+                    float v[E];
+#pragma unroll
+                    for (int e = 0; e < E; ++e) v[e] = s_out[rr * kNarrowLine + c + e];
+                    const int64_t o = o0 + (int64_t)rr * P.Fo + c;
+                    if (c + E <= cols) {
+                        if (BF) store_floats<BF16, E>(static_cast<uint16_t*>(P.out) + o, v);
+                        else store_floats<F32, E>(static_cast<float*>(P.out) + o, v);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < E; ++e)
+                            if (c + e < cols) store_col<BF>(P.out, o + e, v[e]);
+                    }
+                }
+                wave_sync();
+            } else if (row < rows) {
+#pragma unroll
+                for (int i = 0; i < kNarrowCols; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float v[4] = {acc[i][4 * q], acc[i][4 * q + 1], acc[i][4 * q + 2],
+                                            acc[i][4 * q + 3]};
+                        store4<BF>(P.out, (r0 + row) * P.Fo + (ct0 + i) * 32 + 8 * q + 4 * half, v);
+                    }
+            }
+        }
+    }
+}
+
 }  // namespace
 
 hipError_t launch_mx_quantize(const void* x, int dtype, int64_t N, int64_t K, int64_t ldx,
@@ -562,12 +753,30 @@ static hipError_t tiles(const MxParams& p, int bf, hipStream_t s) {
 hipError_t launch_mx_product(const MxParams& p, int x_dtype, int out_dtype, hipStream_t s) {
     if (p.N <= 0) return hipSuccess;
     const int bf = out_dtype == MP_BF16;
+    const int64_t thin = row_tiles_bound(p, kThinRows);
+    const bool few = p.N <= 16 * p.T + 16 && thin <= 65535;
+    // At most 256 columns and 96 KB of LDS (weights and four wavefronts' rows): one read
+    // of x, and no codes in memory.
+    const NarrowShape h = narrow_shape(p.KB, p.Fo);
+    if (!few && p.Fo <= 256 && h.bytes <= (96 << 10)) {
+        const int64_t rt = row_tiles_bound(p, kNarrowTile);
+        const int per_cu = h.bytes <= (40 << 10) ? 4 : (h.bytes <= (53 << 10) ? 3 : (h.bytes <= (80 << 10) ? 2 : 1));
+        const int64_t most = 256 * per_cu;
+        const dim3 g((unsigned)(rt < most ? rt : most)), b(kBlock);
+        if (x_dtype == MP_BF16) {
+            if (bf) hipLaunchKernelGGL((mx_narrow<BF16, true>), g, b, h.bytes, s, p, rt);
+            else hipLaunchKernelGGL((mx_narrow<BF16, false>), g, b, h.bytes, s, p, rt);
+        } else {
+            if (bf) hipLaunchKernelGGL((mx_narrow<F32, true>), g, b, h.bytes, s, p, rt);
+            else hipLaunchKernelGGL((mx_narrow<F32, false>), g, b, h.bytes, s, p, rt);
+        }
+        return hipGetLastError();
+    }
     hipError_t e = launch_mx_quantize(p.x, x_dtype, p.N, p.K, p.ldx, p.x_codes, p.x_scales, nullptr,
                                       s);
     if (e != hipSuccess) return e;
     // few rows a segment: the weights are what is read
-    const int64_t thin = row_tiles_bound(p, kThinRows);
-    if (p.N <= 16 * p.T + 16 && thin <= 65535) {
+    if (few) {
         const dim3 g((unsigned)ceil_div(p.Fo, kThinCols), (unsigned)thin), b(kBlock);
         if (bf) hipLaunchKernelGGL(mx_thin<true>, g, b, 0, s, p);
         else hipLaunchKernelGGL(mx_thin<false>, g, b, 0, s, p);

@@ -291,7 +291,6 @@ __device__ inline void row_stats(const Rows<T>& rows, const Param<V, M>& p, int 
             }
             if constexpr (!BWD) {
                 const float fn = (float)nb, f0 = (float)i0;
-                const float inb = __builtin_amdgcn_rcpf(fn);
                 const float share = fn * __builtin_amdgcn_rcpf(f0 + fn);
                 float m[V] = {}, q[V] = {};
 #pragma unroll
@@ -302,7 +301,8 @@ __device__ inline void row_stats(const Rows<T>& rows, const Param<V, M>& p, int 
                     for (int v = 0; v < V; ++v) m[v] += i < nb ? f[v] : 0.f;
                 }
 #pragma unroll
-                for (int v = 0; v < V; ++v) m[v] *= inb;
+                for (int v = 0; v < V; ++v)  // (quotients: equal rows give their own mean)
+                    m[v] = nb == R ? m[v] * (1.f / R) : m[v] / fn;
 #pragma unroll
                 for (int i = 0; i < R; ++i) {
                     float f[V];
@@ -560,7 +560,7 @@ __global__ __launch_bounds__(short_block(UNIT), 4) void norm_short(NormParams P)
                     entries(g, [&](int i, int at) {
                         a = __builtin_fmaf(width * (float)rows_of_slot(n, i, slots), ent[at], a);
                     });
-                a = over_threads(a) * inv;
+                a = over_threads(a) / ((float)n * (float)cg);
                 if (on)
                     entries(g, [&](int i, int at) {
                         const int r = rows_of_slot(n, i, slots);
@@ -838,19 +838,23 @@ __global__ __launch_bounds__(kJoin) void norm_long_join(NormParams P, int gw, in
                 const int64_t g = g1 + gi;
                 const bool ok = g < P.G;
                 const int64_t cb = g * P.cg, ce = cb + P.cg;
-                const int64_t y0 = cb / col_tile, ny = ok ? (ce - 1) / col_tile - y0 + 1 : 0;
-                const int64_t parts = (t1 - t0 + 1) * ny;
+                const int64_t y0 = cb / col_tile;
+                const int ny = ok ? (int)((ce - 1) / col_tile - y0) + 1 : 0;
+                const int parts = (int)(t1 - t0 + 1) * ny;
+                // (only in its first tile can a segment have another place than 0)
+                const int64_t at0 = t0 * P.places + place_of(P, b, t0 * P.tile_rows);
                 const auto each = [&](auto f) {
-#pragma unroll 4
-                    for (int64_t i = q; i < parts; i += Q) {
-                        const int64_t tile = t0 + i / ny, y = y0 + i % ny;
-                        const int64_t at = tile * P.places + place_of(P, b, tile * P.tile_rows);
+#pragma unroll 8
+                    for (int i = q; i < parts; i += Q) {
+                        const int dt = ny == 1 ? i : i / ny;
+                        const int64_t tile = t0 + dt, y = y0 + (i - dt * ny);
+                        const int64_t at = dt ? tile * P.places : at0;
                         const float2 v = reinterpret_cast<const float2*>(P.stats)[at * P.stat_line + y + g];
-                        const int64_t ra = tile * P.tile_rows > b ? tile * P.tile_rows : b;
+                        const int64_t ra = dt ? tile * P.tile_rows : b;
                         const int64_t rb = (tile + 1) * P.tile_rows < e ? (tile + 1) * P.tile_rows : e;
                         const int64_t ca = y * col_tile > cb ? y * col_tile : cb;
                         const int64_t cz = (y + 1) * col_tile < ce ? (y + 1) * col_tile : ce;
-                        f(v, (float)(rb - ra) * (float)(cz - ca));
+                        f(v, (float)(int)(rb - ra) * (float)(int)(cz - ca));
                     }
                 };
                 const auto total = [&](float* s_v, float v) {
@@ -879,7 +883,7 @@ __global__ __launch_bounds__(kJoin) void norm_long_join(NormParams P, int gw, in
                 } else {
                     float m = 0.f, M2 = 0.f;
                     each([&](float2 v, float n) { m = __builtin_fmaf(v.x, n, m); });
-                    m = total(s_sum, m) * inv;
+                    m = total(s_sum, m) / ((float)(e - b) * (float)P.cg);
                     each([&](float2 v, float n) {
                         const float u = v.x - m;
                         M2 += __builtin_fmaf(u * u, n, v.y);
@@ -895,8 +899,8 @@ __global__ __launch_bounds__(kJoin) void norm_long_join(NormParams P, int gw, in
     }
 }
 
-// The tiles again, from the last to the first (the last are still in the caches):
-// out, or dx.
+// The long segments' rows again, in tiles of apply_rows from the last to the first
+// (the last rows are still in the caches): out, or dx.
 template <typename T, int V, bool BWD>
 __global__ __launch_bounds__(kLong, 4) void norm_long_apply(NormParams P) {
     typedef typename T::raw raw;
@@ -905,8 +909,8 @@ __global__ __launch_bounds__(kLong, 4) void norm_long_apply(NormParams P) {
     const LongTile<V> lt(P);
     const Chunk<V> ck(t, lt.cpr, lt.slots, lt.W);
     const int64_t tile = (int64_t)gridDim.x - 1 - blockIdx.x;
-    const int64_t row0 = tile * P.tile_rows;
-    const int64_t row1 = row0 + P.tile_rows < P.N ? row0 + P.tile_rows : P.N;
+    const int64_t row0 = tile * P.apply_rows;
+    const int64_t row1 = row0 + P.apply_rows < P.N ? row0 + P.apply_rows : P.N;
     const int64_t cc = lt.c0 + ck.c;
     const Groups<V> lg(cc, P.cg);
     const raw* x = static_cast<const raw*>(P.x) + cc;
@@ -1022,9 +1026,13 @@ NormShape norm_shape(int64_t N, int64_t S, int64_t F, int64_t G, int dtype, int 
     }
     h.col_tile = kLong * (int64_t)h.V;
     if (N > h.lmax) {
-        int64_t r = ceil_div(N, 2048);
-        if (r < 32) r = 32;
+        // 4096 tiles for the statistics (2048 leave the last round of workgroups half
+        // empty, 8192 have twice the partials to join), 8192 for the second read
+        // and tiles of 32 KB at the least
+        const int64_t least = ceil_div(32 << 10, F * (dtype == MP_BF16 ? 2 : 4));
+        const int64_t r = ceil_div(N, 4096) < least ? least : ceil_div(N, 4096);
         h.tile_rows = r;
+        h.apply_rows = ceil_div(N, 8192) < least ? least : ceil_div(N, 8192);
         h.places = 2 + (r - 1) / (h.lmax + 1);
         h.long_tiles = ceil_div(N, r);
         h.col_tiles = (int)ceil_div(F, h.col_tile);
@@ -1073,7 +1081,9 @@ static void run(const NormParams& p, const NormShape& h, hipStream_t s) {
             hipLaunchKernelGGL((norm_long_join<BWD>), dim3((unsigned)jb), dim3(kJoin), 0, s, q, gw,
                                h.col_tile);
             if (h.long_tiles)
-                hipLaunchKernelGGL((norm_long_apply<T, V, BWD>), g, dim3(kLong), 0, s, q);
+                hipLaunchKernelGGL((norm_long_apply<T, V, BWD>),
+                                   dim3((unsigned)ceil_div(p.N, h.apply_rows), (unsigned)h.col_tiles),
+                                   dim3(kLong), 0, s, q);
         }
     }
 }
@@ -1084,6 +1094,7 @@ hipError_t launch_norm(NormParams p, const NormShape& h, int dtype, bool backwar
     p.tile_rows = h.tile_rows;
     p.stat_line = h.stat_line;
     p.places = h.places;
+    p.apply_rows = h.apply_rows;
     if (!h.unit || !h.long_tiles) p.flags = nullptr;
     p.short_blocks = h.unit ? h.short_blocks : 0;
 #define MP_NORM(T, V)                              \
