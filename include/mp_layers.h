@@ -182,8 +182,9 @@ int mp_mx_quantize(const void* x, int dtype, int64_t N, int64_t K, int64_t ldx, 
 int mp_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t N, int64_t K,
                      void* out, int dtype, void* stream);
 
-/* Workspace bytes of mp_mx_segment_matmul (the rows' codes and scales). */
-int mp_mx_segment_matmul_workspace(int64_t N, int64_t K, size_t* bytes);
+/* Workspace bytes of mp_mx_segment_matmul (the rows' codes and scales, and all
+ * scales in the order in which they are read). */
+int mp_mx_segment_matmul_workspace(int64_t T, int64_t N, int64_t K, int64_t Fo, size_t* bytes);
 
 /* out[r, o] = sum over k of q(x)[r, k] * W[t][o, k] for the rows r of segment t:
  * mp_segment_matmul for serving, on 4-bit matrix cores, with W quantised

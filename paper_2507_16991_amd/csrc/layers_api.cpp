@@ -60,6 +60,27 @@ int norm_call(const void* ptr, int ptr_itype, int64_t ldx, int64_t F, int act, i
     return MP_OK;
 }
 
+int mx_dims(int64_t T, int64_t N, int64_t K, int64_t Fo) {
+    if (N < 0 || N > INT32_MAX || T < 1 || T > 4096 || K < 1 || K > kMaxF || Fo < 1 || Fo > kMaxF)
+        return MP_ERR_SIZE;
+    return MP_OK;
+}
+
+// Workspace of the 4-bit product: the rows' codes and scales, and both operands'
+// scales in words of four.
+struct MxSpace {
+    size_t x_scales, x_words, w_words, bytes;
+};
+MxSpace mx_space(int64_t T, int64_t N, int64_t K, int64_t Fo) {
+    const size_t KB = (size_t)ceil_div(K, 32), KS = (KB + 3) / 4;
+    MxSpace m;
+    m.x_scales = align_up((size_t)N * KB * 16, 256);
+    m.x_words = m.x_scales + align_up((size_t)N * KB, 256);
+    m.w_words = m.x_words + align_up((size_t)N * KS * 4, 256);
+    m.bytes = m.w_words + align_up((size_t)T * (size_t)Fo * KS * 4, 256);
+    return m;
+}
+
 int route_dims(int dtype, int64_t N, int64_t E, int64_t ldl, int64_t k) {
     if (!valid_dtype(dtype)) return MP_ERR_DTYPE;
     if (N < 0 || N > INT32_MAX || E < 1 || E > 1024 || ldl < E || k < 1 || k > 64 || k > E ||
@@ -283,11 +304,11 @@ int mp_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t N, int
     return hip_status(launch_mx_dequantize(codes, scales, N, K, out, dtype, as_stream(stream)));
 }
 
-int mp_mx_segment_matmul_workspace(int64_t N, int64_t K, size_t* bytes) {
+int mp_mx_segment_matmul_workspace(int64_t T, int64_t N, int64_t K, int64_t Fo, size_t* bytes) {
     if (!bytes) return MP_ERR_NULL;
-    if (N < 0 || N > INT32_MAX || K < 1 || K > kMaxF) return MP_ERR_SIZE;
-    const size_t blocks = (size_t)N * (size_t)ceil_div(K, 32);
-    *bytes = align_up(blocks * 16, 256) + align_up(blocks, 256);
+    const int st = mx_dims(T, N, K, Fo);
+    if (st != MP_OK) return st;
+    *bytes = mx_space(T, N, K, Fo).bytes;
     return MP_OK;
 }
 
@@ -297,16 +318,16 @@ int mp_mx_segment_matmul(const void* seg, int seg_itype, int64_t T, const void* 
                          size_t ws_bytes, void* stream) {
     if (!valid_itype(seg_itype) || !valid_dtype(x_dtype) || !valid_dtype(out_dtype))
         return MP_ERR_DTYPE;
-    if (N < 0 || N > INT32_MAX || T < 1 || T > 4096 || K < 1 || K > kMaxF || ldx < K || Fo < 1 ||
-        Fo > kMaxF)
-        return MP_ERR_SIZE;
+    const int st = mx_dims(T, N, K, Fo);
+    if (st != MP_OK) return st;
+    if (ldx < K) return MP_ERR_SIZE;
     if (!seg || !w_codes || !w_scales || (N > 0 && (!x || !out || !ws))) return MP_ERR_NULL;
     if (!aligned(seg, seg_itype == MP_I64 ? 8 : 4) || !aligned(x, elem(x_dtype)) ||
         !aligned(w_codes, 16) || !aligned(out, elem(out_dtype)) || !aligned(ws, 16))
         return MP_ERR_ALIGN;
-    size_t need = 0;
-    mp_mx_segment_matmul_workspace(N, K, &need);
-    if (ws_bytes < need) return MP_ERR_WORKSPACE;
+    const MxSpace m = mx_space(T, N, K, Fo);
+    if (ws_bytes < m.bytes) return MP_ERR_WORKSPACE;
+    uint8_t* w = static_cast<uint8_t*>(ws);
     MxParams P{};
     P.seg = seg;
     P.seg64 = seg_itype == MP_I64;
@@ -319,8 +340,10 @@ int mp_mx_segment_matmul(const void* seg, int seg_itype, int64_t T, const void* 
     P.Fo = (int)Fo;
     P.w_codes = w_codes;
     P.w_scales = w_scales;
-    P.x_codes = static_cast<uint8_t*>(ws);
-    P.x_scales = P.x_codes + align_up((size_t)N * (size_t)P.KB * 16, 256);
+    P.x_codes = w;
+    P.x_scales = w + m.x_scales;
+    P.x_words = reinterpret_cast<uint32_t*>(w + m.x_words);
+    P.w_words = reinterpret_cast<uint32_t*>(w + m.w_words);
     P.out = out;
     return hip_status(launch_mx_product(P, x_dtype, out_dtype, as_stream(stream)));
 }

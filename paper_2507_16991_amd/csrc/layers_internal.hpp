@@ -188,6 +188,8 @@ struct MxParams {
     const uint8_t* w_scales;  // [T, Fo, KB]
     uint8_t* x_codes;         // workspace [N, KB * 16]
     uint8_t* x_scales;        // workspace [N, KB]
+    uint32_t* x_words;        // workspace [KS, N]: the scales by steps of four blocks
+    uint32_t* w_words;        // workspace [T, KS, Fo]
     void* out;
 };
 hipError_t launch_mx_quantize(const void* x, int dtype, int64_t N, int64_t K, int64_t ldx,

@@ -231,122 +231,131 @@ __device__ inline void store_col(void* out, int64_t at, float v) {
 
 // ---- tiles ------------------------------------------------------------------------------
 // A workgroup of WM x WN wavefronts has 32 FM WM output columns x 32 FN WN rows, a
-// wavefront FM x FN products of 32 x 32.  k in steps of 8 blocks (128 bytes a row),
-// two buffers: while one is multiplied, asynchronous loads fill the other.
-// In LDS the 16-byte pieces of row r lie at piece ^ (r % 8), so that the
+// wavefront FM x FN products of 32 x 32.  k in steps of 4 blocks (64 bytes a row),
+// three buffers: while one is multiplied, asynchronous loads fill the others.  Steps
+// are that short so that two workgroups fit into a CU's LDS, and one multiplies
+// while the other writes its results.
+// In LDS the 16-byte pieces of row r lie at piece ^ (r / 4 % 4), so that the
 // lanes of a fragment (32 rows, one piece) spread over the banks.
-constexpr int kStep = 8;  // blocks of a step
+constexpr int kStep = 4;  // blocks of a step
 constexpr int kRowBytes = kStep * 16;
 
 template <int ROWS>
 struct TileBuffer {
     uint8_t codes[ROWS * kRowBytes];
-    uint2 scales[ROWS];
+    uint32_t scales[ROWS];
 };
 
-// A workgroup's loads of ROWS rows of codes and scales, blocks kb0 .. kb0+7 at a
-// time.  Rows past `rows` repeat the last one (their products are not stored),
-// blocks past KB the last one, under scales of 0: both factors are then 2^-127,
-// and such products vanish.
+// A workgroup's asynchronous loads of ROWS rows, blocks 4 k .. 4 k + 3 of step k.  Rows
+// past `rows` repeat the last one (their products are not stored), blocks past KB
+// the last one, under scales of 0: both factors are then 2^-127, and such products
+// vanish.
 template <int ROWS, int WAVES>
 struct TileLoader {
-    static constexpr int PER = ROWS / 8 / WAVES;  // loads of a wavefront, 8 rows each
+    static constexpr int PER = ROWS / 16 / WAVES;  // loads of a wavefront, 16 rows each
+    static constexpr int LOADS = PER + 1;
     const uint8_t* codes;
-    const uint8_t* scales;  // this thread's row
+    const uint32_t* scales;  // [step][line]: this lane's row of step 0
+    int64_t line;
     uint32_t off[PER];
-    int KB, piece;
-    uint64_t s;
+    int KB, piece, first;    // first: row of this wavefront's scales
 
-    // stride: bytes from one row's scales to the next
-    __device__ TileLoader(const uint8_t* c, const uint8_t* sc, int rows, int kb, int stride) {
-        const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, tid = threadIdx.x;
+    __device__ TileLoader(const uint8_t* c, const uint32_t* sc, int64_t sc_line, int rows, int kb) {
+        const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
         codes = c;
         KB = kb;
-        piece = (lane & 7) ^ (lane >> 3);
+        line = sc_line;
+        piece = (lane & 3) ^ ((lane >> 4) & 3);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int r = (w * PER + i) * 8 + (lane >> 3);
+            const int r = (w * PER + i) * 16 + (lane >> 2);
             off[i] = (uint32_t)((r < rows ? r : rows - 1) * kb) * 16u;
         }
-        scales = sc + (int64_t)(tid < rows ? tid : rows - 1) * stride;
-        s = 0;
+        first = w % (ROWS / 64) * 64;  // (of fewer than 64 rows a wavefront, some load the same)
+        const int r = first + lane;
+        scales = sc + (r < rows ? r : rows - 1);
     }
-    __device__ void fetch_codes(uint8_t* lds, int kb0) const {
-        const int w = threadIdx.x >> 6;
-        const uint32_t at = (uint32_t)(kb0 + piece < KB ? kb0 + piece : KB - 1) * 16u;
+    __device__ void fetch(TileBuffer<ROWS>& to, int k) const {
+        const int w = threadIdx.x >> 6, kb = k * kStep + piece;
+        const uint32_t at = (uint32_t)(kb < KB ? kb : KB - 1) * 16u;
 #pragma unroll
         for (int i = 0; i < PER; ++i)
             __builtin_amdgcn_global_load_lds(
                 (const __attribute__((address_space(1))) void*)(codes + (off[i] + at)),
-                (__attribute__((address_space(3))) void*)(lds + (w * PER + i) * 8 * kRowBytes), 16,
-                0, 0);
-    }
-    // KB >= 8: eight bytes that end with the row at the latest
-    __device__ void fetch_scales(int kb0) {
-        const int k = kb0 + kStep <= KB ? kb0 : KB - kStep;
-        __builtin_memcpy(&s, scales + k, 8);
-    }
-    __device__ uint64_t scales_of(int kb0) const {
-        const int past = kb0 + kStep - KB;
-        return past > 0 ? s >> (8 * past) : s;
-    }
-    __device__ void fetch_few_scales() {  // KB < 8
-        s = 0;
-        for (int i = 0; i < KB; ++i) s |= (uint64_t)scales[i] << (8 * i);
+                (__attribute__((address_space(3))) void*)(to.codes + (w * PER + i) * 16 * kRowBytes),
+                16, 0, 0);
+        __builtin_amdgcn_global_load_lds(
+            (const __attribute__((address_space(1))) void*)(scales + k * line),
+            (__attribute__((address_space(3))) void*)(to.scales + first), 4, 0, 0);
     }
 };
+
+// The scales of R rows, [R, KB] bytes, as a table of words [KS, R]: word (k, r) has those
+// of row r in step k, 0 past KB.  Tiles then load a step's scales as whole lines
+// (from the format's own layout every row is a request of its own: half of all
+// requests to L2, which bound the product: 1170 -> 640 us at 65,536 x 4096 x 4096).
+struct ScaleTable {
+    const uint8_t* in;
+    uint32_t* out;
+    int64_t R, lines;  // rows; rows to a table of words (the segments' weights have one each)
+};
+__global__ __launch_bounds__(kBlock) void mx_scale_words(ScaleTable A, ScaleTable B, int KB, int KS,
+                                                         int64_t blocks_a) {
+    const bool second = (int64_t)blockIdx.x >= blocks_a;
+    const ScaleTable t = second ? B : A;
+    const int64_t r = ((int64_t)blockIdx.x - (second ? blocks_a : 0)) * kBlock + threadIdx.x;
+    if (r >= t.R) return;
+    const int64_t table = t.R == t.lines ? 0 : r / t.lines, in_table = r - table * t.lines;
+    const uint8_t* p = t.in + r * KB;
+    uint32_t* q = t.out + table * KS * t.lines + in_table;
+    const int k0 = blockIdx.y * 4;
+    uint32_t w[4] = {0, 0, 0, 0};
+    if (4 * k0 + 16 <= KB) {
+        __builtin_memcpy(w, p + 4 * k0, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (4 * k0 + i < KB) w[i / 4] |= (uint32_t)p[4 * k0 + i] << (8 * (i % 4));
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (k0 + i < KS) q[(k0 + i) * t.lines] = w[i];
+}
 
 template <int FM, int FN, int BM, int BN>
 __device__ inline void multiply(const TileBuffer<BM>& W, const TileBuffer<BN>& X, int wm,
                                 int wn, int lane, f32x16 (&acc)[FM][FN]) {
     const int half = lane >> 5, row = lane & 31;
-    uint2 sw[FM], sx[FN];
+    int sw[FM], sx[FN];  // byte 2 s is the scale of block 2 s + half
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-        sw[i] = W.scales[(wm * FM + i) * 32 + row];
-        sw[i].x >>= 8 * half;  // now byte 2 (s % 2) is the scale of block 2 s + half
-        sw[i].y >>= 8 * half;
-    }
+    for (int i = 0; i < FM; ++i) sw[i] = (int)(W.scales[(wm * FM + i) * 32 + row] >> (8 * half));
 #pragma unroll
-    for (int j = 0; j < FN; ++j) {
-        sx[j] = X.scales[(wn * FN + j) * 32 + row];
-        sx[j].x >>= 8 * half;
-        sx[j].y >>= 8 * half;
-    }
-    // the next fragments are read while these are multiplied; the scheduling
-    // barriers keep more of them from being read ahead, which spills
+    for (int j = 0; j < FN; ++j) sx[j] = (int)(X.scales[(wn * FN + j) * 32 + row] >> (8 * half));
     uint4 a[2][FM], b[2][FN];
-    const auto read = [&](int s, uint4 (&fa)[FM], uint4 (&fb)[FN]) {
-        const int at = ((2 * s + half) ^ (row & 7)) * 16;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        const int at = ((2 * s + half) ^ ((row >> 2) & 3)) * 16;
 #pragma unroll
         for (int i = 0; i < FM; ++i)
-            fa[i] = *reinterpret_cast<const uint4*>(
+            a[s][i] = *reinterpret_cast<const uint4*>(
                 &W.codes[((wm * FM + i) * 32 + row) * kRowBytes + at]);
 #pragma unroll
         for (int j = 0; j < FN; ++j)
-            fb[j] = *reinterpret_cast<const uint4*>(
+            b[s][j] = *reinterpret_cast<const uint4*>(
                 &X.codes[((wn * FN + j) * 32 + row) * kRowBytes + at]);
-    };
-    read(0, a[0], b[0]);
-#pragma unroll
-    for (int s = 0; s < kStep / 2; ++s) {
-        if (s + 1 < kStep / 2) read(s + 1, a[(s + 1) & 1], b[(s + 1) & 1]);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int i = 0; i < FM; ++i)
-#pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                const int si = (int)(s < 2 ? sw[i].x : sw[i].y), sj = (int)(s < 2 ? sx[j].x : sx[j].y);
-                const i32x8 va = operand(a[s & 1][i]), vb = operand(b[s & 1][j]);
-                if (s & 1)
-                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-                        va, vb, acc[i][j], kFp4, kFp4, 2, si, 2, sj);
-                else
-                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-                        va, vb, acc[i][j], kFp4, kFp4, 0, si, 0, sj);
-            }
-        __builtin_amdgcn_sched_barrier(0);
     }
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                operand(a[0][i]), operand(b[0][j]), acc[i][j], kFp4, kFp4, 0, sw[i], 0, sx[j]);
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                operand(a[1][i]), operand(b[1][j]), acc[i][j], kFp4, kFp4, 2, sw[i], 2, sx[j]);
     // the products stay here: the compiler would sink them past the workgroup's
     // barrier, with all fragments in registers until then
 #pragma unroll
@@ -355,83 +364,29 @@ __device__ inline void multiply(const TileBuffer<BM>& W, const TileBuffer<BN>& X
         for (int j = 0; j < FN; ++j) asm volatile("" : "+v"(acc[i][j]));
 }
 
-template <int FM, int FN, int WM, int WN, bool BF>
-__global__ __launch_bounds__(64 * WM * WN) void mx_tiles(MxParams P, int64_t row_tiles,
-                                                         int col_tiles) {
-    constexpr int BM = 32 * FM * WM, BN = 32 * FN * WN;  // output columns, rows
-    static_assert(64 * WM * WN >= BM && 64 * WM * WN >= BN, "a thread a row of scales");
-    __shared__ __attribute__((aligned(16))) TileBuffer<BM> W0, W1;
-    __shared__ __attribute__((aligned(16))) TileBuffer<BN> X0, X1;
-    // Workgroups go to the XCDs in turn; each XCD has a run of tiles, in
-    // bands of eight row tiles, so that its L2 serves rows and columns again.
+// Workgroups go to the XCDs in turn; each XCD has a run of tiles, in bands of
+// eight row tiles, so that its L2 serves rows and columns again.  False: none left.
+__device__ inline bool pick_tile(int64_t row_tiles, int col_tiles, int64_t& rt, int& ct) {
     const int64_t total = row_tiles * col_tiles, per = (total + 7) / 8;
     const int64_t lin = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    if (lin >= total) return;
+    if (lin >= total) return false;
     const int64_t band = lin / (8 * col_tiles), in = lin - band * 8 * col_tiles;
     const int64_t high = row_tiles - band * 8 < 8 ? row_tiles - band * 8 : 8;
-    const int64_t rt = band * 8 + in % high;
-    const int ct = (int)(in / high);
-    const RowTile tile = row_tile(P, rt, BN);
-    if (tile.t < 0) return;
-    const int KB = P.KB, rows = (int)(tile.r1 - tile.r0);
-    const int c0 = ct * BM, cols = P.Fo - c0 < BM ? P.Fo - c0 : BM;
-    const uint8_t* wc = P.w_codes + (tile.t * P.Fo + c0) * KB * 16;
-    const uint8_t* ws = P.w_scales + (tile.t * P.Fo + c0) * KB;
-    const uint8_t* xc = P.x_codes + tile.r0 * KB * 16;
-    const uint8_t* xs = P.x_scales + tile.r0 * KB;
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, wm = w % WM, wn = w / WM;
+    rt = band * 8 + in % high;
+    ct = (int)(in / high);
+    return true;
+}
 
-    f32x16 acc[FM][FN];
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
-
-    TileLoader<BM, WM * WN> lw(wc, ws, cols, KB, KB);
-    TileLoader<BN, WM * WN> lx(xc, xs, rows, KB, KB);
-    const auto settle = [&](TileBuffer<BM>& Wb, TileBuffer<BN>& Xb, int kb0) {
-        if (tid < BM) Wb.scales[tid] = __builtin_bit_cast(uint2, lw.scales_of(kb0));
-        if (tid < BN) Xb.scales[tid] = __builtin_bit_cast(uint2, lx.scales_of(kb0));
-        __builtin_amdgcn_s_waitcnt(0);  // the asynchronous loads too
-        __syncthreads();
-    };
-    const auto fetch = [&](TileBuffer<BM>& Wb, TileBuffer<BN>& Xb, int kb0) {
-        lw.fetch_codes(Wb.codes, kb0);
-        lx.fetch_codes(Xb.codes, kb0);
-        lw.fetch_scales(kb0);
-        lx.fetch_scales(kb0);
-    };
-    const int steps = (KB + kStep - 1) / kStep;
-    if (KB >= kStep) {
-        fetch(W0, X0, 0);
-        settle(W0, X0, 0);
-    } else {
-        lw.fetch_codes(W0.codes, 0);
-        lx.fetch_codes(X0.codes, 0);
-        lw.fetch_few_scales();
-        lx.fetch_few_scales();
-        if (tid < BM) W0.scales[tid] = __builtin_bit_cast(uint2, lw.s);
-        if (tid < BN) X0.scales[tid] = __builtin_bit_cast(uint2, lx.s);
-        __builtin_amdgcn_s_waitcnt(0);
-        __syncthreads();
-    }
-    int k = 0;
-    for (; k + 1 < steps; k += 2) {
-        fetch(W1, X1, (k + 1) * kStep);
-        multiply<FM, FN, BM, BN>(W0, X0, wm, wn, lane, acc);
-        settle(W1, X1, (k + 1) * kStep);
-        if (k + 2 < steps) fetch(W0, X0, (k + 2) * kStep);
-        multiply<FM, FN, BM, BN>(W1, X1, wm, wn, lane, acc);
-        if (k + 2 < steps) settle(W0, X0, (k + 2) * kStep);
-    }
-    if (k < steps) multiply<FM, FN, BM, BN>(W0, X0, wm, wn, lane, acc);
+// acc to out: rows r0 .. r0+rows of the tile, columns c0 .. c0+cols.
+template <int FM, int FN, bool BF>
+__device__ inline void store_tile(const MxParams& P, const f32x16 (&acc)[FM][FN], int wm, int wn,
+                                  int64_t r0, int rows, int c0, int cols) {
+    const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
         const int r = (wn * FN + j) * 32 + (lane & 31);
         if (r >= rows) continue;
-        const int64_t at = (tile.r0 + r) * P.Fo + c0;
+        const int64_t at = (r0 + r) * P.Fo + c0;
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -448,6 +403,70 @@ __global__ __launch_bounds__(64 * WM * WN) void mx_tiles(MxParams P, int64_t row
                 }
             }
     }
+}
+
+// Three buffers, so that loads have two steps' time to arrive: s_waitcnt of n.
+template <int N>
+__device__ inline void wait_loads() {
+    static_assert(N == 0 || N == 6 || N == 8, "the waits below");
+    if constexpr (N == 8) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+    else if constexpr (N == 6) asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
+template <int FM, int FN, int WM, int WN, bool BF>
+__global__ __launch_bounds__(64 * WM * WN, 2) void mx_tiles(MxParams P, int64_t row_tiles,
+                                                            int col_tiles) {
+    constexpr int BM = 32 * FM * WM, BN = 32 * FN * WN, WAVES = WM * WN;  // columns, rows
+    typedef TileLoader<BM, WAVES> LoadW;
+    typedef TileLoader<BN, WAVES> LoadX;
+    __shared__ __attribute__((aligned(16))) TileBuffer<BM> W0, W1, W2;
+    __shared__ __attribute__((aligned(16))) TileBuffer<BN> X0, X1, X2;
+    int64_t rt;
+    int ct;
+    if (!pick_tile(row_tiles, col_tiles, rt, ct)) return;
+    const RowTile tile = row_tile(P, rt, BN);
+    if (tile.t < 0) return;
+    const int KB = P.KB, rows = (int)(tile.r1 - tile.r0), steps = (KB + kStep - 1) / kStep;
+    const int c0 = ct * BM, cols = P.Fo - c0 < BM ? P.Fo - c0 : BM;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, wm = w % WM, wn = w / WM;
+
+    f32x16 acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+
+    const LoadW lw(P.w_codes + (tile.t * P.Fo + c0) * KB * 16, P.w_words + tile.t * steps * P.Fo + c0,
+                   P.Fo, cols, KB);
+    const LoadX lx(P.x_codes + tile.r0 * KB * 16, P.x_words + tile.r0, P.N, rows, KB);
+    // Step k, from buffer k % 3: its loads have arrived when only those of step k+1 are
+    // left; behind the barrier everybody is done with buffer (k+2) % 3.
+    const auto step = [&](TileBuffer<BM>& Wb, TileBuffer<BN>& Xb, TileBuffer<BM>& Wn,
+                          TileBuffer<BN>& Xn, int k) {
+        if (k + 1 < steps) wait_loads<LoadW::LOADS + LoadX::LOADS>();
+        else wait_loads<0>();
+        __builtin_amdgcn_s_barrier();
+        if (k + 2 < steps) {
+            lw.fetch(Wn, k + 2);
+            lx.fetch(Xn, k + 2);
+        }
+        multiply<FM, FN, BM, BN>(Wb, Xb, wm, wn, lane, acc);
+    };
+    lw.fetch(W0, 0);
+    lx.fetch(X0, 0);
+    if (steps > 1) {
+        lw.fetch(W1, 1);
+        lx.fetch(X1, 1);
+    }
+    for (int k = 0; k < steps; k += 3) {
+        step(W0, X0, W2, X2, k);
+        if (k + 1 < steps) step(W1, X1, W0, X0, k + 1);
+        if (k + 2 < steps) step(W2, X2, W1, X1, k + 2);
+    }
+    store_tile<FM, FN, BF>(P, acc, wm, wn, tile.r0, rows, c0, cols);
 }
 
 // ---- few rows ------------------------------------------------------------------------------
@@ -782,8 +801,14 @@ hipError_t launch_mx_product(const MxParams& p, int x_dtype, int out_dtype, hipS
         else hipLaunchKernelGGL(mx_thin<false>, g, b, 0, s, p);
         return hipGetLastError();
     }
-    const int64_t big = row_tiles_bound(p, 256) * ceil_div(p.Fo, 256);
-    return big >= 256 ? tiles<4, 2, 2, 4>(p, bf, s) : tiles<2, 2, 2, 2>(p, bf, s);
+    const int KS = (int)ceil_div(p.KB, kStep);
+    const ScaleTable wt{p.w_scales, p.w_words, p.T * p.Fo, p.Fo};
+    const ScaleTable xt{p.x_scales, p.x_words, p.N, p.N};
+    const int64_t ba = ceil_div(wt.R, kBlock), bb = ceil_div(xt.R, kBlock);
+    hipLaunchKernelGGL(mx_scale_words, dim3((unsigned)(ba + bb), (unsigned)ceil_div(KS, 4)),
+                       dim3(kBlock), 0, s, wt, xt, p.KB, KS, ba);
+    const int64_t big = row_tiles_bound(p, 128) * ceil_div(p.Fo, 256);
+    return big >= 512 ? tiles<4, 2, 2, 2>(p, bf, s) : tiles<2, 2, 2, 2>(p, bf, s);
 }
 
 }  // namespace mp

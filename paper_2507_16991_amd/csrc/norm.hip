@@ -1013,10 +1013,10 @@ NormShape norm_shape(int64_t N, int64_t S, int64_t F, int64_t G, int dtype, int 
         // Many segments: up to 128 KB of one are its unit's.  Few: at most eight rows of
         // a thread, as longer ones have more of the chip in tiles.
         h.lmax = 8 * (int64_t)h.slots;
-        if (S >= 4096) {
-            const int64_t rows = (128 << 10) / (W * (dtype == MP_BF16 ? 2 : 4));
-            h.lmax = rows > h.lmax ? rows : h.lmax;
-        }
+        // A call of 64 KB in all has no long ones: one launch instead of four.
+        const int64_t bytes = W * (dtype == MP_BF16 ? 2 : 4);
+        const int64_t rows = S >= 4096 ? (128 << 10) / bytes : (N * bytes <= (64 << 10) ? N : 0);
+        h.lmax = rows > h.lmax ? rows : h.lmax;
         h.lpg = pow2_below(h.unit / h.tile_groups, 64);
         const int64_t units = short_block(h.unit) / h.unit;
         const int64_t cap = 2048;

@@ -45,7 +45,7 @@ def _layers():
         L.mp_route_backward.argtypes = [p, i32, i64, i64, i64, i64, p, i32, p, p, p, p, p, p, p]
         L.mp_mx_quantize.argtypes = [p, i32, i64, i64, i64, p, p, p, p]
         L.mp_mx_dequantize.argtypes = [p, p, i64, i64, p, i32, p]
-        L.mp_mx_segment_matmul_workspace.argtypes = [i64, i64, psz]
+        L.mp_mx_segment_matmul_workspace.argtypes = [i64, i64, i64, i64, psz]
         L.mp_mx_segment_matmul.argtypes = [p, i32, i64, p, i32, i64, i64, i64, p, p, i64, p, i32, p, sz,
                                            p]
         for name in ("mp_mx_quantize", "mp_mx_dequantize", "mp_mx_segment_matmul_workspace",
@@ -316,9 +316,9 @@ def mp_mx_dequantize(codes, scales, N, K, out, dtype, stream=None):
         _ptr(codes), _ptr(scales), N, K, _ptr(out), dtype, _stream(stream)))
 
 
-def mp_mx_segment_matmul_workspace(N, K) -> int:
+def mp_mx_segment_matmul_workspace(T, N, K, Fo) -> int:
     _layers()
-    return _bytes("mp_mx_segment_matmul_workspace", N, K)
+    return _bytes("mp_mx_segment_matmul_workspace", T, N, K, Fo)
 
 
 def mp_mx_segment_matmul(seg, seg_itype, T, x, x_dtype, N, K, ldx, w_codes, w_scales, Fo, out,
@@ -389,7 +389,7 @@ def mx_segment_matmul(seg, x, codes, scales, *, out_dtype=torch.float32, out=Non
     _on_gpu(seg, x, codes, scales, out)
     dt, it = _dtype_code(x.dtype), _itype_code(seg.dtype)
     xp, ldx = _rows_ptr(x)
-    nb = mp_mx_segment_matmul_workspace(N, K)
+    nb = mp_mx_segment_matmul_workspace(T, N, K, Fo)
     with _on(stream):
         if out is None:
             out = torch.empty(N, Fo, dtype=out_dtype, device=x.device)

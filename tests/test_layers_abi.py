@@ -175,6 +175,7 @@ def test_product_refusals(status, change):
 
 
 def test_product_workspace():
-    assert mp.mp_mx_segment_matmul_workspace(100, 64) >= 100 * 34
-    with pytest.raises(mp.MPError):
-        mp.mp_mx_segment_matmul_workspace(100, 0)
+    assert mp.mp_mx_segment_matmul_workspace(2, 100, 64, 32) >= 100 * 34
+    for bad in ((0, 100, 64, 32), (2, -1, 64, 32), (2, 100, 0, 32), (2, 100, 64, 0), (4097, 1, 1, 1)):
+        with pytest.raises(mp.MPError):
+            mp.mp_mx_segment_matmul_workspace(*bad)
