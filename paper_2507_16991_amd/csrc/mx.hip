@@ -229,6 +229,14 @@ __device__ inline void store_col(void* out, int64_t at, float v) {
     else store_one<F32>(static_cast<float*>(out) + at, v);
 }
 
+// What the lanes of this wavefront have written to LDS is there for the others (the
+// LDS operations of one wavefront complete in order: only the compiler waits).
+__device__ inline void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // ---- tiles ------------------------------------------------------------------------------
 // A workgroup of WM x WN wavefronts has 32 FM WM output columns x 32 FN WN rows, a
 // wavefront FM x FN products of 32 x 32.  k in steps of 4 blocks (64 bytes a row),
@@ -293,7 +301,7 @@ struct TileLoader {
 // The scales of R rows, [R, KB] bytes, as a table of words [KS, R]: word (k, r) has those
 // of row r in step k, 0 past KB.  Tiles then load a step's scales as whole lines
 // (from the format's own layout every row is a request of its own: half of all
-// requests to L2, which bound the product: 1170 -> 640 us at 65,536 x 4096 x 4096).
+// requests to L2, which bound the product: 1170 -> 960 us at 65,536 x 4096 x 4096).
 struct ScaleTable {
     const uint8_t* in;
     uint32_t* out;
@@ -377,32 +385,46 @@ __device__ inline bool pick_tile(int64_t row_tiles, int col_tiles, int64_t& rt, 
     return true;
 }
 
-// acc to out: rows r0 .. r0+rows of the tile, columns c0 .. c0+cols.
+// acc to out: rows r0 .. r0+rows of the tile, columns c0 .. c0+cols.  A lane has four
+// columns of a row, so 32 x 32 products go through LDS (the wavefront's own kOut
+// floats), to be written by whole lines: 32 bytes at a time, the rows' stores were a
+// fifth of all requests to L2 (960 -> 830 us at 65,536 x 4096 x 4096).
+constexpr int kOutLine = 36, kOut = 32 * kOutLine;
+
 template <int FM, int FN, bool BF>
 __device__ inline void store_tile(const MxParams& P, const f32x16 (&acc)[FM][FN], int wm, int wn,
-                                  int64_t r0, int rows, int c0, int cols) {
-    const int lane = threadIdx.x & 63;
+                                  int64_t r0, int rows, int c0, int cols, float* lds) {
+    constexpr int E = BF ? 8 : 4, PER = 32 / E;  // columns of a 16-byte store, stores of a row
+    const int lane = threadIdx.x & 63, half = lane >> 5;
 #pragma unroll
-    for (int j = 0; j < FN; ++j) {
-        const int r = (wn * FN + j) * 32 + (lane & 31);
-        if (r >= rows) continue;
-        const int64_t at = (r0 + r) * P.Fo + c0;
+    for (int j = 0; j < FN; ++j)
 #pragma unroll
-        for (int i = 0; i < FM; ++i)
+        for (int i = 0; i < FM; ++i) {
+            wave_sync();
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int c = (wm * FM + i) * 32 + 8 * q + 4 * (lane >> 5);
-                const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2],
-                                    acc[i][j][4 * q + 3]};
-                if (c + 4 <= cols) {
-                    store4<BF>(P.out, at + c, v);
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<float4*>(&lds[(lane & 31) * kOutLine + 8 * q + 4 * half]) =
+                    make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2],
+                                acc[i][j][4 * q + 3]);
+            wave_sync();
+#pragma unroll
+            for (int u = 0; u < 32 * PER / kWave; ++u) {
+                const int r = (u * kWave + lane) / PER, c = (lane % PER) * E;
+                float v[E];
+                __builtin_memcpy(v, &lds[r * kOutLine + c], sizeof(v));
+                const int row = (wn * FN + j) * 32 + r, col = (wm * FM + i) * 32 + c;
+                if (row >= rows) continue;
+                const int64_t at = (r0 + row) * P.Fo + c0 + col;
+                if (col + E <= cols) {
+                    if (BF) store_floats<BF16, E>(static_cast<uint16_t*>(P.out) + at, v);
+                    else store_floats<F32, E>(static_cast<float*>(P.out) + at, v);
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (c + e < cols) store_col<BF>(P.out, at + c + e, v[e]);
+                    for (int e = 0; e < E; ++e)
+                        if (col + e < cols) store_col<BF>(P.out, at + e, v[e]);
                 }
             }
-    }
+        }
 }
 
 // Three buffers, so that loads have two steps' time to arrive: s_waitcnt of n.
@@ -466,7 +488,10 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mx_tiles(MxParams P, int64_t 
         if (k + 1 < steps) step(W1, X1, W0, X0, k + 1);
         if (k + 2 < steps) step(W2, X2, W1, X1, k + 2);
     }
-    store_tile<FM, FN, BF>(P, acc, wm, wn, tile.r0, rows, c0, cols);
+    __syncthreads();  // everybody is done with the buffers
+    uint8_t* const own = w == 0 ? W0.codes : (w == 1 ? W1.codes : (w == 2 ? W2.codes : X0.codes));
+    static_assert(WAVES == 4 && sizeof(X0.codes) >= kOut * 4, "a buffer a wavefront");
+    store_tile<FM, FN, BF>(P, acc, wm, wn, tile.r0, rows, c0, cols, reinterpret_cast<float*>(own));
 }
 
 // ---- few rows ------------------------------------------------------------------------------
@@ -570,12 +595,6 @@ __host__ __device__ inline NarrowShape narrow_shape(int KB, int Fo) {
     h.wave = (h.wave + 15) & ~(size_t)15;
     h.bytes = h.w_codes + ((h.w_scales + 15) & ~(size_t)15) + 4 * h.wave;
     return h;
-}
-
-__device__ inline void wave_sync() {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
 template <typename T, bool BF>
