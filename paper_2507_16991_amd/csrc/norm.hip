@@ -1025,11 +1025,14 @@ NormShape norm_shape(int64_t N, int64_t S, int64_t F, int64_t G, int dtype, int 
         h.lds = (size_t)units * (2 * h.V * (h.unit + kPad) + 2 * h.tile_groups) * 4;
     }
     h.col_tile = kLong * (int64_t)h.V;
+    if (S == 1 && N > h.lmax) h.unit = h.short_blocks = 0;  // (the host knows its length)
     if (N > h.lmax) {
         // 4096 tiles for the statistics (2048 leave the last round of workgroups half
         // empty, 8192 have twice the partials to join), 8192 for the second read
         // and tiles of 32 KB at the least
-        const int64_t least = ceil_div(32 << 10, F * (dtype == MP_BF16 ? 2 : 4));
+        // (4 KB where the average segment is a long one and the tiles have all the work)
+        const int64_t least =
+            ceil_div(N > S * h.lmax ? 4 << 10 : 32 << 10, F * (dtype == MP_BF16 ? 2 : 4));
         const int64_t r = ceil_div(N, 4096) < least ? least : ceil_div(N, 4096);
         h.tile_rows = r;
         h.apply_rows = ceil_div(N, 8192) < least ? least : ceil_div(N, 8192);
