@@ -337,6 +337,8 @@ __global__ __launch_bounds__(kFinish) void route_finish(RouteParams P, int block
 // sum_j w_j dw_j,
 //   p_e (d_e - sum p d + 2 dz lse / R)  [- p_e S without renorm]
 //   + w_j (dw_j - S)  [w_j dw_j without renorm] where e is the row's j-th choice.
+// Bound by its vector instructions, k V comparisons a lane: 169k rows of 64 bf16
+// experts, k = 8, 28 us (60 MB).
 template <typename T, int V, int L>
 __global__ __launch_bounds__(kBlock) void route_bwd(RouteParams P) {
     constexpr int RW = kWave / L;

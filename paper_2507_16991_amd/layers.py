@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 
 import torch
 
@@ -56,11 +57,14 @@ def _layers():
     return _lib
 
 
+_NO_CONTEXT = contextlib.nullcontext()
+
+
 def _on(stream):
     """What the wrappers allocate and free while they enqueue on `stream` belongs to that stream, so
     that memory is not given away while its kernels run."""
     if stream is None:
-        return contextlib.nullcontext()
+        return _NO_CONTEXT
     if not isinstance(stream, torch.cuda.Stream):
         stream = torch.cuda.ExternalStream(_stream(stream))
     return torch.cuda.stream(stream)
@@ -68,10 +72,15 @@ def _on(stream):
 
 def _on_gpu(*tensors):
     """Kernels run on the current GPU: an operand elsewhere is refused."""
-    dev = torch.cuda.current_device() if torch.cuda.is_available() else None
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != dev):
+        if t is not None and (not t.is_cuda or t.get_device() != torch.cuda.current_device()):
             raise ValueError(f"operands must be on the current GPU, got one on {t.device}")
+
+
+@functools.lru_cache(maxsize=4096)
+def _sized(query, *sizes):
+    """Workspace bytes, a function of the sizes alone."""
+    return query(*sizes)
 
 
 def _table(t):
@@ -140,7 +149,7 @@ def group_norm(ptr, x, groups, *, weight=None, bias=None, eps=1e-5, act="none", 
     _on_gpu(ptr, x, weight, bias, out)
     dt, it = _dtype_code(x.dtype), _itype_code(ptr.dtype)
     xp, ldx = _rows_ptr(x)
-    nb = mp_group_norm_workspace(N, S, F, G, dt, 0)
+    nb = _sized(mp_group_norm_workspace, N, S, F, G, dt, 0)
     dev = x.device
     with _on(stream):
         if out is None:
@@ -168,7 +177,7 @@ def group_norm_backward(ptr, x, dout, groups, mean, rstd, *, weight=None, bias=N
     _on_gpu(ptr, x, dout, mean, rstd, weight, bias)
     dt, it = _dtype_code(x.dtype), _itype_code(ptr.dtype)
     xp, ldx = _rows_ptr(x)
-    nb = mp_group_norm_workspace(N, S, F, G, dt, 1)
+    nb = _sized(mp_group_norm_workspace, N, S, F, G, dt, 1)
     dev = x.device
     with _on(stream):
         dx = torch.empty(N, F, dtype=dx_dtype or x.dtype, device=dev) if want_dx else None
@@ -268,7 +277,7 @@ def route(logits, k, *, mask=None, renorm=True, stream=None):
     dev = logits.device
     dt = _dtype_code(logits.dtype)
     lp, ldl = _rows_ptr(logits)
-    nb = mp_route_workspace(N, E)
+    nb = _sized(mp_route_workspace, N, E)
     with _on(stream):
         idx = torch.empty(N, max(k, 0), dtype=torch.int32, device=dev)
         weight = torch.empty(N, max(k, 0), dtype=torch.float32, device=dev)
@@ -389,7 +398,7 @@ def mx_segment_matmul(seg, x, codes, scales, *, out_dtype=torch.float32, out=Non
     _on_gpu(seg, x, codes, scales, out)
     dt, it = _dtype_code(x.dtype), _itype_code(seg.dtype)
     xp, ldx = _rows_ptr(x)
-    nb = mp_mx_segment_matmul_workspace(T, N, K, Fo)
+    nb = _sized(mp_mx_segment_matmul_workspace, T, N, K, Fo)
     with _on(stream):
         if out is None:
             out = torch.empty(N, Fo, dtype=out_dtype, device=x.device)
