@@ -30,7 +30,7 @@ namespace {
 constexpr int kLong = 256;        // threads of the long path's workgroups
 constexpr int kPad = 16;          // LDS line of a thread's v-th channel: UNIT + 16 floats,
                                   // so that consecutive channels lie on different banks
-constexpr int kJoin = 1024;
+constexpr int kJoin = 512;
 
 // Rows of a batch: loads that a thread has in flight.
 constexpr int kShortRows = 8;
@@ -817,11 +817,11 @@ __global__ __launch_bounds__(kLong, 4) void norm_long_stats(NormParams P) {
 
 // The partials of every long segment joined: mean and rstd, or the means of
 // gamma da and gamma da xhat (P.ca, P.cb).  A workgroup looks for its segments
-// among 1024 at a time; gw (a power of two) threads have neighbouring groups, and
-// kJoin / gw share a group's partials.
+// among 512 at a time; gw (a power of two, at most 64) threads have neighbouring
+// groups, and kJoin / gw share a group's partials.
 template <bool BWD>
 __global__ __launch_bounds__(kJoin) void norm_long_join(NormParams P, int gw, int64_t col_tile) {
-    __shared__ float s_sum[kJoin], s_sum2[kJoin];
+    __shared__ float s_sum[kJoin / kWave][kWave];
     __shared__ int64_t s_seg[kJoin];
     __shared__ int s_n;
     const int t = threadIdx.x, gi = t & (gw - 1), q = t / gw, Q = kJoin / gw;
@@ -863,15 +863,15 @@ __global__ __launch_bounds__(kJoin) void norm_long_join(NormParams P, int gw, in
                         f(v, (float)(int)(rb - ra) * (float)(int)(cz - ca));
                     }
                 };
-                const auto total = [&](float* s_v, float v) {
+                // over the threads of a group: lanes gw apart, then the wavefronts in order
+                const auto total = [&](float v) {
+                    for (int o = kWave / 2; o >= gw; o >>= 1) v += __shfl_xor(v, o);
                     __syncthreads();
-                    s_v[t] = v;
+                    if ((t & 63) < gw) s_sum[t >> 6][gi] = v;
                     __syncthreads();
-                    for (int o = Q / 2; o > 0; o >>= 1) {
-                        if (q < o) s_v[t] += s_v[t + o * gw];
-                        __syncthreads();
-                    }
-                    return s_v[gi];
+                    float r = s_sum[0][gi];
+                    for (int w = 1; w < kJoin / kWave; ++w) r += s_sum[w][gi];
+                    return r;
                 };
                 const float inv = 1.f / ((float)(e - b) * (float)P.cg);
                 if constexpr (BWD) {
@@ -880,8 +880,8 @@ __global__ __launch_bounds__(kJoin) void norm_long_join(NormParams P, int gw, in
                         A += v.x;
                         B += v.y;
                     });
-                    A = total(s_sum, A) * inv;
-                    B = total(s_sum2, B) * inv;
+                    A = total(A) * inv;
+                    B = total(B) * inv;
                     if (q == 0 && ok) {
                         P.ca[s * P.G + g] = A;
                         P.cb[s * P.G + g] = B;
@@ -889,12 +889,12 @@ __global__ __launch_bounds__(kJoin) void norm_long_join(NormParams P, int gw, in
                 } else {
                     float m = 0.f, M2 = 0.f;
                     each([&](float2 v, float n) { m = __builtin_fmaf(v.x, n, m); });
-                    m = total(s_sum, m) / ((float)(e - b) * (float)P.cg);
+                    m = total(m) / ((float)(e - b) * (float)P.cg);
                     each([&](float2 v, float n) {
                         const float u = v.x - m;
                         M2 += __builtin_fmaf(u * u, n, v.y);
                     });
-                    M2 = total(s_sum2, M2) * inv;
+                    M2 = total(M2) * inv;
                     if (q == 0 && ok) {
                         P.mean[s * P.G + g] = m;
                         P.rstd[s * P.G + g] = 1.f / sqrtf(M2 + P.eps);
@@ -1034,13 +1034,15 @@ NormShape norm_shape(int64_t N, int64_t S, int64_t F, int64_t G, int dtype, int 
     h.col_tile = kLong * (int64_t)h.V;
     if (S == 1 && N > h.lmax) h.unit = h.short_blocks = 0;  // (the host knows its length)
     if (N > h.lmax) {
-        // 4096 tiles for the statistics (2048 leave the last round of workgroups half
-        // empty, 8192 have twice the partials to join), 8192 for the second read
-        // and tiles of 32 KB at the least
-        // (4 KB where the average segment is a long one and the tiles have all the work)
+        // Tiles of the statistics: 4096 (2048 leave the forward's last round of workgroups
+        // half empty), 2048 backward (two rounds of what the chip holds; half the partials
+        // and lines to add: 329 -> 315 us for 2.4M x 100); 8192 for the second read; and
+        // of 32 KB at the least (4 KB where the average segment is a long one and the
+        // tiles have all the work).
         const int64_t least =
             ceil_div(N > S * h.lmax ? 4 << 10 : 32 << 10, F * (dtype == MP_BF16 ? 2 : 4));
-        const int64_t r = ceil_div(N, 4096) < least ? least : ceil_div(N, 4096);
+        int64_t r = ceil_div(N, backward ? 2048 : 4096);
+        if (r < least) r = least;
         h.tile_rows = r;
         h.apply_rows = ceil_div(N, 8192) < least ? least : ceil_div(N, 8192);
         h.places = 2 + (r - 1) / (h.lmax + 1);
@@ -1086,7 +1088,7 @@ static void run(const NormParams& p, const NormShape& h, hipStream_t s) {
         if (h.long_tiles)
             hipLaunchKernelGGL((norm_long_stats<T, V, BWD>), g, dim3(kLong), h.long_lds, s, q);
         if (!BWD || q.out) {
-            const int gw = pow2_below(p.G, kJoin);
+            const int gw = pow2_below(p.G, kWave);
             const int64_t jb = p.S < 1024 ? p.S : 1024;
             hipLaunchKernelGGL((norm_long_join<BWD>), dim3((unsigned)jb), dim3(kJoin), 0, s, q, gw,
                                h.col_tile);
