@@ -686,7 +686,7 @@ struct LongTile {
 
 // Partials of rows [row0, row1) of a segment: its place among the tile's, then
 // blockIdx.y + group: {mean, M2} or {sum gamma da, sum gamma da xhat}.  (2.4M x 100
-// bf16: forward 118 us, 4.1 TB/s; backward with gelu 312 us, of which its slope's
+// bf16: forward 118 us, 4.1 TB/s; backward with gelu 301 us, of which its slope's
 // vector instructions are about half.)
 template <typename T, int V, bool BWD>
 __global__ __launch_bounds__(kLong, 4) void norm_long_stats(NormParams P) {
@@ -906,7 +906,7 @@ __global__ __launch_bounds__(kJoin) void norm_long_join(NormParams P, int gw, in
 }
 
 // Bound by memory, gelu also by its arithmetic (2.4M x 100 bf16: forward 180 us, 5.4
-// TB/s; backward with gelu 273 us).  The long segments' rows again, in tiles of apply_rows from the last to the first
+// TB/s; backward with gelu 281 us).  The long segments' rows again, in tiles of apply_rows from the last to the first
 // (the last rows are still in the caches): out, or dx.
 template <typename T, int V, bool BWD>
 __global__ __launch_bounds__(kLong, 4) void norm_long_apply(NormParams P) {
