@@ -192,8 +192,10 @@ def _ptr(t):
 
 def _rows_ptr(t):
     """Address of a 2-D table whose rows may be strided (stride(1) == 1,
-    stride(0) >= shape[1]), and that stride in elements."""
-    if t.dim() != 2 or (t.shape[0] > 1 and t.stride(1) != 1) or t.stride(0) < t.shape[1]:
+    stride(0) >= shape[1]), and that stride in elements.  (The columns of a
+    single row have a stride too; only that of one value or none is of no matter.)"""
+    if (t.dim() != 2 or (t.stride(1) != 1 and (t.shape[0] > 1 or t.numel() > 1))
+            or t.stride(0) < t.shape[1]):
         raise ValueError("feature tables passed to libmp must have unit column stride")
     if t.numel() == 0:
         return _ptr(t.contiguous()), int(t.shape[1])

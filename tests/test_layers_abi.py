@@ -179,3 +179,19 @@ def test_product_workspace():
     for bad in ((0, 100, 64, 32), (2, -1, 64, 32), (2, 100, 0, 32), (2, 100, 64, 0), (4097, 1, 1, 1)):
         with pytest.raises(mp.MPError):
             mp.mp_mx_segment_matmul_workspace(*bad)
+
+
+@pytest.mark.parametrize("rows", [1, 2])
+def test_tables_of_strided_columns_are_refused(rows):
+    """A view of every second column, of one row as of several."""
+    buf = torch.arange(32.0).view(2, 16)
+    with pytest.raises(ValueError):
+        mp._rows_ptr(buf[:rows, ::2])
+
+
+def test_tables_of_strided_rows_are_taken():
+    buf = torch.arange(32.0).view(2, 16)
+    for t, ld in ((buf, 16), (buf[:, 3:8], 16), (buf[:1, 3:8], 5), (buf[:, 2:3], 16), (buf[:0, ::2], 8),
+                  (buf[1:, 5:6], 1), (buf[1:, 4:10:8], 1)):
+        address, stride = mp._rows_ptr(t)
+        assert stride == ld and (not t.numel() or address == t.data_ptr())
