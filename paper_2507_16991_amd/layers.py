@@ -349,13 +349,13 @@ def mx_quantize(x, *, want_values=False, stream=None):
 
     The weights of mx_segment_matmul are mx_quantize(W.transpose(1, 2)) of segment_matmul's W."""
     K = int(x.shape[-1])
-    # (of a table the rows may be strided; other shapes are made contiguous)
-    rows = x if x.dim() == 2 else x.contiguous().view(-1, K)
-    N = int(rows.shape[0])
     _on_gpu(x)
-    xp, ldx = _rows_ptr(rows)
     lead, kb = tuple(x.shape[:-1]), _blocks(K)
     with _on(stream):
+        # (of a table the rows may be strided; other shapes are made contiguous, by and for the stream)
+        rows = x if x.dim() == 2 else x.contiguous().view(-1, K)
+        N = int(rows.shape[0])
+        xp, ldx = _rows_ptr(rows)
         codes = torch.empty(*lead, 16 * kb, dtype=torch.uint8, device=x.device)
         scales = torch.empty(*lead, kb, dtype=torch.uint8, device=x.device)
         values = torch.empty(x.shape, dtype=x.dtype, device=x.device) if want_values else None

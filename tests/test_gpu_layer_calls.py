@@ -31,3 +31,24 @@ def test_one_row_of_strided_columns_is_refused():
     assert torch.equal(buf.view(-1).cpu(), torch.arange(32.0))
     # one value has no stride to be wrong about
     assert mp.dropout(buf[1:, 4:10:8], 0.0, 1).tolist() == [[20.0]]
+
+
+def test_transposed_weights_quantised_on_a_side_stream():
+    """What the stream's own earlier work writes is what is quantised, also through a view that has to
+    be copied; the copy's memory is not given to other work meanwhile."""
+    g = torch.Generator().manual_seed(3)
+    W = torch.randn(4, 512, 384, generator=g).bfloat16().to(DEV)
+    want = mp.mx_quantize(W.transpose(1, 2).contiguous())
+    target = torch.zeros_like(W)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        for _ in range(20):  # earlier work that keeps the stream busy
+            target.add_(1).sub_(1)
+        target.copy_(W)
+    got = mp.mx_quantize(target.transpose(1, 2), stream=s)
+    for _ in range(4):  # of the copy's size, on the current stream
+        torch.full_like(W, 7.0)
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)

@@ -195,3 +195,35 @@ def test_tables_of_strided_rows_are_taken():
                   (buf[1:, 5:6], 1), (buf[1:, 4:10:8], 1)):
         address, stride = mp._rows_ptr(t)
         assert stride == ld and (not t.numel() or address == t.data_ptr())
+
+
+def test_quantize_copies_a_view_on_the_stream_of_the_call(monkeypatch):
+    """A transposed weight is made contiguous within the context of the call's stream, which orders the
+    copy after its producer and before the kernel, and owns its memory."""
+    inside, copies, calls = [], [], []
+
+    class On:
+        def __init__(self, stream):
+            self.stream = stream
+
+        def __enter__(self):
+            inside.append(self.stream)
+
+        def __exit__(self, *_):
+            inside.pop()
+
+    contiguous = torch.Tensor.contiguous
+
+    def copy(t, *a, **k):
+        copies.append(list(inside))
+        return contiguous(t, *a, **k)
+
+    monkeypatch.setattr(layers, "_on", On)
+    monkeypatch.setattr(layers, "_on_gpu", lambda *_: None)
+    monkeypatch.setattr(torch.Tensor, "contiguous", copy)
+    monkeypatch.setattr(layers, "mp_mx_quantize", lambda *a: calls.append((a, list(inside))))
+    w = torch.zeros(2, 64, 40)
+    codes, scales = mp.mx_quantize(w.transpose(1, 2), stream="side")
+    assert codes.shape == (2, 40, 32) and scales.shape == (2, 40, 2)
+    assert copies == [["side"]] and len(calls) == 1 and calls[0][1] == ["side"]
+    assert calls[0][0][2:5] == (80, 64, 64)
