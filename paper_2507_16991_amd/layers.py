@@ -10,6 +10,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import functools
+import math
 
 import torch
 
@@ -347,13 +348,15 @@ def mx_quantize(x, *, want_values=False, stream=None):
     with want_values also the values that they stand for, in x's shape and dtype (training with
     quantised values: use them in the forward pass and hand their gradient to x unchanged).
 
-    The weights of mx_segment_matmul are mx_quantize(W.transpose(1, 2)) of segment_matmul's W."""
+    The weights of mx_segment_matmul are mx_quantize(W.transpose(1, 2)) of segment_matmul's W; one type's
+    may come as a table, W.t().  Views of other strides than a table's are copied."""
     K = int(x.shape[-1])
     _on_gpu(x)
     lead, kb = tuple(x.shape[:-1]), _blocks(K)
     with _on(stream):
-        # (of a table the rows may be strided; other shapes are made contiguous, by and for the stream)
-        rows = x if x.dim() == 2 else x.contiguous().view(-1, K)
+        # (of a table the rows may be strided; other views are made contiguous, by and for the stream)
+        table = x.dim() == 2 and x.stride(1) == 1 and x.stride(0) >= K
+        rows = x if table else x.contiguous().view(math.prod(lead), K)
         N = int(rows.shape[0])
         xp, ldx = _rows_ptr(rows)
         codes = torch.empty(*lead, 16 * kb, dtype=torch.uint8, device=x.device)

@@ -52,3 +52,17 @@ def test_transposed_weights_quantised_on_a_side_stream():
     torch.cuda.synchronize()
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+def test_one_transposed_weight_is_quantised_as_several_are():
+    """Views of a table: transposed, of every second column, repeated, of one row."""
+    w = torch.randn(96, 40, generator=torch.Generator().manual_seed(4)).to(DEV)
+    for view in (w.t(), w[:, ::2], w[:1, ::2], w[:1].expand(5, 40), w[:, :1].t(), w[:, :1]):
+        got = mp.mx_quantize(view, want_values=True)
+        want = mp.mx_quantize(view.clone(memory_format=torch.contiguous_format), want_values=True)
+        _, scales, values = ref.mx_quantize(ref.f64(view))
+        assert np.array_equal(got[1].cpu().numpy(), scales) and np.array_equal(ref.f64(got[2]), values)
+        for a, b in zip(got, want):
+            assert a.shape == b.shape and torch.equal(a, b)
+    empty = mp.mx_quantize(w[:0].t().contiguous().t())
+    assert empty[0].shape == (0, 32) and empty[1].shape == (0, 2)

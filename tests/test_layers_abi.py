@@ -227,3 +227,16 @@ def test_quantize_copies_a_view_on_the_stream_of_the_call(monkeypatch):
     assert codes.shape == (2, 40, 32) and scales.shape == (2, 40, 2)
     assert copies == [["side"]] and len(calls) == 1 and calls[0][1] == ["side"]
     assert calls[0][0][2:5] == (80, 64, 64)
+
+
+def test_quantize_takes_views_of_one_table(monkeypatch):
+    """What reaches the library: a table of strided rows as it is, other views as contiguous copies."""
+    calls = []
+    monkeypatch.setattr(layers, "_on_gpu", lambda *_: None)
+    monkeypatch.setattr(layers, "mp_mx_quantize", lambda *a: calls.append(a))
+    w = torch.zeros(64, 40)
+    for view, n, k, ld in ((w, 64, 40, 40), (w[:, 3:36], 64, 33, 40), (w.t(), 40, 64, 64),
+                           (w[:, ::2], 64, 20, 20), (w[:1, ::2], 1, 20, 20), (w[:1].expand(5, 40), 5, 40, 40)):
+        mp.mx_quantize(view)
+        assert calls[-1][2:5] == (n, k, ld)
+        assert (calls[-1][0] == view.data_ptr()) == (view.stride(1) == 1 and view.stride(0) >= k)
