@@ -1120,7 +1120,8 @@ hipError_t launch_norm(NormParams p, const NormShape& h, int dtype, bool backwar
         else { MP_NORM(F32, 1); }
     }
 #undef MP_NORM
-    if (backward && p.part)
+    // (a call without rows may need no workspace, so p.part does not say: zeros are written)
+    if (backward && dgamma)
         hipLaunchKernelGGL(norm_param_grads, dim3((unsigned)ceil_div(2 * p.F, kGradCols)),
                            dim3(kGradBlock), 0, s, p, h.long_tiles, dgamma, dbeta);
     return hipGetLastError();

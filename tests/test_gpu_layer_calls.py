@@ -66,3 +66,19 @@ def test_one_transposed_weight_is_quantised_as_several_are():
             assert a.shape == b.shape and torch.equal(a, b)
     empty = mp.mx_quantize(w[:0].t().contiguous().t())
     assert empty[0].shape == (0, 32) and empty[1].shape == (0, 2)
+
+
+@pytest.mark.parametrize("f,g", [(8, 2), (4096, 1), (4097, 1), (20000, 1), (20000, 4)])
+def test_parameter_gradients_of_no_rows_are_zero(f, g):
+    """Also of groups too wide for the short path, whose call without rows needs no workspace."""
+    x, ptr = torch.empty(0, f, device=DEV), torch.zeros(4, dtype=torch.int32, device=DEV)
+    _, mean, rstd = mp.group_norm(ptr, x, g)
+    assert bool((mean == 0).all()) and bool((rstd == 0).all())
+    dw, db = torch.full((f,), 7.0, device=DEV), torch.full((f,), 7.0, device=DEV)
+    nb = mp.mp_group_norm_workspace(0, 3, f, g, mp.MP_F32, 1)
+    ws = torch.empty(nb, dtype=torch.uint8, device=DEV) if nb else None
+    mp.mp_group_norm_backward(ptr, mp.MP_I32, x, mp.MP_F32, x, 0, 3, f, f, g, None, None, mean, rstd, 0,
+                              x, mp.MP_F32, dw, db, ws, nb)
+    assert bool((dw == 0).all()) and bool((db == 0).all())
+    _, dw, db = mp.group_norm_backward(ptr, x, x, g, mean, rstd)
+    assert bool((dw == 0).all()) and bool((db == 0).all())
