@@ -315,7 +315,9 @@ __device__ inline void row_stats(const Rows<T>& rows, const Param<V, M>& p, int 
                 }
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    const float u = m[v] - A[v];
+                    // (the first batch is not joined: u is its mean, whose square may be
+                    // infinite, times 0)
+                    const float u = i0 ? m[v] - A[v] : 0.f;
                     A[v] = i0 ? __builtin_fmaf(u, share, A[v]) : m[v];
                     B[v] += __builtin_fmaf(u * u, f0 * share, q[v]);
                 }

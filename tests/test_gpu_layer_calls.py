@@ -82,3 +82,19 @@ def test_parameter_gradients_of_no_rows_are_zero(f, g):
     assert bool((dw == 0).all()) and bool((db == 0).all())
     _, dw, db = mp.group_norm_backward(ptr, x, x, g, mean, rstd)
     assert bool((dw == 0).all()) and bool((db == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,s,f,g", [(7, 1, 8, 2), (100, 1, 16, 4), (100, 3, 15, 5), (300, 20, 3, 1),
+                                     (20000, 1, 16, 4), (20000, 2, 12, 3), (9000, 2, 6000, 1)])
+def test_means_whose_squares_overflow(n, s, f, g, dtype):
+    """Equal rows of a power of two past 2^64, whose sums are exact: no variance."""
+    top = 2.0 ** 66
+    ptr = torch.tensor([n * i // s for i in range(s + 1)], dtype=torch.int32, device=DEV)
+    x = torch.full((n, f), top, device=DEV, dtype=dtype)
+    x[:, f // 2:] *= -1 if g > 1 and f % (2 * g) == 0 and g % 2 == 0 else 1
+    out, mean, rstd = mp.group_norm(ptr, x, g)
+    assert bool((out == 0).all()) and bool((mean.abs() == top).all())
+    assert torch.allclose(rstd, torch.full_like(rstd, 1e-5 ** -0.5), rtol=1e-6, atol=0)
+    dx, dw, db = mp.group_norm_backward(ptr, x, torch.ones_like(x), g, mean, rstd)
+    assert all(bool(t.isfinite().all()) for t in (dx, dw, db))
