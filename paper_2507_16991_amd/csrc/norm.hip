@@ -234,6 +234,14 @@ __device__ inline void unit_sync() {
     }
 }
 
+// 2^-floor(log2 c) and its inverse, for c >= 1: the squares of c values are added up
+// times the first, so that their sum is finite where the variance is.  Products
+// by them are exact, and the bits are those of the plain sum.
+__device__ inline float down_of(float c) {
+    return __uint_as_float((254u << 23) - (__float_as_uint(c) & 0x7F800000u));
+}
+__device__ inline float up_of(float c) { return __uint_as_float(__float_as_uint(c) & 0x7F800000u); }
+
 __device__ inline int rows_of_slot(int64_t n, int slot, int slots) {
     return n > slot ? (int)((n - slot + slots - 1) / slots) : 0;
 }
@@ -495,7 +503,7 @@ __global__ __launch_bounds__(short_block(UNIT), 4) void norm_short(NormParams P)
             continue;
         }
         const int n = (int)n64;
-        const float inv = 1.f / ((float)n * (float)cg);
+        const float count = (float)n * (float)cg, inv = 1.f / count, down = down_of(count);
         rows.mine = ck.on ? rows_of_slot(n, ck.slot, slots) : 0;
         const int64_t r0 = rows.mine ? b + ck.slot : b;
         rows.x = x + r0 * P.ldx;
@@ -566,14 +574,14 @@ __global__ __launch_bounds__(short_block(UNIT), 4) void norm_short(NormParams P)
                     entries(g, [&](int i, int at) {
                         a = __builtin_fmaf(width * (float)rows_of_slot(n, i, slots), ent[at], a);
                     });
-                a = over_threads(a) / ((float)n * (float)cg);
+                a = over_threads(a) / count;
                 if (on)
                     entries(g, [&](int i, int at) {
                         const int r = rows_of_slot(n, i, slots);
                         const float q = ent[at] - a;
-                        e += r > 0 ? __builtin_fmaf(q * q, width * (float)r, ent2[at]) : 0.f;
+                        e += r > 0 ? __builtin_fmaf(q * q, width * down * (float)r, ent2[at] * down) : 0.f;
                     });
-                e = over_threads(e) * inv;
+                e = over_threads(e) * (inv * up_of(count));
                 if (on && l == 0) {
                     const float rs = 1.f / sqrtf(e + P.eps);
                     s_a[g] = a;
@@ -687,7 +695,8 @@ struct LongTile {
 };
 
 // Partials of rows [row0, row1) of a segment: its place among the tile's, then
-// blockIdx.y + group: {mean, M2} or {sum gamma da, sum gamma da xhat}.  (2.4M x 100
+// blockIdx.y + group: {mean, M2 times down_of(its values)} or {sum gamma da, sum gamma
+// da xhat}.  (2.4M x 100
 // bf16: forward 118 us, 4.1 TB/s; backward with gelu 301 us, of which its slope's
 // vector instructions are about half.)
 template <typename T, int V, bool BWD>
@@ -773,14 +782,14 @@ __global__ __launch_bounds__(kLong, 4) void norm_long_stats(NormParams P) {
                 if (g < lt.gn) {
                     int gb, ge;
                     range(g, gb, ge);
-                    const float m = s_a[g];
+                    const float m = s_a[g], down = down_of((float)n * (float)(ge - gb));
                     const int w = ge - gb, ds = P.lpg / w, dc = P.lpg - ds * w;
                     int slot = l / w, c = l - slot * w;
                     while (slot < lt.slots) {
                         const int p = place<V, UNIT>(slot, gb + c, lt.cpr, lt.W);
                         const int rows = rows_of_slot(n, slot, lt.slots);
                         const float u = ent[p] - m;
-                        sum += rows > 0 ? __builtin_fmaf(u * u, (float)rows, ent2[p]) : 0.f;
+                        sum += rows > 0 ? __builtin_fmaf(u * u, down * (float)rows, ent2[p] * down) : 0.f;
                         slot += ds;
                         c += dc;
                         if (c >= w) {
@@ -875,7 +884,7 @@ __global__ __launch_bounds__(kJoin) void norm_long_join(NormParams P, int gw, in
                     for (int w = 1; w < kJoin / kWave; ++w) r += s_sum[w][gi];
                     return r;
                 };
-                const float inv = 1.f / ((float)(e - b) * (float)P.cg);
+                const float count = (float)(e - b) * (float)P.cg, inv = 1.f / count;
                 if constexpr (BWD) {
                     float A = 0.f, B = 0.f;
                     each([&](float2 v, float) {
@@ -891,12 +900,13 @@ __global__ __launch_bounds__(kJoin) void norm_long_join(NormParams P, int gw, in
                 } else {
                     float m = 0.f, M2 = 0.f;
                     each([&](float2 v, float n) { m = __builtin_fmaf(v.x, n, m); });
-                    m = total(m) / ((float)(e - b) * (float)P.cg);
+                    m = total(m) / count;
+                    const float down = down_of(count);
                     each([&](float2 v, float n) {
                         const float u = v.x - m;
-                        M2 += __builtin_fmaf(u * u, n, v.y);
+                        M2 += __builtin_fmaf(u * u, n * down, v.y * (up_of(n) * down));
                     });
-                    M2 = total(M2) * inv;
+                    M2 = total(M2) * (inv * up_of(count));
                     if (q == 0 && ok) {
                         P.mean[s * P.G + g] = m;
                         P.rstd[s * P.G + g] = 1.f / sqrtf(M2 + P.eps);

@@ -98,3 +98,21 @@ def test_means_whose_squares_overflow(n, s, f, g, dtype):
     assert torch.allclose(rstd, torch.full_like(rstd, 1e-5 ** -0.5), rtol=1e-6, atol=0)
     dx, dw, db = mp.group_norm_backward(ptr, x, torch.ones_like(x), g, mean, rstd)
     assert all(bool(t.isfinite().all()) for t in (dx, dw, db))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,s,f,g", [(7, 1, 8, 2), (100, 1, 16, 4), (100, 3, 15, 5), (300, 20, 3, 1),
+                                     (20000, 1, 16, 4), (20000, 2, 12, 3), (9000, 2, 6000, 1)])
+def test_finite_variances_whose_sums_overflow(n, s, f, g, dtype):
+    """About means past 2^64, within the rounding of x - mean."""
+    top = 2.0 ** 66
+    ptr = torch.tensor([n * i // s for i in range(s + 1)], dtype=torch.int32, device=DEV)
+    # a spread of 1/64 of the mean: bf16 holds it, and its square is below 2^128 (2^120)
+    x = (top * (1 + torch.randn(n, f, generator=torch.Generator().manual_seed(n)) / 64)).to(dtype).to(DEV)
+    out, mean, rstd = mp.group_norm(ptr, x, g, out_dtype=torch.float32)
+    r = ref.group_norm(ptr.cpu().numpy(), ref.f64(x), g, np.ones(f), np.zeros(f), 1e-5, "none")
+    # C u (1 + max|x| rstd) of xhat's size, C = 64 (a run of that many terms): max|x| rstd is below 128
+    t = 64 * 2.0 ** -24 * (1 + 128)
+    assert np.abs(ref.f64(x)).max() * r["rstd"].max() < 128 or n * f // (s * g) < 64
+    if n * f // (s * g) >= 64:
+        assert np.all(np.abs(ref.f64(out) - r["out"]) <= t * (1 + np.abs(r["out"])))
