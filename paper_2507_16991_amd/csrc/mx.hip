@@ -794,15 +794,15 @@ static hipError_t tiles(const MxParams& p, int bf, hipStream_t s) {
 hipError_t launch_mx_product(const MxParams& p, int x_dtype, int out_dtype, hipStream_t s) {
     if (p.N <= 0) return hipSuccess;
     const int bf = out_dtype == MP_BF16;
-    const int64_t thin = row_tiles_bound(p, kThinRows);
-    const bool few = p.N <= 16 * p.T + 16 && thin <= 65535;
+    const bool few = p.N <= 16 * p.T + 16;
     // At most 256 columns and 96 KB of LDS (weights and four wavefronts' rows): one read
     // of x, and no codes in memory.
     const NarrowShape h = narrow_shape(p.KB, p.Fo);
     if (!few && p.Fo <= 256 && h.bytes <= (96 << 10)) {
         const int64_t rt = row_tiles_bound(p, kNarrowTile);
-        const int per_cu = h.bytes <= (40 << 10) ? 4 : (h.bytes <= (53 << 10) ? 3 : (h.bytes <= (80 << 10) ? 2 : 1));
-        const int64_t most = 256 * per_cu;
+        // as many workgroups as the CUs hold at once, with 160 KB of LDS each: never more
+        // than two (a workgroup has 66 KB for its wavefronts' results alone)
+        const int64_t most = 256 * (h.bytes <= (80 << 10) ? 2 : 1);
         const dim3 g((unsigned)(rt < most ? rt : most)), b(kBlock);
         if (x_dtype == MP_BF16) {
             if (bf) hipLaunchKernelGGL((mx_narrow<BF16, true>), g, b, h.bytes, s, p, rt);
@@ -818,7 +818,9 @@ hipError_t launch_mx_product(const MxParams& p, int x_dtype, int out_dtype, hipS
     if (e != hipSuccess) return e;
     // few rows a segment: the weights are what is read
     if (few) {
-        const dim3 g((unsigned)ceil_div(p.Fo, kThinCols), (unsigned)thin), b(kBlock);
+        // (at most 8193 row tiles, as T <= 4096)
+        const dim3 g((unsigned)ceil_div(p.Fo, kThinCols), (unsigned)row_tiles_bound(p, kThinRows)),
+            b(kBlock);
         if (bf) hipLaunchKernelGGL(mx_thin<true>, g, b, 0, s, p);
         else hipLaunchKernelGGL(mx_thin<false>, g, b, 0, s, p);
         return hipGetLastError();

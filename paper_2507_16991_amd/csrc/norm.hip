@@ -1063,7 +1063,7 @@ NormShape norm_shape(int64_t N, int64_t S, int64_t F, int64_t G, int dtype, int 
         h.stat_line = h.col_tiles + G;
         // threads of a group: as many as a full column tile's groups leave
         const int64_t gn = h.col_tiles > 1 ? ceil_div(h.col_tile, cg) + 1 : G;
-        h.long_lpg = pow2_below(kLong / (gn < 1 ? 1 : gn), 64);
+        h.long_lpg = pow2_below(kLong / gn, 64);
         h.long_lds = (size_t)(gn + 1) * 4;
     }
     return h;
