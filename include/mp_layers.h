@@ -196,8 +196,9 @@ int mp_mx_segment_matmul_workspace(int64_t T, int64_t N, int64_t K, int64_t Fo, 
  *   x       [N, K] of x_dtype, row stride ldx.
  *   w_codes [T, Fo, KB * 16], w_scales [T, Fo, KB].
  *   out     [N, Fo] contiguous of out_dtype, from fp32 sums.
- * Sizes: 0 <= N <= INT32_MAX, 1 <= T <= 4096, 1 <= K, Fo <= 65536; w_codes and
- * ws 16-byte aligned. */
+ * Sizes: 0 <= N <= INT32_MAX, 1 <= T <= 4096, 1 <= K, Fo <= 65536, and where K > 128 or
+ * Fo > 256 also (N / 128 + min(T, N)) * ceil(Fo / 256) <= 2^24 - 8 (the tiles of a
+ * launch); w_codes and ws 16-byte aligned. */
 int mp_mx_segment_matmul(const void* seg, int seg_itype, int64_t T, const void* x, int x_dtype,
                          int64_t N, int64_t K, int64_t ldx, const uint8_t* w_codes,
                          const uint8_t* w_scales, int64_t Fo, void* out, int out_dtype, void* ws,

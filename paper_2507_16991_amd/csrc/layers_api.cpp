@@ -63,7 +63,7 @@ int norm_call(const void* ptr, int ptr_itype, int64_t ldx, int64_t F, int act, i
 int mx_dims(int64_t T, int64_t N, int64_t K, int64_t Fo) {
     if (N < 0 || N > INT32_MAX || T < 1 || T > 4096 || K < 1 || K > kMaxF || Fo < 1 || Fo > kMaxF)
         return MP_ERR_SIZE;
-    return MP_OK;
+    return mx_product_fits(T, N, K, Fo) ? MP_OK : MP_ERR_SIZE;
 }
 
 // Workspace of the 4-bit product: the rows' codes and scales, and both operands'

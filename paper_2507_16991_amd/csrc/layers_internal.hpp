@@ -196,6 +196,8 @@ hipError_t launch_mx_quantize(const void* x, int dtype, int64_t N, int64_t K, in
                               uint8_t* codes, uint8_t* scales, void* values, hipStream_t s);
 hipError_t launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t N, int64_t K,
                                 void* out, int dtype, hipStream_t s);
+// Whether a product of these sizes has no more tiles than a launch can hold.
+bool mx_product_fits(int64_t T, int64_t N, int64_t K, int64_t Fo);
 hipError_t launch_mx_product(const MxParams& p, int x_dtype, int out_dtype, hipStream_t s);
 
 }  // namespace mp

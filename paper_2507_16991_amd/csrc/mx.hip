@@ -776,29 +776,45 @@ hipError_t launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int
 
 // Tiles of BM rows that segments of N rows can have at most: every segment that
 // has rows may end in a part of one.
+static int64_t row_tiles_bound(int64_t T, int64_t N, int64_t BM) {
+    return N / BM + (T < N ? T : N);
+}
 static int64_t row_tiles_bound(const MxParams& p, int64_t BM) {
-    return p.N / BM + (p.T < p.N ? p.T : p.N);
+    return row_tiles_bound(p.T, p.N, BM);
 }
 
 template <int FM, int FN, int WM, int WN>
 static hipError_t tiles(const MxParams& p, int bf, hipStream_t s) {
     const int64_t rt = row_tiles_bound(p, 32 * FN * WN), ct = ceil_div(p.Fo, 32 * FM * WM);
-    const int64_t grid = ceil_div(rt * ct, 8) * 8;
-    if (grid > INT32_MAX) return hipErrorInvalidValue;
-    const dim3 g((unsigned)grid), b(64 * WM * WN);
+    const dim3 g((unsigned)(ceil_div(rt * ct, 8) * 8)), b(64 * WM * WN);
     if (bf) hipLaunchKernelGGL((mx_tiles<FM, FN, WM, WN, true>), g, b, 0, s, p, rt, (int)ct);
     else hipLaunchKernelGGL((mx_tiles<FM, FN, WM, WN, false>), g, b, 0, s, p, rt, (int)ct);
     return hipGetLastError();
+}
+
+// (the smaller tiles are taken for fewer than 512 of these)
+static int64_t wide_tiles(int64_t T, int64_t N, int64_t Fo) {
+    return row_tiles_bound(T, N, 128) * ceil_div(Fo, 256);
+}
+
+// At most 256 columns and 96 KB of LDS (weights and four wavefronts' rows): one read
+// of x, and no codes in memory.
+static bool is_narrow(const NarrowShape& h, int64_t Fo) {
+    return Fo <= 256 && h.bytes <= (96 << 10);
+}
+
+// A launch has fewer than 2^32 threads, and a tile 256 of them.
+bool mx_product_fits(int64_t T, int64_t N, int64_t K, int64_t Fo) {
+    return is_narrow(narrow_shape((int)ceil_div(K, kMxBlock), (int)Fo), Fo) ||
+           wide_tiles(T, N, Fo) <= (1 << 24) - 8;
 }
 
 hipError_t launch_mx_product(const MxParams& p, int x_dtype, int out_dtype, hipStream_t s) {
     if (p.N <= 0) return hipSuccess;
     const int bf = out_dtype == MP_BF16;
     const bool few = p.N <= 16 * p.T + 16;
-    // At most 256 columns and 96 KB of LDS (weights and four wavefronts' rows): one read
-    // of x, and no codes in memory.
     const NarrowShape h = narrow_shape(p.KB, p.Fo);
-    if (!few && p.Fo <= 256 && h.bytes <= (96 << 10)) {
+    if (!few && is_narrow(h, p.Fo)) {
         const int64_t rt = row_tiles_bound(p, kNarrowTile);
         // as many workgroups as the CUs hold at once, with 160 KB of LDS each: never more
         // than two (a workgroup has 66 KB for its wavefronts' results alone)
@@ -831,8 +847,7 @@ hipError_t launch_mx_product(const MxParams& p, int x_dtype, int out_dtype, hipS
     const int64_t ba = ceil_div(wt.R, kBlock), bb = ceil_div(xt.R, kBlock);
     hipLaunchKernelGGL(mx_scale_words, dim3((unsigned)(ba + bb), (unsigned)ceil_div(KS, 4)),
                        dim3(kBlock), 0, s, wt, xt, p.KB, KS, ba);
-    const int64_t big = row_tiles_bound(p, 128) * ceil_div(p.Fo, 256);
-    return big >= 512 ? tiles<4, 2, 2, 2>(p, bf, s) : tiles<2, 2, 2, 2>(p, bf, s);
+    return wide_tiles(p.T, p.N, p.Fo) >= 512 ? tiles<4, 2, 2, 2>(p, bf, s) : tiles<2, 2, 2, 2>(p, bf, s);
 }
 
 }  // namespace mp

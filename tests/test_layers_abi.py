@@ -240,3 +240,19 @@ def test_quantize_takes_views_of_one_table(monkeypatch):
         mp.mx_quantize(view)
         assert calls[-1][2:5] == (n, k, ld)
         assert (calls[-1][0] == view.data_ptr()) == (view.stride(1) == 1 and view.stride(0) >= k)
+
+
+def test_products_of_more_tiles_than_a_launch_holds_are_refused():
+    """By the host, as a size: (N / 128 + min(T, N)) * ceil(Fo / 256) tiles, 2^24 - 8 at most; products
+    of few columns and little LDS have no such tiles."""
+    query = mp.mp_mx_segment_matmul_workspace
+    assert query(1, 2 ** 23 - 256, 32, 65536) > 0   # (2^16 - 1) * 256
+    for t, n, k, fo in ((1, 2 ** 23 - 128, 32, 65536), (2, 2 ** 31 - 1, 32, 65536),
+                        (1, 2 ** 31 - 1, 65536, 16), (1, 2 ** 31 - 1, 32, 257)):
+        with pytest.raises(mp.MPError) as e:
+            query(t, n, k, fo)
+        assert e.value.status == -2
+        refused("mp_mx_segment_matmul", PRODUCT, -2, T=t, N=n, K=k, ldx=k, Fo=fo,
+                ws_bytes=2 ** 62)
+    for t, n, k, fo in ((1, 2 ** 31 - 1, 32, 1), (4096, 2 ** 31 - 1, 64, 256), (3, 2 ** 31 - 1, 128, 128)):
+        assert query(t, n, k, fo) > 0
