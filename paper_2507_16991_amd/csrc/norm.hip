@@ -1077,7 +1077,7 @@ static void short_path(const NormParams& q, const NormShape& h, dim3 g, hipStrea
         hipLaunchKernelGGL((norm_short<T, V, 128, BWD, WHOLE>), g, dim3(128), h.lds, s, q);
     else if (h.unit == 256)
         hipLaunchKernelGGL((norm_short<T, V, 256, BWD, WHOLE>), g, dim3(256), h.lds, s, q);
-    else
+    else if constexpr (V > 1)  // (rows of one chunk a channel are narrow)
         hipLaunchKernelGGL((norm_short<T, V, 1024, BWD, WHOLE>), g, dim3(1024), h.lds, s, q);
 }
 
@@ -1091,8 +1091,10 @@ static void run(const NormParams& p, const NormShape& h, hipStream_t s) {
         q.lpg = h.lpg;
         const dim3 g((unsigned)h.short_blocks, (unsigned)h.tiles);
         // (of a width that is a multiple of V no chunk is moved back)
-        if (V > 1 && p.cg % V == 0) short_path<T, V, BWD, true>(q, h, g, s);
-        else short_path<T, V, BWD, false>(q, h, g, s);
+        const bool whole = V > 1 && p.cg % V == 0;
+        if constexpr (V > 1)
+            if (whole) short_path<T, V, BWD, true>(q, h, g, s);
+        if (!whole) short_path<T, V, BWD, false>(q, h, g, s);
     }
     if (!h.unit || h.long_tiles) {
         q.lpg = h.long_lpg;
