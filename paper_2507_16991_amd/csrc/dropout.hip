@@ -89,7 +89,7 @@ __device__ inline void drop_chunk(const typename T::raw* x, const typename T::ra
 }
 
 // Contiguous tables without ids: element numbers are places.  Bound by memory: 2.4M x
-// 100 bf16 with a residual 248 us (5.9 TB/s), without 149 us (6.6 TB/s).
+// 100 bf16 with a residual 252 us (5.8 TB/s), without 162 us (6.0 TB/s).
 template <typename T, bool RES>
 __global__ __launch_bounds__(kBlock) void dropout_flat(DropoutParams P) {
     typedef typename T::raw raw;
@@ -106,7 +106,9 @@ __global__ __launch_bounds__(kBlock) void dropout_flat(DropoutParams P) {
 
 // Any strides and ids: a workgroup takes whole rows, a thread one Philox block
 // of a row (of F elements a row has at most (F + 14) / 8, as it may begin
-// inside one).  ROWS: one word for the row, and the chunks begin with it.
+// inside one).  ROWS: one word for the row, and the chunks begin with it.  (2.4M rows by
+// ids: 128 bf16 247 us, 5.1 TB/s; 100 bf16, whose chunks are cut at both ends of a row,
+// 365 us, 2.7 TB/s.  Whole rows of 100 bf16 270 us.)
 template <typename T, bool RES, bool ROWS>
 __global__ __launch_bounds__(kBlock) void dropout_rows(DropoutParams P, uint32_t cpr,
                                                        uint32_t rows_per_block) {
@@ -142,8 +144,8 @@ __global__ __launch_bounds__(kBlock) void dropout_rows(DropoutParams P, uint32_t
 
 // One element a row, as edge weights have, without a stride: every row has a
 // Philox block of its own, so the generator's products bound it; a thread
-// takes four rows with 16-byte loads (124M fp32 weights 288 us, 5.1 TB/s; one row a
-// thread by dropout_rows 1061 us).
+// takes four rows with 16-byte loads (124M fp32 weights, calls in a row: 290 us, 5.1
+// TB/s; one row a thread by dropout_rows 1061 us).
 template <typename T, bool RES>
 __global__ __launch_bounds__(kBlock) void dropout_scalars(DropoutParams P) {
     typedef typename T::raw raw;

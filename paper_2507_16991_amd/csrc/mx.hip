@@ -118,7 +118,7 @@ __device__ inline void store8(typename T::raw* p, int k0, int K, const float (&v
 }
 
 // A workgroup takes rows_per_block rows, a thread eight values of one.  Bound by
-// memory: 32,768 x 4096 bf16 with values 107 us (5.7 TB/s).
+// memory: 32,768 x 4096 bf16 with values 112 us (5.4 TB/s).
 template <typename T>
 __global__ __launch_bounds__(kBlock) void mx_quantize(const typename T::raw* x, int64_t N, int K,
                                                       int64_t ldx, int rows_per_block,
@@ -302,7 +302,7 @@ struct TileLoader {
 // The scales of R rows, [R, KB] bytes, as a table of words [KS, R]: word (k, r) has those
 // of row r in step k, 0 past KB.  Tiles then load a step's scales as whole lines
 // (from the format's own layout every row is a request of its own: half of all
-// requests to L2, which bound the product: 1170 -> 960 us at 65,536 x 4096 x 4096).
+// requests to L2: with it 1170 us at 65,536 x 4096 x 4096, without 960 at that time).
 struct ScaleTable {
     const uint8_t* in;
     uint32_t* out;
@@ -389,7 +389,7 @@ __device__ inline bool pick_tile(int64_t row_tiles, int col_tiles, int64_t& rt, 
 // acc to out: rows r0 .. r0+rows of the tile, columns c0 .. c0+cols.  A lane has four
 // columns of a row, so 32 x 32 products go through LDS (the wavefront's own kOut
 // floats), to be written by whole lines: 32 bytes at a time, the rows' stores were a
-// fifth of all requests to L2 (960 -> 830 us at 65,536 x 4096 x 4096).
+// fifth of all requests to L2 (130 of 960 us at 65,536 x 4096 x 4096; now 850 to 920).
 constexpr int kOutLine = 36, kOut = 32 * kOutLine;
 
 template <int FM, int FN, bool BF>
@@ -499,7 +499,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mx_tiles(MxParams P, int64_t 
 // A workgroup has 16 output columns and up to 16 rows of a segment; its four
 // wavefronts take steps of four blocks (k = 128) in turn, weights straight from
 // memory, kThinDeep loads in flight, and their sums are added in LDS.  (16 rows of 8
-// experts of 2048 x 4096, 36 MB of weights: 10.6 us.)
+// experts of 2048 x 4096, 36 MB of weights: 10.9 us.)
 constexpr int kThinRows = 16, kThinCols = 16, kThinDeep = 4;
 
 template <bool BF>
@@ -562,7 +562,7 @@ __global__ __launch_bounds__(kBlock) void mx_thin(MxParams P) {
 // (lanes along the row, so that loads are whole lines), multiplies, and hands the
 // results back through the same LDS, to write rows of out in whole pieces.
 // No wavefront waits for another but when the segment changes.  (2.6M bf16 rows, 128
-// -> 128: 314 us, 4.3 TB/s; quantised in a pass of its own 606 us.)
+// -> 128, calls in a row: 314 us, 4.3 TB/s; quantised in a pass of its own 606 us.)
 constexpr int kNarrowRows = 32, kNarrowTile = 32 * 4;  // rows of a wavefront, of a workgroup
 constexpr int kNarrowCols = 4;                         // column tiles of a pass (accumulators)
 // floats to a row of results in LDS: two rows of a store lie on other banks
@@ -792,13 +792,16 @@ static hipError_t tiles(const MxParams& p, int bf, hipStream_t s) {
     return hipGetLastError();
 }
 
-// (the smaller tiles are taken for fewer than 512 of these)
+// The smaller tiles are taken for fewer than 512 of these, two to a CU.  (4096 -> 4096, wide
+// and smaller: 256 tiles 41 and 38 us, 384 tiles 50 and 50, 512 tiles 58 and 65.)
 static int64_t wide_tiles(int64_t T, int64_t N, int64_t Fo) {
     return row_tiles_bound(T, N, 128) * ceil_div(Fo, 256);
 }
 
 // At most 256 columns and 96 KB of LDS (weights and four wavefronts' rows): one read
-// of x, and no codes in memory.
+// of x, and no codes in memory.  (1M bf16 rows against tiles: 128 -> 128 127 and 211
+// us.  Past 80 KB a CU has one workgroup: 128 -> 256 274 and 224 us, but 16 and 22 for
+// 20,000 rows, where one launch instead of three counts.)
 static bool is_narrow(const NarrowShape& h, int64_t Fo) {
     return Fo <= 256 && h.bytes <= (96 << 10);
 }
@@ -812,6 +815,9 @@ bool mx_product_fits(int64_t T, int64_t N, int64_t K, int64_t Fo) {
 hipError_t launch_mx_product(const MxParams& p, int x_dtype, int out_dtype, hipStream_t s) {
     if (p.N <= 0) return hipSuccess;
     const int bf = out_dtype == MP_BF16;
+    // Where segments have 16 rows on average each is a thin tile.  (8 types, 4096 -> 4096,
+    // thin against tiles: 8 rows each 31 and 32 us, 16 rows 36 and 35, 18 rows 55 and 36.
+    // One type: 32 rows 18 and 25, and thin would lead up to 64, 21 and 26.)
     const bool few = p.N <= 16 * p.T + 16;
     const NarrowShape h = narrow_shape(p.KB, p.Fo);
     if (!few && is_narrow(h, p.Fo)) {

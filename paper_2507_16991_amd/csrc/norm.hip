@@ -6,8 +6,8 @@
 // out by length:
 //   * short segments: a unit (a wavefront, or a workgroup) takes a whole
 //     segment, statistics and normalisation in one launch; the second read of
-//     its rows comes from the caches.  (Rows kept in registers in between were
-//     slower: 128 registers and spills instead of 64, so half the wavefronts.)
+//     its rows comes from the caches.  (Rows kept in registers in between were no
+//     faster; the kernels take 97 to 128 registers without that.)
 //   * long segments (more than lmax rows): tiles of `tile_rows` rows, whatever
 //     the segments' lengths, leave partial statistics (norm_long_stats), a
 //     workgroup joins those of a segment (norm_long_join), and the tiles
@@ -32,14 +32,16 @@ constexpr int kPad = 16;          // LDS line of a thread's v-th channel: UNIT +
                                   // so that consecutive channels lie on different banks
 constexpr int kJoin = 512;
 
-// Rows of a batch: loads that a thread has in flight.
+// Rows of a batch: loads that a thread has in flight.  (Eight spill 8 to 37 registers
+// in the short backward of fp32, and 6 in that of bf16 where a chunk has several
+// groups; fewer rows there have not been measured.)
 constexpr int kShortRows = 8;
 constexpr int long_rows(bool bf16, bool backward) { return bf16 || !backward ? 8 : 4; }
 
 // ---- activations ----------------------------------------------------------------------
 // The standard normal distribution and density at z.  With a = |z| and t =
 // 1 / (1 + 0.29 a), Q(a) = 1 - Phi(a) = exp(-a^2 / 2) t P(t): a least-maximum
-// fit of degree 6 made for this file (error 8e-8 against Q, 6e-5 of Q out to
+// fit of degree 6 made for this file (error 8.4e-8 against Q, 8e-5 of Q out to
 // a = 14).  The exponential serves the density too.
 __device__ inline void normal(float z, float& Phi, float& e) {
     const float a = fabsf(z);
@@ -309,7 +311,7 @@ __device__ inline void row_stats(const Rows<T>& rows, const Param<V, M>& p, int 
                     for (int v = 0; v < V; ++v) m[v] += i < nb ? f[v] : 0.f;
                 }
 #pragma unroll
-                for (int v = 0; v < V; ++v)  // (quotients: equal rows give their own mean)
+                for (int v = 0; v < V; ++v)  // (a quotient: the mean is exact where the sum is)
                     m[v] = nb == R ? m[v] * (1.f / R) : m[v] / fn;
 #pragma unroll
                 for (int i = 0; i < R; ++i) {
@@ -410,7 +412,7 @@ constexpr int short_block(int unit) { return unit == 64 ? 256 : unit; }
 // WHOLE: a chunk lies within one group (F / G a multiple of V), so a thread has one
 // mean and leaves one entry in LDS instead of V.
 //
-// 190k rows of 128 bf16 channels in 8192 segments, relu: forward 48 us, backward 58
+// 190k rows of 128 bf16 channels in 8192 segments, relu: forward 48 us, backward 59
 // us, bound by the instructions and latencies of segments of 23 rows (2.0 and 2.5
 // TB/s).  Wavefronts as units, with twice the rows a thread: 51 and 88 us.
 template <typename T, int V, int UNIT, bool BWD, bool WHOLE>
@@ -697,7 +699,7 @@ struct LongTile {
 // Partials of rows [row0, row1) of a segment: its place among the tile's, then
 // blockIdx.y + group: {mean, M2 times down_of(its values)} or {sum gamma da, sum gamma
 // da xhat}.  (2.4M x 100
-// bf16: forward 118 us, 4.1 TB/s; backward with gelu 301 us, of which its slope's
+// bf16: forward 125 us, 3.9 TB/s; backward with gelu 318 us, of which its slope's
 // vector instructions are about half.)
 template <typename T, int V, bool BWD>
 __global__ __launch_bounds__(kLong, 4) void norm_long_stats(NormParams P) {
@@ -917,9 +919,9 @@ __global__ __launch_bounds__(kJoin) void norm_long_join(NormParams P, int gw, in
     }
 }
 
-// Bound by memory, gelu also by its arithmetic (2.4M x 100 bf16: forward 180 us, 5.4
-// TB/s; backward with gelu 281 us).  The long segments' rows again, in tiles of apply_rows from the last to the first
-// (the last rows are still in the caches): out, or dx.
+// The long segments' rows again, in tiles of apply_rows from the last to the first (the
+// last rows are still in the caches): out, or dx.  Bound by memory, gelu also by its
+// arithmetic (2.4M x 100 bf16: forward 192 us, 5.1 TB/s; backward with gelu 291 us).
 template <typename T, int V, bool BWD>
 __global__ __launch_bounds__(kLong, 4) void norm_long_apply(NormParams P) {
     typedef typename T::raw raw;
@@ -1030,9 +1032,16 @@ NormShape norm_shape(int64_t N, int64_t S, int64_t F, int64_t G, int dtype, int 
         if (!h.unit) h.unit = h.cpr <= 256 ? 256 : 1024;
         h.slots = h.unit / h.cpr;
         // Many segments: up to 128 KB of one are its unit's.  Few: at most eight rows of
-        // a thread, as longer ones have more of the chip in tiles.
+        // a thread, as longer ones have more of the chip in tiles.  (1M x 64 bf16, forward,
+        // by a unit against by tiles: 4,096 segments 74 and 126 us if even, 124 and 166 if
+        // ragged; 16,384 ragged 109 and 227.  Below, units have even segments faster, 73
+        // and 102 for 1,024, but ragged ones slower: 127 and 126, backward 243 and 202;
+        // 64 of them 124 and 99.  128 channels, 4,096 ragged: 216 and 238, backward 394
+        // and 365.)
         h.lmax = 8 * (int64_t)h.slots;
-        // A call of 64 KB in all has no long ones: one launch instead of four.
+        // A call of 64 KB in all has no long ones: one launch instead of four.  (64 KB of 64
+        // bf16 channels: 15 us against 21 for one segment and 25 for two.  At 128 KB it is
+        // 18 and 21, but backward 28 and 26; at 256 KB 30 and 21.)
         const int64_t bytes = W * (dtype == MP_BF16 ? 2 : 4);
         const int64_t rows = S >= 4096 ? (128 << 10) / bytes : (N * bytes <= (64 << 10) ? N : 0);
         h.lmax = rows > h.lmax ? rows : h.lmax;
