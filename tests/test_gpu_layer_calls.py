@@ -116,3 +116,45 @@ def test_finite_variances_whose_sums_overflow(n, s, f, g, dtype):
     assert np.abs(ref.f64(x)).max() * r["rstd"].max() < 128 or n * f // (s * g) < 64
     if n * f // (s * g) >= 64:
         assert np.all(np.abs(ref.f64(out) - r["out"]) <= t * (1 + np.abs(r["out"])))
+
+
+@pytest.mark.parametrize("n,s", [(2708, 1), (3000, 200), (60000, 5000), (20000, 3)])
+def test_captured_graphs_replay(n, s):
+    """Norm, router and 4-bit products, forward and backward, with their workspaces: every replay on new
+    inputs gives the bits of the eager calls."""
+    f, e, k = 64, 16, 2
+    r = np.random.default_rng(n)
+    p = np.concatenate([[0], np.sort(r.integers(0, n + 1, s - 1)), [n]]).astype(np.int32)
+    ptr = torch.from_numpy(p).to(DEV)
+    seg = torch.tensor([0, n // 3, n], dtype=torch.int32, device=DEV)
+    short = torch.tensor([0, 7, 20], dtype=torch.int32, device=DEV)
+    g = torch.Generator().manual_seed(n)
+    x = torch.randn(n, f, generator=g).bfloat16().to(DEV)
+    w = torch.randn(f, e, generator=g).to(DEV)
+    codes, scales = mp.mx_quantize(torch.randn(2, 48, f, generator=g).to(DEV))
+
+    def step():
+        out, mean, rstd = mp.group_norm(ptr, x, 8, act="gelu")
+        dx, dw, db = mp.group_norm_backward(ptr, x, out, 8, mean, rstd, act="gelu")
+        logits = mp.segment_matmul([0, n], out, w.bfloat16()[None])
+        idx, weight, counts, loss = mp.route(logits, k)
+        dl = mp.route_backward(logits, idx, weight, counts, dweight=weight, dloss=loss)
+        y = mp.mx_segment_matmul(seg, out, codes, scales)
+        few = mp.mx_segment_matmul(short, out[:20], codes, scales)
+        return [out, mean, rstd, dx, dw, db, idx, weight, counts, loss, dl, y, few]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for i in range(4):
+        x.copy_(torch.randn(n, f, generator=g).bfloat16())
+        want = step()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
