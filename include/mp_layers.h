@@ -11,6 +11,10 @@
  *                       balance and z losses, and its gradient
  *   mp_mx_*             microscaled 4-bit floating point: quantisation, and
  *                       the product of row segments with 4-bit weights
+ *   mp_embed            embedding rows by id, and the table's gradient
+ *   mp_rms_norm         root-mean-square norm with the residual's addition, in
+ *                       the rows' type or in 8 bits, and its gradients
+ *   mp_expert_mlp       the chosen experts of few rows in one call
  *
  * The dispatch between them is mp.h's: mp_coo_to_csr of (row, expert) pairs
  * sorts rows by expert and its rowptr is the segments of the products;
@@ -202,6 +206,94 @@ int mp_mx_segment_matmul_workspace(int64_t T, int64_t N, int64_t K, int64_t Fo, 
 int mp_mx_segment_matmul(const void* seg, int seg_itype, int64_t T, const void* x, int x_dtype,
                          int64_t N, int64_t K, int64_t ldx, const uint8_t* w_codes,
                          const uint8_t* w_scales, int64_t Fo, void* out, int out_dtype, void* ws,
+                         size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Embedding rows by id, times a scale:
+ *   out[r] = scale * table[ids[r]]
+ * An id outside [0, V), or equal to padding (-1: there is none), is padding:
+ * its row is 0 and reaches no gradient.
+ *   ids     [N] of ids_itype.
+ *   table   [V, F] of dtype, row v at element v * ldt (ldt >= F).
+ *   out     [N, F] contiguous of out_dtype; must not overlap the table.
+ * Sizes: 0 <= N <= INT32_MAX, 1 <= V < INT32_MAX, 1 <= F <= 65536.
+ * ------------------------------------------------------------------------- */
+int mp_embed(const void* ids, int ids_itype, int64_t N, const void* table, int dtype, int64_t V,
+             int64_t F, int64_t ldt, int64_t padding, float scale, void* out, int out_dtype,
+             void* stream);
+
+/* Workspace bytes of mp_embed_backward. */
+int mp_embed_backward_workspace(int64_t N, int64_t V, int64_t F, size_t* bytes);
+
+/* dL/dtable given dout = dL/dout [N, F] of dtype, row stride ldd:
+ *   dtable[v] = scale * sum over the rows r of id v of dout[r]
+ * summed in fp32 in the order of the rows, over rows sorted by id; the sums of
+ * an id of many rows are joined from chunks of it.
+ *   dtable  [V, F] contiguous of dtable_dtype, written in full (0 for an id of
+ *           no row); must not overlap dout.  All of it is NaN if the sort gave
+ *           up (MP_ERR_SORT, as for mp_coo_to_csr).
+ *   ws      16-byte aligned. */
+int mp_embed_backward(const void* ids, int ids_itype, int64_t N, const void* dout, int dtype,
+                      int64_t V, int64_t F, int64_t ldd, int64_t padding, float scale,
+                      void* dtable, int dtable_dtype, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Root-mean-square norm of every row, after the residual's addition:
+ *   total = x + residual, rounded to dtype (x itself without a residual)
+ *   rstd  = 1 / sqrt(mean over the row of total^2 + eps)
+ *   out   = total * rstd * weight[c]
+ * The norm is that of total as it is stored, from which the gradient starts.
+ *   x         [N, F] of dtype, row stride ldx.
+ *   residual  [N, F] of dtype, row stride ldr, or NULL.
+ *   weight    [F] fp32 or NULL (1).
+ *   eps       at least the smallest normal fp32, at most 1e30.
+ *   total     [N, F] contiguous of dtype, or NULL; may be x or residual itself
+ *             (same address, rows contiguous), must not overlap them otherwise.
+ *   out       [N, F] contiguous of out_dtype; must not overlap x, residual or
+ *             total.
+ *   rstd      [N] fp32 or NULL (the gradient takes it).
+ * Sizes: 0 <= N <= INT32_MAX, 1 <= F <= 65536.
+ * ------------------------------------------------------------------------- */
+int mp_rms_norm(const void* x, int dtype, int64_t N, int64_t F, int64_t ldx, const void* residual,
+                int64_t ldr, const float* weight, float eps, void* total, void* out, int out_dtype,
+                float* rstd, void* stream);
+
+/* The same with out in microscaled 8-bit floating point (MXFP8 of the OCP
+ * Microscaling Formats, 2023, with E4M3 values): KB = ceil(F / 32) blocks of 32
+ * values of a row, each with a scale byte s (E8M0: 2^(s - 127); 255: every value
+ * is NaN).
+ *   codes   [N, KB * 32] bytes, 0 past F, 16-byte aligned;  scales [N, KB] bytes.
+ *   values  [N, F] contiguous of dtype: what they stand for (exact in either
+ *           type but for bf16 values below 2^-126), or NULL.
+ * The scale of a block is 2^(floor(log2 max|out|) - 8), no less than 2^-127 (a
+ * block of zeros has s = 0); values are divided by it, rounded to nearest even,
+ * and saturate at 448.  A block that holds an infinity or NaN gets s = 255. */
+int mp_rms_norm_mx8(const void* x, int dtype, int64_t N, int64_t F, int64_t ldx,
+                    const void* residual, int64_t ldr, const float* weight, float eps, void* total,
+                    uint8_t* codes, uint8_t* scales, void* values, float* rstd, void* stream);
+
+/* The values that 8-bit codes and scales of that layout stand for: out [N, K]
+ * contiguous of dtype; codes 16-byte aligned. */
+int mp_mx8_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t N, int64_t K,
+                      void* out, int dtype, void* stream);
+
+/* Workspace bytes of mp_rms_norm_backward (partial sums of dweight). */
+int mp_rms_norm_backward_workspace(int64_t N, int64_t F, int dtype, size_t* bytes);
+
+/* Gradients given dout = dL/dout [N, F] of dtype (contiguous), the forward's total
+ * (row stride ldt; x where there was no residual) and rstd:
+ *   xhat = total * rstd,  g = dout * weight
+ *   dx         = rstd * (g - xhat * mean over the row of g * xhat) + dtotal
+ *   dweight[c] = sum over the rows of dout * xhat
+ *   dtotal   [N, F] contiguous of dtype: the gradient that reaches total by
+ *            itself, or NULL (0).
+ *   dx       [N, F] contiguous of dx_dtype, the gradient of x and of residual, or
+ *            NULL; must not overlap the inputs.
+ *   dweight  [F] fp32 or NULL; not both outputs NULL.
+ *   ws       16-byte aligned; none is needed without dweight. */
+int mp_rms_norm_backward(const void* total, int dtype, int64_t N, int64_t F, int64_t ldt,
+                         const void* dout, const float* rstd, const float* weight,
+                         const void* dtotal, void* dx, int dx_dtype, float* dweight, void* ws,
                          size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus

@@ -94,6 +94,68 @@ size_t route_bytes(int64_t N, int64_t E) {
     return blocks > 1 ? (size_t)blocks * (size_t)(2 * E + 2) * 4 : 0;
 }
 
+// Workspace of the embedding's gradient, in pieces that start on 256 bytes.
+struct EmbedSpace {
+    size_t key, row, col, rowptr, status, part, sort, sort_bytes, bytes;
+};
+int embed_space(int64_t N, int64_t V, int64_t F, EmbedSpace& m) {
+    if (N < 0 || N > INT32_MAX || V < 1 || V >= INT32_MAX || F < 1 || F > kMaxF) return MP_ERR_SIZE;
+    const int st = mp_coo_to_csr_workspace(N, V + 1, MP_I32, 0, &m.sort_bytes);
+    if (st != MP_OK) return st;
+    size_t at = 0;
+    const auto take = [&](size_t bytes) {
+        const size_t b = at;
+        at = align_up(at + bytes, 256);
+        return b;
+    };
+    const int64_t C = embed_chunk(N);
+    m.key = take((size_t)N * 4);
+    m.row = take((size_t)N * 4);
+    m.col = take((size_t)N * 4);
+    m.rowptr = take((size_t)(V + 2) * 4);
+    m.status = take(4);
+    m.part = take(N > C ? (size_t)ceil_div(N, C) * 2 * (size_t)F * 4 : 0);
+    m.sort = take(m.sort_bytes);
+    m.bytes = at;
+    return MP_OK;
+}
+
+int rms_call(int dtype, int64_t N, int64_t F, int64_t ld) {
+    if (!valid_dtype(dtype)) return MP_ERR_DTYPE;
+    return N < 0 || N > INT32_MAX || F < 1 || F > kMaxF || ld < F ? MP_ERR_SIZE : MP_OK;
+}
+
+size_t rms_bytes(int64_t N, int64_t F, int dtype) {
+    const int64_t parts = rms_parts(N, F, dtype);
+    return parts > 1 ? (size_t)parts * (size_t)F * 4 : 0;
+}
+
+// What both forms of the forward check and pass on.
+int rms_forward(RmsParams& P, const void* x, int dtype, int64_t N, int64_t F, int64_t ldx,
+                const void* residual, int64_t ldr, const float* weight, float eps, void* total,
+                float* rstd) {
+    const int st = rms_call(dtype, N, F, ldx);
+    if (st != MP_OK) return st;
+    if ((residual && ldr < F) || !(eps >= FLT_MIN && eps <= 1e30f)) return MP_ERR_SIZE;
+    if (total && ((total == x && ldx != F) || (total == residual && ldr != F))) return MP_ERR_SIZE;
+    if (N > 0 && !x) return MP_ERR_NULL;
+    const size_t b = elem(dtype);
+    if (!aligned(x, b) || !aligned(residual, b) || !aligned(total, b) || !aligned(weight, 4) ||
+        !aligned(rstd, 4))
+        return MP_ERR_ALIGN;
+    P.x = x;
+    P.residual = residual;
+    P.weight = weight;
+    P.N = N;
+    P.F = F;
+    P.ldx = ldx;
+    P.ldr = ldr;
+    P.eps = eps;
+    P.total = total;
+    P.rstd = rstd;
+    return MP_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -346,6 +408,165 @@ int mp_mx_segment_matmul(const void* seg, int seg_itype, int64_t T, const void* 
     P.w_words = reinterpret_cast<uint32_t*>(w + m.w_words);
     P.out = out;
     return hip_status(launch_mx_product(P, x_dtype, out_dtype, as_stream(stream)));
+}
+
+int mp_embed(const void* ids, int ids_itype, int64_t N, const void* table, int dtype, int64_t V,
+             int64_t F, int64_t ldt, int64_t padding, float scale, void* out, int out_dtype,
+             void* stream) {
+    if (!valid_itype(ids_itype) || !valid_dtype(dtype) || !valid_dtype(out_dtype))
+        return MP_ERR_DTYPE;
+    if (N < 0 || N > INT32_MAX || V < 1 || V >= INT32_MAX || F < 1 || F > kMaxF || ldt < F)
+        return MP_ERR_SIZE;
+    if (N > 0 && (!ids || !table || !out)) return MP_ERR_NULL;
+    if (!aligned(ids, ids_itype == MP_I64 ? 8 : 4) || !aligned(table, elem(dtype)) ||
+        !aligned(out, elem(out_dtype)))
+        return MP_ERR_ALIGN;
+    EmbedParams P{};
+    P.ids = ids;
+    P.ids64 = ids_itype == MP_I64;
+    P.N = N;
+    P.V = V;
+    P.F = F;
+    P.padding = padding;
+    P.scale = scale;
+    P.in = table;
+    P.ld = ldt;
+    P.out = out;
+    P.out_bf16 = out_dtype == MP_BF16;
+    return hip_status(launch_embed(P, dtype, as_stream(stream)));
+}
+
+int mp_embed_backward_workspace(int64_t N, int64_t V, int64_t F, size_t* bytes) {
+    if (!bytes) return MP_ERR_NULL;
+    EmbedSpace m;
+    const int st = embed_space(N, V, F, m);
+    if (st != MP_OK) return st;
+    *bytes = m.bytes;
+    return MP_OK;
+}
+
+int mp_embed_backward(const void* ids, int ids_itype, int64_t N, const void* dout, int dtype,
+                      int64_t V, int64_t F, int64_t ldd, int64_t padding, float scale,
+                      void* dtable, int dtable_dtype, void* ws, size_t ws_bytes, void* stream) {
+    if (!valid_itype(ids_itype) || !valid_dtype(dtype) || !valid_dtype(dtable_dtype))
+        return MP_ERR_DTYPE;
+    EmbedSpace m;
+    int st = embed_space(N, V, F, m);
+    if (st != MP_OK) return st;
+    if (ldd < F) return MP_ERR_SIZE;
+    if ((N > 0 && (!ids || !dout)) || !dtable || !ws) return MP_ERR_NULL;
+    if (!aligned(ids, ids_itype == MP_I64 ? 8 : 4) || !aligned(dout, elem(dtype)) ||
+        !aligned(dtable, elem(dtable_dtype)) || !aligned(ws, 16))
+        return MP_ERR_ALIGN;
+    if (ws_bytes < m.bytes) return MP_ERR_WORKSPACE;
+    char* w = static_cast<char*>(ws);
+    int32_t* key = reinterpret_cast<int32_t*>(w + m.key);
+    int32_t* row = reinterpret_cast<int32_t*>(w + m.row);
+    int32_t* col = reinterpret_cast<int32_t*>(w + m.col);
+    int32_t* rowptr = reinterpret_cast<int32_t*>(w + m.rowptr);
+    int32_t* status = reinterpret_cast<int32_t*>(w + m.status);
+    EmbedParams P{};
+    P.ids = ids;
+    P.ids64 = ids_itype == MP_I64;
+    P.N = N;
+    P.V = V;
+    P.F = F;
+    P.padding = padding;
+    P.scale = scale;
+    P.in = dout;
+    P.ld = ldd;
+    P.out = dtable;
+    P.out_bf16 = dtable_dtype == MP_BF16;
+    P.rowptr = rowptr;
+    P.row = col;
+    P.key = key;
+    P.status = status;
+    P.part = reinterpret_cast<float*>(w + m.part);
+    st = hip_status(launch_embed_keys(P, key, row, as_stream(stream)));
+    if (st == MP_OK)
+        st = mp_coo_to_csr(row, key, N, V + 1, rowptr, MP_I32, col, nullptr, nullptr, nullptr,
+                           w + m.sort, m.sort_bytes, status, stream);
+    if (st != MP_OK) return st;
+    return hip_status(launch_embed_backward(P, dtype, as_stream(stream)));
+}
+
+int mp_rms_norm(const void* x, int dtype, int64_t N, int64_t F, int64_t ldx, const void* residual,
+                int64_t ldr, const float* weight, float eps, void* total, void* out, int out_dtype,
+                float* rstd, void* stream) {
+    if (!valid_dtype(out_dtype)) return MP_ERR_DTYPE;
+    RmsParams P{};
+    const int st =
+        rms_forward(P, x, dtype, N, F, ldx, residual, ldr, weight, eps, total, rstd);
+    if (st != MP_OK) return st;
+    if (N > 0 && !out) return MP_ERR_NULL;
+    if (!aligned(out, elem(out_dtype))) return MP_ERR_ALIGN;
+    P.out = out;
+    P.out_bf16 = out_dtype == MP_BF16;
+    return hip_status(launch_rms(P, dtype, as_stream(stream)));
+}
+
+int mp_rms_norm_mx8(const void* x, int dtype, int64_t N, int64_t F, int64_t ldx,
+                    const void* residual, int64_t ldr, const float* weight, float eps, void* total,
+                    uint8_t* codes, uint8_t* scales, void* values, float* rstd, void* stream) {
+    RmsParams P{};
+    const int st =
+        rms_forward(P, x, dtype, N, F, ldx, residual, ldr, weight, eps, total, rstd);
+    if (st != MP_OK) return st;
+    if (N > 0 && (!codes || !scales)) return MP_ERR_NULL;
+    if (!aligned(codes, 16) || !aligned(values, elem(dtype))) return MP_ERR_ALIGN;
+    P.codes = codes;
+    P.scales = scales;
+    P.out = values;
+    P.out_bf16 = dtype == MP_BF16;
+    return hip_status(launch_rms(P, dtype, as_stream(stream)));
+}
+
+int mp_mx8_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t N, int64_t K,
+                      void* out, int dtype, void* stream) {
+    if (!valid_dtype(dtype)) return MP_ERR_DTYPE;
+    if (N < 0 || N > INT32_MAX || K < 1 || K > kMaxF) return MP_ERR_SIZE;
+    if (N > 0 && (!codes || !scales || !out)) return MP_ERR_NULL;
+    if (!aligned(codes, 16) || !aligned(out, elem(dtype))) return MP_ERR_ALIGN;
+    return hip_status(launch_mx8_dequantize(codes, scales, N, K, out, dtype, as_stream(stream)));
+}
+
+int mp_rms_norm_backward_workspace(int64_t N, int64_t F, int dtype, size_t* bytes) {
+    if (!bytes) return MP_ERR_NULL;
+    const int st = rms_call(dtype, N, F, F);
+    if (st != MP_OK) return st;
+    *bytes = rms_bytes(N, F, dtype);
+    return MP_OK;
+}
+
+int mp_rms_norm_backward(const void* total, int dtype, int64_t N, int64_t F, int64_t ldt,
+                         const void* dout, const float* rstd, const float* weight,
+                         const void* dtotal, void* dx, int dx_dtype, float* dweight, void* ws,
+                         size_t ws_bytes, void* stream) {
+    const int st = rms_call(dtype, N, F, ldt);
+    if (st != MP_OK) return st;
+    if (!valid_dtype(dx_dtype)) return MP_ERR_DTYPE;
+    const size_t need = dweight ? rms_bytes(N, F, dtype) : 0;
+    if ((N > 0 && (!total || !dout || !rstd)) || (!dx && !dweight) || (need && !ws))
+        return MP_ERR_NULL;
+    if (!aligned(total, elem(dtype)) || !aligned(dout, elem(dtype)) || !aligned(rstd, 4) ||
+        !aligned(weight, 4) || !aligned(dtotal, elem(dtype)) || !aligned(dx, elem(dx_dtype)) ||
+        !aligned(dweight, 4) || !aligned(ws, 16))
+        return MP_ERR_ALIGN;
+    if (ws_bytes < need) return MP_ERR_WORKSPACE;
+    RmsParams P{};
+    P.x = total;
+    P.ldx = ldt;
+    P.N = N;
+    P.F = F;
+    P.dout = dout;
+    P.rstd = const_cast<float*>(rstd);
+    P.weight = weight;
+    P.dtotal = dtotal;
+    P.out = dx;
+    P.out_bf16 = dx_dtype == MP_BF16;
+    P.dweight = dweight;
+    P.part = static_cast<float*>(ws);
+    return hip_status(launch_rms_backward(P, dtype, as_stream(stream)));
 }
 
 }  // extern "C"

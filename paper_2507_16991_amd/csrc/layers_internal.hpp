@@ -99,6 +99,50 @@ __device__ inline void store_one(typename T::raw* p, float v) {
     else *p = (uint16_t)pack_bf16(v, 0.f);
 }
 
+// ---- reductions over L neighbouring lanes --------------------------------------
+template <int CTRL>
+__device__ inline uint32_t dpp(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true);
+}
+
+// op over aligned groups of L lanes, the result in all of them: lanes 1 and 2
+// apart by quad permutes, then mirrored halves and rows of 16 (whose quads,
+// then halves, are already equal), then 16 and 32 apart.
+template <int L, typename Op>
+__device__ inline uint32_t reduce(uint32_t x, Op op) {
+    if constexpr (L > 1) x = op(x, dpp<0xB1>(x));   // quad_perm [1, 0, 3, 2]
+    if constexpr (L > 2) x = op(x, dpp<0x4E>(x));   // quad_perm [2, 3, 0, 1]
+    if constexpr (L > 4) x = op(x, dpp<0x141>(x));  // row_half_mirror
+    if constexpr (L > 8) x = op(x, dpp<0x140>(x));  // row_mirror
+    if constexpr (L > 16) x = op(x, (uint32_t)__shfl_xor((int)x, 16));
+    if constexpr (L > 32) x = op(x, (uint32_t)__shfl_xor((int)x, 32));
+    return x;
+}
+template <int L>
+__device__ inline uint32_t reduce_max(uint32_t x) {
+    return reduce<L>(x, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+template <int L>
+__device__ inline uint32_t reduce_min(uint32_t x) {
+    return reduce<L>(x, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+}
+template <int L>
+__device__ inline uint32_t reduce_add(uint32_t x) {
+    return reduce<L>(x, [](uint32_t a, uint32_t b) { return a + b; });
+}
+template <int L>
+__device__ inline float reduce_sum(float x) {
+    return __uint_as_float(reduce<L>(__float_as_uint(x), [](uint32_t a, uint32_t b) {
+        return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+    }));
+}
+template <int L>
+__device__ inline float reduce_fmax(float x) {
+    return __uint_as_float(reduce<L>(__float_as_uint(x), [](uint32_t a, uint32_t b) {
+        return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+    }));
+}
+
 // ---- dropout (dropout.hip) -----------------------------------------------------
 struct DropoutParams {
     const void* x;
@@ -199,5 +243,53 @@ hipError_t launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int
 // Whether a product of these sizes has no more tiles than a launch can hold.
 bool mx_product_fits(int64_t T, int64_t N, int64_t K, int64_t Fo);
 hipError_t launch_mx_product(const MxParams& p, int x_dtype, int out_dtype, hipStream_t s);
+
+// ---- root-mean-square norm (rms.hip) ---------------------------------------------------
+struct RmsParams {
+    const void* x;
+    const void* residual;  // nullptr: none
+    const float* weight;   // nullptr: 1
+    int64_t N, F, ldx, ldr;
+    float eps;
+    void* total;           // nullptr: not wanted
+    float* rstd;           // forward: nullptr: not wanted
+    void* out;             // forward: nullptr for a result in 8 bits alone; backward: dx or nullptr
+    int out_bf16;
+    uint8_t* codes;        // forward, in 8 bits
+    uint8_t* scales;
+    // backward (x: the forward's total)
+    const void* dout;
+    const void* dtotal;    // nullptr: 0
+    float* dweight;        // nullptr: not wanted
+    float* part;           // workspace [rms_parts][F]
+};
+// Lines of partial weight gradients (1: none are needed).
+int64_t rms_parts(int64_t N, int64_t F, int dtype);
+hipError_t launch_rms(const RmsParams& p, int dtype, hipStream_t s);
+hipError_t launch_rms_backward(const RmsParams& p, int dtype, hipStream_t s);
+hipError_t launch_mx8_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t N, int64_t K,
+                                 void* out, int dtype, hipStream_t s);
+
+// ---- embeddings (embed.hip) --------------------------------------------------------------
+struct EmbedParams {
+    const void* ids;
+    int ids64;
+    int64_t N, V, F, padding;  // padding: this id counts as one outside the table (-1: none)
+    float scale;
+    const void* in;            // the table, or dout
+    int64_t ld;
+    void* out;                 // rows, or the table's gradient
+    int out_bf16;
+    // backward
+    const int32_t* rowptr;     // [V + 2] positions of every id; ids outside come last
+    const int32_t* row;        // [N] the row at every position
+    const int32_t* key;        // [N] the id of every row, V outside
+    const int32_t* status;     // the sort's
+    float* part;               // [embed_chunks][2][F]
+};
+int64_t embed_chunk(int64_t N);
+hipError_t launch_embed(const EmbedParams& p, int dtype, hipStream_t s);
+hipError_t launch_embed_keys(const EmbedParams& p, int32_t* key, int32_t* row, hipStream_t s);
+hipError_t launch_embed_backward(const EmbedParams& p, int dtype, hipStream_t s);
 
 }  // namespace mp

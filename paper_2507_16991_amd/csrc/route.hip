@@ -22,50 +22,6 @@ constexpr int kBlock = 512;
 constexpr int kWaves = kBlock / kWave;
 constexpr int kFinish = 1024;  // threads of the launch that adds the partial sums
 
-// ---- reductions over L neighbouring lanes --------------------------------------
-template <int CTRL>
-__device__ inline uint32_t dpp(uint32_t x) {
-    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true);
-}
-
-// op over aligned groups of L lanes, the result in all of them: lanes 1 and 2
-// apart by quad permutes, then mirrored halves and rows of 16 (whose quads,
-// then halves, are already equal), then 16 and 32 apart.
-template <int L, typename Op>
-__device__ inline uint32_t reduce(uint32_t x, Op op) {
-    if constexpr (L > 1) x = op(x, dpp<0xB1>(x));   // quad_perm [1, 0, 3, 2]
-    if constexpr (L > 2) x = op(x, dpp<0x4E>(x));   // quad_perm [2, 3, 0, 1]
-    if constexpr (L > 4) x = op(x, dpp<0x141>(x));  // row_half_mirror
-    if constexpr (L > 8) x = op(x, dpp<0x140>(x));  // row_mirror
-    if constexpr (L > 16) x = op(x, (uint32_t)__shfl_xor((int)x, 16));
-    if constexpr (L > 32) x = op(x, (uint32_t)__shfl_xor((int)x, 32));
-    return x;
-}
-template <int L>
-__device__ inline uint32_t reduce_max(uint32_t x) {
-    return reduce<L>(x, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
-}
-template <int L>
-__device__ inline uint32_t reduce_min(uint32_t x) {
-    return reduce<L>(x, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
-}
-template <int L>
-__device__ inline uint32_t reduce_add(uint32_t x) {
-    return reduce<L>(x, [](uint32_t a, uint32_t b) { return a + b; });
-}
-template <int L>
-__device__ inline float reduce_sum(float x) {
-    return __uint_as_float(reduce<L>(__float_as_uint(x), [](uint32_t a, uint32_t b) {
-        return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
-    }));
-}
-template <int L>
-__device__ inline float reduce_fmax(float x) {
-    return __uint_as_float(reduce<L>(__float_as_uint(x), [](uint32_t a, uint32_t b) {
-        return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
-    }));
-}
-
 // exp(x) for x <= 0 (and NaN): 2^(x log2 e) with the product's rounding error
 // put back to first order, relative error about 2^-23.
 __device__ inline float exp_neg(float x) {

@@ -1,5 +1,6 @@
 """Python binding of the operators around the aggregation (``include/mp_layers.h``): group norm with
-an activation, dropout, the softmax router and microscaled 4-bit floating point.
+an activation, dropout, the softmax router, microscaled 4-bit floating point, embeddings,
+root-mean-square norm and the experts of few rows.
 
 As in the package's root, ``mp_*`` functions carry the names of the C ABI and take tensors or None for
 pointers; the others size and allocate outputs and workspaces with torch.  The root re-exports all of
@@ -21,7 +22,10 @@ __all__ = ["MP_ACT", "mp_group_norm_workspace", "mp_group_norm", "mp_group_norm_
            "group_norm", "group_norm_backward", "mp_dropout", "dropout", "dropout_backward", "mp_route_workspace", "mp_route",
            "mp_route_backward", "route", "route_backward", "mp_mx_quantize", "mp_mx_dequantize",
            "mp_mx_segment_matmul_workspace", "mp_mx_segment_matmul", "mx_quantize", "mx_dequantize",
-           "mx_segment_matmul"]
+           "mx_segment_matmul", "mp_embed", "mp_embed_backward_workspace", "mp_embed_backward", "embed",
+           "embed_backward", "mp_rms_norm", "mp_rms_norm_mx8", "mp_rms_norm_backward_workspace",
+           "mp_rms_norm_backward", "mp_mx8_dequantize", "rms_norm", "rms_norm_mx8", "rms_norm_backward",
+           "mx8_dequantize"]
 
 MP_ACT = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 
@@ -50,7 +54,17 @@ def _layers():
         L.mp_mx_segment_matmul_workspace.argtypes = [i64, i64, i64, i64, psz]
         L.mp_mx_segment_matmul.argtypes = [p, i32, i64, p, i32, i64, i64, i64, p, p, i64, p, i32, p, sz,
                                            p]
-        for name in ("mp_mx_quantize", "mp_mx_dequantize", "mp_mx_segment_matmul_workspace",
+        L.mp_embed.argtypes = [p, i32, i64, p, i32, i64, i64, i64, i64, f32, p, i32, p]
+        L.mp_embed_backward_workspace.argtypes = [i64, i64, i64, psz]
+        L.mp_embed_backward.argtypes = [p, i32, i64, p, i32, i64, i64, i64, i64, f32, p, i32, p, sz, p]
+        L.mp_rms_norm.argtypes = [p, i32, i64, i64, i64, p, i64, p, f32, p, p, i32, p, p]
+        L.mp_rms_norm_mx8.argtypes = [p, i32, i64, i64, i64, p, i64, p, f32, p, p, p, p, p, p]
+        L.mp_mx8_dequantize.argtypes = [p, p, i64, i64, p, i32, p]
+        L.mp_rms_norm_backward_workspace.argtypes = [i64, i64, i32, psz]
+        L.mp_rms_norm_backward.argtypes = [p, i32, i64, i64, i64, p, p, p, p, p, i32, p, p, sz, p]
+        for name in ("mp_embed", "mp_embed_backward_workspace", "mp_embed_backward", "mp_rms_norm",
+                     "mp_rms_norm_mx8", "mp_mx8_dequantize", "mp_rms_norm_backward_workspace",
+                     "mp_rms_norm_backward", "mp_mx_quantize", "mp_mx_dequantize", "mp_mx_segment_matmul_workspace",
                      "mp_mx_segment_matmul", "mp_group_norm_workspace", "mp_group_norm", "mp_group_norm_backward",
                      "mp_dropout", "mp_route_workspace", "mp_route", "mp_route_backward"):
             getattr(L, name).restype = i32
@@ -409,3 +423,203 @@ def mx_segment_matmul(seg, x, codes, scales, *, out_dtype=torch.float32, out=Non
         mp_mx_segment_matmul(seg, it, T, xp, dt, N, K, ldx, codes, scales, Fo, out,
                              _dtype_code(out.dtype), ws, nb, stream)
     return out
+
+
+# ---- embeddings ------------------------------------------------------------------------------
+
+def mp_embed(ids, ids_itype, N, table, dtype, V, F, ldt, padding, scale, out, out_dtype, stream=None):
+    """table: a tensor (rows may be strided) or a raw address."""
+    tp = _rows_ptr(table)[0] if isinstance(table, torch.Tensor) else table
+    _check("mp_embed", _layers().mp_embed(
+        _ptr(ids), ids_itype, N, tp, dtype, V, F, ldt, padding, scale, _ptr(out), out_dtype,
+        _stream(stream)))
+
+
+def mp_embed_backward_workspace(N, V, F) -> int:
+    _layers()
+    return _bytes("mp_embed_backward_workspace", N, V, F)
+
+
+def mp_embed_backward(ids, ids_itype, N, dout, dtype, V, F, ldd, padding, scale, dtable, dtable_dtype,
+                      ws, ws_bytes, stream=None):
+    """dout: a tensor (rows may be strided) or a raw address."""
+    dp = _rows_ptr(dout)[0] if isinstance(dout, torch.Tensor) else dout
+    _check("mp_embed_backward", _layers().mp_embed_backward(
+        _ptr(ids), ids_itype, N, dp, dtype, V, F, ldd, padding, scale, _ptr(dtable), dtable_dtype,
+        _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def _padding(padding):
+    if padding is not None and padding < 0:
+        raise ValueError("padding must be an id of the table (ids outside it are padding anyway)")
+    return -1 if padding is None else int(padding)
+
+
+def embed(ids, table, *, scale=1.0, padding=None, out_dtype=None, out=None, stream=None):
+    """scale * table[ids], [N, F] of out_dtype (default the table's): ids [N] int32 or int64, table
+    [V, F].  Ids outside [0, V), and the id `padding`, give rows of zeros."""
+    V, F = int(table.shape[0]), int(table.shape[1])
+    if ids.dim() != 1:
+        raise ValueError("ids [N] expected")
+    N = int(ids.shape[0])
+    if out is not None and tuple(out.shape) != (N, F):
+        raise ValueError("out must be [N, F]")
+    pad = _padding(padding)
+    _on_gpu(ids, table, out)
+    dt, it = _dtype_code(table.dtype), _itype_code(ids.dtype)
+    tp, ldt = _rows_ptr(table)
+    if out is None:
+        with _on(stream):
+            out = torch.empty(N, F, dtype=out_dtype or table.dtype, device=table.device)
+    mp_embed(ids, it, N, tp, dt, V, F, ldt, pad, scale, out, _dtype_code(out.dtype), stream)
+    return out
+
+
+def embed_backward(ids, dout, V, *, scale=1.0, padding=None, out_dtype=None, out=None, stream=None):
+    """dL/dtable [V, F] of out_dtype (default dout's) of embed given dout = dL/dout [N, F], in full: 0 for
+    ids of no row.  Sums are in fp32 and in the rows' order, whatever runs beside."""
+    V, N, F = int(V), int(dout.shape[0]), int(dout.shape[1])
+    if ids.dim() != 1 or int(ids.shape[0]) != N:
+        raise ValueError("ids [N] and dout [N, F] expected")
+    if out is not None and tuple(out.shape) != (V, F):
+        raise ValueError("out must be [V, F]")
+    pad = _padding(padding)
+    _on_gpu(ids, dout, out)
+    dt, it = _dtype_code(dout.dtype), _itype_code(ids.dtype)
+    dp, ldd = _rows_ptr(dout)
+    nb = _sized(mp_embed_backward_workspace, N, V, F)
+    with _on(stream):
+        if out is None:
+            out = torch.empty(V, F, dtype=out_dtype or dout.dtype, device=dout.device)
+        ws = _workspace(nb, dout.device)
+        mp_embed_backward(ids, it, N, dp, dt, V, F, ldd, pad, scale, out, _dtype_code(out.dtype), ws, nb,
+                          stream)
+    return out
+
+
+# ---- root-mean-square norm ---------------------------------------------------------------------
+
+def mp_rms_norm(x, dtype, N, F, ldx, residual, ldr, weight, eps, total, out, out_dtype, rstd,
+                stream=None):
+    """x and residual: tensors (rows may be strided) or raw addresses."""
+    xp, rp = (_rows_ptr(t)[0] if isinstance(t, torch.Tensor) else t for t in (x, residual))
+    _check("mp_rms_norm", _layers().mp_rms_norm(
+        xp, dtype, N, F, ldx, rp, ldr, _ptr(weight), eps, _ptr(total), _ptr(out), out_dtype, _ptr(rstd),
+        _stream(stream)))
+
+
+def mp_rms_norm_mx8(x, dtype, N, F, ldx, residual, ldr, weight, eps, total, codes, scales, values, rstd,
+                    stream=None):
+    xp, rp = (_rows_ptr(t)[0] if isinstance(t, torch.Tensor) else t for t in (x, residual))
+    _check("mp_rms_norm_mx8", _layers().mp_rms_norm_mx8(
+        xp, dtype, N, F, ldx, rp, ldr, _ptr(weight), eps, _ptr(total), _ptr(codes), _ptr(scales),
+        _ptr(values), _ptr(rstd), _stream(stream)))
+
+
+def mp_mx8_dequantize(codes, scales, N, K, out, dtype, stream=None):
+    _check("mp_mx8_dequantize", _layers().mp_mx8_dequantize(
+        _ptr(codes), _ptr(scales), N, K, _ptr(out), dtype, _stream(stream)))
+
+
+def mp_rms_norm_backward_workspace(N, F, dtype) -> int:
+    _layers()
+    return _bytes("mp_rms_norm_backward_workspace", N, F, dtype)
+
+
+def mp_rms_norm_backward(total, dtype, N, F, ldt, dout, rstd, weight, dtotal, dx, dx_dtype, dweight, ws,
+                         ws_bytes, stream=None):
+    tp = _rows_ptr(total)[0] if isinstance(total, torch.Tensor) else total
+    _check("mp_rms_norm_backward", _layers().mp_rms_norm_backward(
+        tp, dtype, N, F, ldt, _ptr(dout), _ptr(rstd), _ptr(weight), _ptr(dtotal), _ptr(dx), dx_dtype,
+        _ptr(dweight), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def _rms_operands(x, weight, residual, total):
+    N, F = int(x.shape[0]), int(x.shape[1])
+    _vector(weight, F, torch.float32, "weight")
+    _like(residual, x, "residual")
+    _like(total, x, "total")
+    _on_gpu(x, weight, residual, total)
+    xp, ldx = _rows_ptr(x)
+    rp, ldr = _rows_ptr(residual) if residual is not None else (None, F)
+    return N, F, _dtype_code(x.dtype), xp, ldx, rp, ldr
+
+
+def rms_norm(x, weight=None, *, residual=None, eps=1e-5, out_dtype=None, out=None, total=None,
+             stream=None):
+    """Root-mean-square norm of the rows of x [N, F], or of x + residual: (out [N, F] of out_dtype
+    (default x's), total [N, F]: the sum as it is stored (x itself without a residual), rstd [N] fp32);
+    the latter two go to rms_norm_backward.  weight [F] fp32.  total may be given, as x or residual
+    itself to be overwritten."""
+    N, F, dt, xp, ldx, rp, ldr = _rms_operands(x, weight, residual, total)
+    if out is not None and out.shape != x.shape:
+        raise ValueError("out must have the shape of x")
+    _on_gpu(out)
+    dev = x.device
+    with _on(stream):
+        if out is None:
+            out = torch.empty(N, F, dtype=out_dtype or x.dtype, device=dev)
+        rstd = torch.empty(N, dtype=torch.float32, device=dev)
+        if residual is not None and total is None:
+            total = torch.empty(N, F, dtype=x.dtype, device=dev)
+        mp_rms_norm(xp, dt, N, F, ldx, rp, ldr, weight, eps, total, out, _dtype_code(out.dtype), rstd,
+                    stream)
+    return out, x if total is None else total, rstd
+
+
+def rms_norm_mx8(x, weight=None, *, residual=None, eps=1e-5, want_values=False, total=None, stream=None):
+    """rms_norm in microscaled 8 bits: (codes [N, 32 KB] uint8, scales [N, KB] uint8, values, total),
+    KB = ceil(F / 32).  values: what they stand for, [N, F] of x's dtype, or None without want_values;
+    total as rms_norm's.  (codes, scales) are rows of expert_mlp."""
+    N, F, dt, xp, ldx, rp, ldr = _rms_operands(x, weight, residual, total)
+    dev, kb = x.device, _blocks(F)
+    with _on(stream):
+        codes = torch.empty(N, 32 * kb, dtype=torch.uint8, device=dev)
+        scales = torch.empty(N, kb, dtype=torch.uint8, device=dev)
+        values = torch.empty(N, F, dtype=x.dtype, device=dev) if want_values else None
+        if residual is not None and total is None:
+            total = torch.empty(N, F, dtype=x.dtype, device=dev)
+        mp_rms_norm_mx8(xp, dt, N, F, ldx, rp, ldr, weight, eps, total, codes, scales, values, None,
+                        stream)
+    return codes, scales, values, x if total is None else total
+
+
+def _mx8(codes, scales, K):
+    kb = _blocks(K)
+    if (codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.dim() != 2
+            or codes.shape[1] != 32 * kb or tuple(scales.shape) != (codes.shape[0], kb)):
+        raise ValueError(f"codes [N, {32 * kb}] and scales [N, {kb}] of uint8 expected for K = {K}")
+
+
+def mx8_dequantize(codes, scales, K, *, dtype=torch.float32, stream=None):
+    """The values [N, K] that 8-bit codes and scales stand for."""
+    _mx8(codes, scales, K)
+    _on_gpu(codes, scales)
+    with _on(stream):
+        out = torch.empty(codes.shape[0], int(K), dtype=dtype, device=codes.device)
+        mp_mx8_dequantize(codes, scales, int(codes.shape[0]), int(K), out, _dtype_code(dtype), stream)
+    return out
+
+
+def rms_norm_backward(total, dout, rstd, weight=None, *, dtotal=None, dx_dtype=None, want_dx=True,
+                      want_dw=True, stream=None):
+    """Gradients of rms_norm given dout [N, F] (dtype of x), its total and rstd, and dtotal (the gradient
+    that reaches total by itself): (dx [N, F] of dx_dtype (default x's), of x and of residual alike, or
+    None; dweight [F] fp32 or None)."""
+    N, F = int(total.shape[0]), int(total.shape[1])
+    _like(dout, total, "dout")
+    _like(dtotal, total, "dtotal")
+    _vector(rstd, N, torch.float32, "rstd")
+    _vector(weight, F, torch.float32, "weight")
+    _on_gpu(total, dout, rstd, weight, dtotal)
+    dt = _dtype_code(total.dtype)
+    tp, ldt = _rows_ptr(total)
+    nb = _sized(mp_rms_norm_backward_workspace, N, F, dt) if want_dw else 0
+    dev = total.device
+    with _on(stream):
+        dx = torch.empty(N, F, dtype=dx_dtype or total.dtype, device=dev) if want_dx else None
+        dw = torch.empty(F, dtype=torch.float32, device=dev) if want_dw else None
+        ws = _workspace(nb, dev) if nb else None
+        mp_rms_norm_backward(tp, dt, N, F, ldt, dout, rstd, weight, dtotal, dx,
+                             _dtype_code(dx.dtype) if want_dx else MP_F32, dw, ws, nb, stream)
+    return dx, dw

@@ -1,0 +1,162 @@
+"""Embedding rows by id and the table's gradient against their definitions in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2507_16991_amd as mp
+import row_refs as ref
+from layer_refs import f64
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def make(n, v, f, dtype, itype, spread="popular", seed=0, bad=True):
+    r = np.random.default_rng([seed, n, v, f])
+    u = r.random(n)
+    ids = np.minimum((np.exp(u * np.log(v + 1)) - 1 if spread == "popular" else u * v).astype(np.int64),
+                     v - 1)
+    if spread == "one":
+        ids[:] = v // 2
+    if bad and n > 2:  # outside the table: padding
+        ids[r.integers(0, n)] = -1
+        ids[r.integers(0, n)] = v
+        ids[r.integers(0, n)] = np.iinfo(np.int32).min if itype == torch.int32 else -2 ** 40
+        if itype == torch.int64:
+            ids[r.integers(0, n)] = 2 ** 32  # (0 once cut to 32 bits)
+    g = torch.Generator().manual_seed(seed)
+    table = torch.randn(v, f, generator=g).to(dtype)
+    dout = torch.randn(n, f, generator=g).to(dtype)
+    return torch.from_numpy(ids).to(itype).to(DEV), table.to(DEV), dout.to(DEV)
+
+
+def check_forward(ids, table, scale, padding, out):
+    want = ref.embed(ids.cpu().numpy().astype(np.int64), f64(table), scale, padding)
+    # the product rounded to fp32, then to out's type
+    tol = np.abs(want) * (ref.U + ref.half_step(out.dtype) * (1 + ref.U))
+    assert (np.abs(f64(out) - want) <= tol).all()
+
+
+def check_backward(ids, dout, v, scale, padding, grad):
+    want, size, count = ref.embed_backward(ids.cpu().numpy().astype(np.int64), f64(dout), v, scale, padding)
+    # count additions and the product, each off by half a step of at most the sum of magnitudes
+    tol = size * (count[:, None] + 1) * ref.U
+    tol = tol + (np.abs(want) + tol) * (ref.half_step(grad.dtype) if grad.dtype == BF16 else 0)
+    assert (np.abs(f64(grad) - want) <= tol).all()
+    assert not f64(grad)[count == 0].any()
+
+
+@pytest.mark.parametrize("itype", [torch.int32, torch.int64])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,v,f", [(1, 1, 1), (1, 7, 128), (3, 5, 3), (65, 300, 7), (64, 64, 8), (1000, 37, 100),
+                                   (777, 20011, 33), (5000, 999, 4), (300, 41, 2049), (20000, 3, 1), (17, 9, 65536)])
+def test_rows_and_gradient(n, v, f, dtype, itype):
+    ids, table, dout = make(n, v, f, dtype, itype)
+    check_forward(ids, table, 1.7, None, mp.embed(ids, table, scale=1.7))
+    check_backward(ids, dout, v, 1.7, None, mp.embed_backward(ids, dout, v, scale=1.7))
+
+
+@pytest.mark.parametrize("dtype,out", [(F32, BF16), (BF16, F32)])
+def test_other_output_type(dtype, out):
+    ids, table, dout = make(500, 90, 50, dtype, torch.int64)
+    check_forward(ids, table, 0.3, None, mp.embed(ids, table, scale=0.3, out_dtype=out))
+    check_backward(ids, dout, 90, 0.3, None, mp.embed_backward(ids, dout, 90, scale=0.3, out_dtype=out))
+
+
+# ids of 63, 64 and 65 rows next to each other, and of ranges that begin and end inside of and on the
+# borders of the chunks in which long ones are summed
+@pytest.mark.parametrize("f", [1, 20, 129, 1500])
+@pytest.mark.parametrize("counts", [(64, 64, 64), (65, 63, 65, 64), (1, 127, 65, 190, 1, 64, 66), (200,),
+                                    (0, 3, 1000, 0, 0, 700, 5), (64, 65, 64, 129, 128, 127, 0)])
+def test_long_and_short_ids(counts, f):
+    ids = np.repeat(np.arange(len(counts)), counts)
+    ids = np.random.default_rng(5).permutation(ids)
+    dout = torch.randn(len(ids), f, generator=torch.Generator().manual_seed(f)).to(DEV)
+    t = torch.from_numpy(ids).to(DEV)
+    check_backward(t, dout, len(counts), 1.0, None, mp.embed_backward(t, dout, len(counts)))
+
+
+def test_one_id_has_all_rows():
+    ids, _, dout = make(70001, 513, 24, BF16, torch.int32, spread="one")
+    check_backward(ids, dout, 513, 2.0, None, mp.embed_backward(ids, dout, 513, scale=2.0))
+
+
+def test_large_batch():
+    """Past the sort of small inputs, chunks of more than 64 positions."""
+    ids, table, dout = make(1100003, 30011, 5, F32, torch.int64)
+    check_forward(ids, table, 1.0, None, mp.embed(ids, table))
+    check_backward(ids, dout, 30011, 1.0, None, mp.embed_backward(ids, dout, 30011))
+
+
+def test_padding_row_holds_anything():
+    ids, table, dout = make(400, 30, 40, F32, torch.int64, bad=False)
+    table[4] = float("nan")
+    dout[ids == 4] = float("inf")
+    out = mp.embed(ids, table, padding=4)
+    grad = mp.embed_backward(ids, dout, 30, padding=4)
+    check_forward(ids, torch.where(table.isnan(), 0, table), 1.0, 4, out)
+    check_backward(ids, torch.where(dout.isinf(), 0, dout), 30, 1.0, 4, grad)
+
+
+def test_everything_is_padding_and_nothing_is_there():
+    ids = torch.full((100,), -5, device=DEV, dtype=torch.int64)
+    dout = torch.full((100, 12), float("nan"), device=DEV)
+    assert not mp.embed(ids, torch.ones(3, 12, device=DEV)).any()
+    assert not mp.embed_backward(ids, dout, 3).any()
+    none = ids[:0]
+    assert mp.embed(none, torch.ones(3, 12, device=DEV)).shape == (0, 12)
+    assert not mp.embed_backward(none, dout[:0], 3).any()
+
+
+def test_strided_rows():
+    ids, table, dout = make(300, 50, 24, F32, torch.int32)
+    wide_t, wide_d = torch.full((50, 31), 9.0, device=DEV), torch.full((300, 29), 9.0, device=DEV)
+    wide_t[:, 3:27], wide_d[:, 1:25] = table, dout
+    assert torch.equal(mp.embed(ids, wide_t[:, 3:27]), mp.embed(ids, table))
+    assert torch.equal(mp.embed_backward(ids, wide_d[:, 1:25], 50), mp.embed_backward(ids, dout, 50))
+
+
+def test_same_bits_again_and_on_another_stream():
+    ids, table, dout = make(30000, 700, 64, BF16, torch.int64)
+    first = mp.embed_backward(ids, dout, 700)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    other = mp.embed_backward(ids, dout, 700, stream=s)
+    rows = mp.embed(ids, table, stream=s)
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(first, other) and torch.equal(rows, mp.embed(ids, table))
+
+
+def test_gradient_is_that_of_the_rows():
+    """<dout, embed(table + t d) - embed(table)> = t <dtable, d>: embed is linear in the table."""
+    ids, table, dout = make(900, 77, 31, F32, torch.int64)
+    grad = mp.embed_backward(ids, dout, 77, scale=3.0)
+    d = torch.randn(table.shape, generator=torch.Generator().manual_seed(9)).to(DEV)
+    lhs = float((mp.embed(ids, d, scale=3.0).double() * dout.double()).sum())
+    size = float((mp.embed(ids, d, scale=3.0).double() * dout.double()).abs().sum())
+    # every term is off by a rounding of the forward, and by at most 900 additions in the gradient
+    assert abs(lhs - float((grad.double() * d.double()).sum())) <= size * 902 * ref.U
+
+
+def test_replayed_from_a_graph():
+    ids, table, dout = make(20000, 3000, 40, F32, torch.int64)
+    out, grad = torch.empty(20000, 40, device=DEV), torch.empty(3000, 40, device=DEV)
+
+    def step():
+        mp.embed(ids, table, out=out)
+        mp.embed_backward(ids, dout, 3000, out=grad)
+
+    step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for seed in range(3):
+        new = make(20000, 3000, 40, F32, torch.int64, seed=seed + 1)
+        for a, b in zip((ids, table, dout), new):
+            a.copy_(b)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, mp.embed(ids, table))
+        assert torch.equal(grad, mp.embed_backward(ids, dout, 3000))
