@@ -296,6 +296,42 @@ int mp_rms_norm_backward(const void* total, int dtype, int64_t N, int64_t F, int
                          const void* dtotal, void* dx, int dx_dtype, float* dweight, void* ws,
                          size_t ws_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * The experts of few rows: for serving, all that follows the router, in two
+ * launches and without sorting the rows or waiting for the host.
+ *   z = w1[e] x,  h = act(z), or with `gated` act(z[0 .. H-1]) * z[H .. 2H-1]
+ *   out[r] = residual[r] + sum over the choices j of row r, e = idx[r, j], of
+ *            weight[r, j] * w2[e] h
+ * A choice with idx outside [0, E) adds nothing; an expert chosen twice by a row
+ * counts with both weights.  Weights of experts that no row chose are not read.
+ *   x          [N, K] of x_dtype, row stride ldx; or, with x_scales, 8-bit codes
+ *              [N, KB * 32] and scales [N, KB] as mp_rms_norm_mx8 writes them
+ *              (KB = ceil(K / 32); x_dtype and ldx are not looked at; codes
+ *              past K are 0).
+ *   idx        [N, k] int32, weight [N, k] fp32: mp_route's.
+ *   w1, w2     [E, (1 + gated) H, K] and [E, Fo, H] bf16; or, with w1_scales and
+ *              w2_scales (both or neither), 4-bit codes and scales as
+ *              mp_mx_quantize writes them for tables of these shapes, 16-byte
+ *              aligned (values past the largest fp32 are infinite).
+ *   residual   [N, Fo] of out_dtype, row stride ldr, or NULL.
+ *   out        [N, Fo] contiguous of out_dtype; may be residual itself (ldr = Fo),
+ *              must not overlap the inputs otherwise.
+ * Products of fp32 or bf16 values with bf16 or 4-bit ones are exact but for fp32
+ * values under a bf16 result, and h, which are taken to 16 bits of their mantissa (to
+ * all of them where out is fp32); 8-bit values and weights below 2^-126 are rounded
+ * to steps of 2^-133 (bf16's); sums are in fp32.
+ * Sizes: 0 <= N <= 64, 1 <= k <= E <= 1024, N * k <= 1024, 1 <= K, H, Fo <= 65536.
+ * ws 16-byte aligned; calls that may overlap need one each.
+ * ------------------------------------------------------------------------- */
+int mp_expert_mlp_workspace(int64_t N, int64_t k, int64_t H, int64_t Fo, int out_dtype,
+                            size_t* bytes);
+
+int mp_expert_mlp(const void* x, int x_dtype, const uint8_t* x_scales, int64_t N, int64_t K,
+                  int64_t ldx, const int32_t* idx, const float* weight, int64_t k, int64_t E,
+                  int64_t H, int64_t Fo, const void* w1, const uint8_t* w1_scales, const void* w2,
+                  const uint8_t* w2_scales, int act, int gated, const void* residual, int64_t ldr,
+                  void* out, int out_dtype, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

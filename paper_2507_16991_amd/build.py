@@ -19,7 +19,8 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 SOURCES = ["scan.hip", "sort.hip", "spmm.hip", "backward.hip", "gmm.hip", "messages.hip",
            "layout.hip", "probe.hip", "dropout.hip", "route.hip", "norm.hip",
-           "mx.hip", "rms.hip", "embed.hip", "api.cpp", "layers_api.cpp"]
+           "mx.hip", "rms.hip", "embed.hip", "experts.hip",
+           "api.cpp", "layers_api.cpp"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

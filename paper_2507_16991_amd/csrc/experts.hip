@@ -1,0 +1,635 @@
+// The chosen experts of few rows: up and gate product, activation and weight, down
+// product and the sum over a row's experts, in two launches (include/mp_layers.h).
+//
+// Bound by reading the chosen experts' weights, once.  Every workgroup finds the
+// experts that some row chose and the rows of each from idx by itself (a count
+// and a scan in LDS), so that no launch is spent on it.
+//   up:    a workgroup has 32 weight rows of an expert (16 of the gate and their 16
+//          of the other half), its wavefronts share K; h = act(.) * weight is left
+//          as a sum of bf16 terms.
+//   down:  a workgroup has 32 output columns and a share of the (expert, step of K)
+//          items, its wavefronts a run of them; what they add to each row is
+//          joined in LDS, and the shares by the workgroup that ends last.
+// Products run on v_mfma_f32_16x16x32_bf16, weights first, so that a lane's
+// accumulators are neighbouring columns of one row.  4-bit weights are exact in
+// bf16, and so are 8-bit rows; fp32 values are taken as sums of bf16 terms, three
+// of which are exact (two, off by 2^-16, where the result is bf16).
+#include "layers_internal.hpp"
+
+namespace mp {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kBlock = 256;
+constexpr int kWaves = kBlock / kWave;
+constexpr int kStep = 128;    // elements of K of a step, 32 for a quarter of the lanes
+constexpr int kCols = 32;     // weight rows of a workgroup
+constexpr int kLine = 36;     // floats of a row's sums in LDS
+
+// 2^(s - 127) (s = 0 is subnormal); NaN for 255.
+__device__ inline float scale_value(uint32_t s) {
+    return __uint_as_float(s == 255 ? 0x7FC00000u : (s ? s << 23 : 0x00400000u));
+}
+
+// ---- the rows of every expert ------------------------------------------------------
+// In LDS: the pairs (row, choice) of each expert that has any.  A choice that repeats
+// an expert of its row is left out; its weight goes to the first.
+struct Lists {
+    int* first;      // [E + 1] first place of an expert's pairs
+    int* cursor;     // [E] (the count, at first)
+    int* active;     // [E] experts that have pairs, in order
+    int* chosen;     // [P] expert of a pair, or -1
+    int* pairs;      // [P] by expert
+    int* total;      // [1] how many are active
+};
+__host__ __device__ inline int list_words(int E, int P) { return 3 * E + 2 * P + 2; }
+
+__device__ inline Lists carve(int* lds, int E, int P) {
+    Lists l;
+    l.first = lds;
+    l.cursor = l.first + E + 1;
+    l.active = l.cursor + E;
+    l.chosen = l.active + E;
+    l.pairs = l.chosen + P;
+    l.total = l.pairs + P;
+    return l;
+}
+
+__device__ inline void find_rows(const ExpertParams& p, const Lists& l) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    for (int i = tid; i < p.P; i += kBlock) {
+        const int e = p.idx[i];
+        l.chosen[i] = e >= 0 && e < p.E ? e : -1;
+    }
+    for (int e = tid; e < p.E; e += kBlock) l.cursor[e] = 0;
+    __syncthreads();
+    for (int i = tid; i < p.P; i += kBlock) {
+        const int e = l.chosen[i];
+        bool again = e < 0;
+        for (int j = i - i % p.k; j < i; ++j) again |= l.chosen[j] == e;
+        l.pairs[i] = again ? -1 : e;
+    }
+    __syncthreads();
+    for (int i = tid; i < p.P; i += kBlock) {
+        l.chosen[i] = l.pairs[i];
+        if (l.pairs[i] >= 0) atomicAdd(&l.cursor[l.pairs[i]], 1);
+    }
+    __syncthreads();
+    if (tid < 64) {  // a wavefront's scan, 64 experts at a time
+        int places = 0, experts = 0;
+        for (int e0 = 0; e0 < p.E; e0 += 64) {
+            const int e = e0 + lane, n = e < p.E ? l.cursor[e] : 0;
+            int sum = n;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int v = __shfl_up(sum, o);
+                if (lane >= o) sum += v;
+            }
+            const uint64_t some = __ballot(n > 0);
+            if (e < p.E) {
+                l.first[e] = places + sum - n;
+                l.cursor[e] = places + sum - n;
+            }
+            if (n > 0) l.active[experts + (int)count_below(some)] = e;
+            places += __shfl(sum, 63);
+            experts += __popcll(some);
+        }
+        if (lane == 0) {
+            l.first[p.E] = places;
+            *l.total = experts;
+        }
+    }
+    __syncthreads();
+    // (the order of an expert's pairs is left open: each has its own row of h and of
+    // the sums, whatever its place in a product)
+    for (int i = tid; i < p.P; i += kBlock)
+        if (l.chosen[i] >= 0) l.pairs[atomicAdd(&l.cursor[l.chosen[i]], 1)] = i;
+    __syncthreads();
+}
+
+// ---- operands ------------------------------------------------------------------------
+// A step's 128 elements of K lie on four quarters of the lanes; quarter q has, in its
+// i-th of four products, the elements at(i, q) .. + 7.  Any order will do that both
+// operands share: 4-bit weights take a whole block to a lane (16 bytes), bf16 ones
+// go through memory by whole lines.
+struct WeightsMx4 {
+    static constexpr int kSteps = 4;  // steps whose loads are under way
+    struct Raw {
+        uint32_t c[4];
+        uint32_t s;
+    };
+    struct Row {
+        const uint8_t* codes;
+        const uint8_t* scales;
+    };
+    __device__ static int at(int i, int q) { return 32 * q + 8 * i; }
+    __device__ static Row row(const void* w, const uint8_t* scales, int64_t r, int K) {
+        const int64_t KB = (K + 31) / 32;
+        return Row{static_cast<const uint8_t*>(w) + r * KB * 16, scales + r * KB};
+    }
+    __device__ static Raw load(const Row& w, int s, int q, int K) {
+        const int KB = (K + 31) / 32, b = 4 * s + q;
+        Raw r = {};
+        if (b < KB) {
+            __builtin_memcpy(r.c, w.codes + (int64_t)b * 16, 16);
+            if (4 * s + 4 <= KB) {
+                __builtin_memcpy(&r.s, w.scales + 4 * s, 4);
+                r.s = (r.s >> (8 * q)) & 255;
+            } else {
+                r.s = w.scales[b];
+            }
+        }
+        return r;
+    }
+    __device__ static void unpack(const Raw& r, bf16x8 (&v)[4]) {
+        const float f = scale_value(r.s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            bf16x2 t[4];
+            t[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.c[i], f, 0);
+            t[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.c[i], f, 1);
+            t[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.c[i], f, 2);
+            t[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.c[i], f, 3);
+            __builtin_memcpy(&v[i], t, 16);
+        }
+    }
+};
+
+// Eight bf16 elements k .. k+7 of a row of K, zero past its end.
+__device__ inline bf16x8 load_bf16(const uint16_t* p, int k, int K) {
+    uint16_t u[8] = {};
+    if (k + 8 <= K) {
+        __builtin_memcpy(u, p + k, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (k + i < K) u[i] = p[k + i];
+    }
+    bf16x8 v;
+    __builtin_memcpy(&v, u, 16);
+    return v;
+}
+
+struct WeightsBf16 {
+    static constexpr int kSteps = 2;
+    struct Raw {
+        bf16x8 v[4];
+    };
+    typedef const uint16_t* Row;
+    __device__ static int at(int i, int q) { return 32 * i + 8 * q; }
+    __device__ static Row row(const void* w, const uint8_t*, int64_t r, int K) {
+        return static_cast<const uint16_t*>(w) + r * K;
+    }
+    __device__ static Raw load(const Row& w, int s, int q, int K) {
+        Raw r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.v[i] = load_bf16(w, kStep * s + at(i, q), K);
+        return r;
+    }
+    __device__ static void unpack(const Raw& r, bf16x8 (&v)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = r.v[i];
+    }
+};
+
+// An fp32 value as a sum of bf16 terms: its upper 16 bits, and so on of what is
+// left; of two terms the second is rounded.  Three are exact.  An infinity or NaN
+// is its first term.
+template <int T>
+__device__ inline void split(float x, uint16_t (&t)[T]) {
+    const uint32_t u = __float_as_uint(x);
+    float r = x - __uint_as_float(u & 0xFFFF0000u);
+    const bool finite = (u & 0x7F800000u) != 0x7F800000u;
+    // (the bits of a NaN may all lie in the lower half)
+    t[0] = (uint16_t)((u >> 16) | (!finite && (u & 0xFFFF) ? 0x40u : 0u));
+    r = finite ? r : 0.f;
+    if constexpr (T == 3) {
+        const uint32_t m = __float_as_uint(r);
+        t[1] = (uint16_t)(m >> 16);
+        r -= __uint_as_float(m & 0xFFFF0000u);
+    }
+    t[T - 1] = (uint16_t)pack_bf16(r, 0.f);
+}
+
+// Rows: kTerms bf16 terms of every element.
+template <int TERMS>
+struct RowsF32 {
+    static constexpr int kTerms = TERMS;
+    struct Raw {
+        float v[4][8];
+    };
+    typedef const float* Row;
+    __device__ static Row row(const ExpertParams& p, int r) {
+        return static_cast<const float*>(p.x) + r * p.ldx;
+    }
+    template <typename W>
+    __device__ static void load(Raw& r, const ExpertParams&, Row x, int s, int q, int K) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int k = kStep * s + W::at(i, q);
+            if (k + 8 <= K) {
+                __builtin_memcpy(r.v[i], x + k, 32);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) r.v[i][j] = k + j < K ? x[k + j] : 0.f;
+            }
+        }
+    }
+    __device__ static void unpack(const Raw& r, int i, bf16x8 (&v)[TERMS]) {
+        uint16_t t[TERMS][8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            uint16_t u[TERMS];
+            split<TERMS>(r.v[i][j], u);
+#pragma unroll
+            for (int m = 0; m < TERMS; ++m) t[m][j] = u[m];
+        }
+#pragma unroll
+        for (int m = 0; m < TERMS; ++m) __builtin_memcpy(&v[m], t[m], 16);
+    }
+};
+
+struct RowsBf16 {
+    static constexpr int kTerms = 1;
+    struct Raw {
+        bf16x8 v[4];
+    };
+    typedef const uint16_t* Row;
+    __device__ static Row row(const ExpertParams& p, int r) {
+        return static_cast<const uint16_t*>(p.x) + r * p.ldx;
+    }
+    template <typename W>
+    __device__ static void load(Raw& r, const ExpertParams&, Row x, int s, int q, int K) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.v[i] = load_bf16(x, kStep * s + W::at(i, q), K);
+    }
+    __device__ static void unpack(const Raw& r, int i, bf16x8 (&v)[1]) { v[0] = r.v[i]; }
+};
+
+struct RowsMx8 {
+    static constexpr int kTerms = 1;
+    struct Raw {
+        uint32_t c[4][2];
+        uint32_t s[4];
+    };
+    struct Row {
+        const uint8_t* codes;
+        const uint8_t* scales;
+    };
+    __device__ static Row row(const ExpertParams& p, int r) {
+        const int64_t KB = (p.K + 31) / 32;
+        return Row{static_cast<const uint8_t*>(p.x) + r * KB * 32, p.x_scales + r * KB};
+    }
+    template <typename W>
+    __device__ static void load(Raw& r, const ExpertParams&, const Row& x, int s, int q, int K) {
+        const int KB = (K + 31) / 32;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int k = kStep * s + W::at(i, q), b = k / 32;
+            r.c[i][0] = r.c[i][1] = r.s[i] = 0;
+            if (b < KB) {
+                __builtin_memcpy(r.c[i], x.codes + k, 8);
+                r.s[i] = x.scales[b];
+            }
+        }
+    }
+    __device__ static void unpack(const Raw& r, int i, bf16x8 (&v)[1]) {
+        const float f = scale_value(r.s[i]);
+        bf16x2 t[4];
+        t[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.c[i][0], f, false);
+        t[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.c[i][0], f, true);
+        t[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.c[i][1], f, false);
+        t[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.c[i][1], f, true);
+        __builtin_memcpy(&v[0], t, 16);
+    }
+};
+
+// Rows of h: TERMS planes, filled up with zeros to whole steps.
+template <int TERMS>
+struct RowsOfH {
+    static constexpr int kTerms = TERMS;
+    struct Raw {
+        bf16x8 v[TERMS][4];
+    };
+    typedef const uint16_t* Row;
+    template <typename W>
+    __device__ static void load(Raw& r, const ExpertParams& p, Row x, int s, int q, int) {
+#pragma unroll
+        for (int m = 0; m < TERMS; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                __builtin_memcpy(&r.v[m][i],
+                                 x + (int64_t)m * p.P * p.Hp + kStep * s + W::at(i, q), 16);
+    }
+    __device__ static void unpack(const Raw& r, int i, bf16x8 (&v)[TERMS]) {
+#pragma unroll
+        for (int m = 0; m < TERMS; ++m) v[m] = r.v[m][i];
+    }
+};
+
+// acc[t][m] += weight rows w[t] (this lane's of each 16) times rows x[m] (this lane's
+// of each 16; `has` where there is one), steps s0, s0 + by, ... below s1.  K: of the
+// weights, KX: of the rows.
+template <typename W, typename X, int M>
+__device__ inline void multiply(const ExpertParams& p, const typename W::Row (&w)[2],
+                                const typename X::Row (&x)[M], const bool (&has)[M], int K, int KX,
+                                int s0, int s1, int by, f32x4 (&acc)[2][M]) {
+    // as many steps' loads under way as registers allow: rows of fp32 or of many
+    // are taken one step at a time
+    constexpr int U = M > 1 ? 1 : (sizeof(typename X::Raw) > 64 && W::kSteps > 2 ? 2 : W::kSteps);
+    const int q = (threadIdx.x & 63) >> 4;
+    for (int s = s0; s < s1; s += U * by) {
+        typename W::Raw rw[U][2];
+        typename X::Raw rx[U][M];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int at = s + u * by;
+            if (at < s1) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) rw[u][t] = W::load(w[t], at, q, K);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int at = s + u * by;
+#pragma unroll
+            for (int m = 0; m < M; ++m) {
+                rx[u][m] = typename X::Raw{};
+                if (at < s1 && has[m]) X::template load<W>(rx[u][m], p, x[m], at, q, KX);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (s + u * by >= s1) break;
+            bf16x8 a[2][4];
+            W::unpack(rw[u][0], a[0]);
+            W::unpack(rw[u][1], a[1]);
+#pragma unroll
+            for (int m = 0; m < M; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    bf16x8 b[X::kTerms];
+                    X::unpack(rx[u][m], i, b);
+#pragma unroll
+                    for (int c = X::kTerms - 1; c >= 0; --c)
+#pragma unroll
+                        for (int t = 0; t < 2; ++t)
+                            acc[t][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[t][i], b[c],
+                                                                                acc[t][m], 0, 0, 0);
+                }
+        }
+    }
+}
+
+// ---- up ---------------------------------------------------------------------------------
+__device__ inline float activate(float z, int act) {
+    if (act == MP_ACT_RELU) return z < 0.f ? 0.f : z;  // (NaN stays)
+    if (act == MP_ACT_SILU) return z / (1.f + expf(-z));
+    if (act == MP_ACT_GELU) return 0.5f * z * erfcf(z * -0.707106781f);
+    return z;
+}
+
+// The pairs of expert e, at most 16 M of them, and the weight rows of a tile.
+template <typename W, typename X, bool GATED, int M>
+__device__ inline void up_rows(const ExpertParams& p, const Lists& l, int e, int tile,
+                               float* sums) {
+    constexpr int COLS = GATED ? 16 : 32;  // columns of h
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int begin = l.first[e], n = l.first[e + 1] - begin;
+    const int64_t rows = (int64_t)(1 + GATED) * p.H;
+    typename W::Row w[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        int c = tile * COLS + (GATED ? 0 : 16 * t) + (lane & 15);
+        c = c < p.H ? c : p.H - 1;  // (columns past the last are not stored)
+        w[t] = W::row(p.w1, p.w1_scales, e * rows + (GATED ? t * (int64_t)p.H : 0) + c, p.K);
+    }
+    typename X::Row x[M];
+    bool has[M];
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+        const int at = 16 * m + (lane & 15);
+        has[m] = at < n;
+        x[m] = X::row(p, has[m] ? l.pairs[begin + at] / p.k : 0);
+    }
+    f32x4 acc[2][M] = {};
+    multiply<W, X, M>(p, w, x, has, p.K, p.K, wave, (p.K + kStep - 1) / kStep, kWaves, acc);
+
+    // the wavefronts' sums: [wave][t][m][i][lane]
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int m = 0; m < M; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                sums[((((wave * 2 + t) * M + m) * 4 + i) << 6) + lane] = acc[t][m][i];
+    __syncthreads();
+    const int i = threadIdx.x >> 6;
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+        const int at = 16 * m + (lane & 15);
+        if (at >= n) continue;
+        const int pair = l.pairs[begin + at], j0 = pair % p.k, r0 = pair - j0;
+        float z[2] = {0.f, 0.f};
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+            for (int v = 0; v < kWaves; ++v)
+                z[t] += sums[((((v * 2 + t) * M + m) * 4 + i) << 6) + lane];
+        // the weight of this choice, and of later ones of the same expert
+        float weight = p.weight[pair];
+        for (int j = j0 + 1; j < p.k; ++j)
+            if (p.idx[r0 + j] == e) weight += p.weight[r0 + j];
+        const int c = 4 * (lane >> 4) + i;
+#pragma unroll
+        for (int t = 0; t < (GATED ? 1 : 2); ++t) {
+            float h = activate(z[t], p.act);
+            if (GATED) h *= z[1];
+            h *= weight;
+            const int col = tile * COLS + 16 * t + c;
+            if (col >= p.H) continue;
+            uint16_t term[3];
+            if (p.planes == 3) {
+                split<3>(h, term);
+            } else {
+                uint16_t two[2];
+                split<2>(h, two);
+                term[0] = two[0];
+                term[1] = two[1];
+                term[2] = 0;
+            }
+            for (int v = 0; v < p.planes; ++v)
+                p.h[((int64_t)v * p.P + pair) * p.Hp + col] = term[v];
+        }
+    }
+}
+
+template <typename W, typename X, bool GATED>
+__global__ __launch_bounds__(kBlock) void expert_up(ExpertParams p, int tiles) {
+    extern __shared__ int lds[];
+    const Lists l = carve(lds, p.E, p.P);
+    float* sums = reinterpret_cast<float*>(lds + (list_words(p.E, p.P) + 3) / 4 * 4);
+    if (p.splits > 1 && blockIdx.x == 0)  // (for the second launch)
+        for (int c = threadIdx.x; c < (p.Fo + kCols - 1) / kCols; c += kBlock) p.arrived[c] = 0;
+    find_rows(p, l);
+    const int slot = blockIdx.x / tiles, tile = blockIdx.x - slot * tiles;
+    if (slot >= *l.total) return;
+    const int e = l.active[slot], n = l.first[e + 1] - l.first[e];
+    if (n <= 16) {
+        up_rows<W, X, GATED, 1>(p, l, e, tile, sums);
+    } else {
+        up_rows<W, X, GATED, 4>(p, l, e, tile, sums);  // (no more than 64 rows)
+    }
+    if (tile == tiles - 1) {  // zeros fill the last step of the rows of h
+        const int more = p.Hp - p.H;
+        for (int i = threadIdx.x; i < n * more; i += kBlock)
+            for (int v = 0; v < p.planes; ++v)
+                p.h[((int64_t)v * p.P + l.pairs[l.first[e] + i / more]) * p.Hp + p.H + i % more] = 0;
+    }
+}
+
+// ---- down -----------------------------------------------------------------------------
+// The sums of this wavefront for the pairs of expert e, steps s0 .. s1-1.
+template <typename W, typename X, int M>
+__device__ inline void down_rows(const ExpertParams& p, const Lists& l, int e, int c0, int s0,
+                                 int s1, float* mine) {
+    const int lane = threadIdx.x & 63;
+    const int begin = l.first[e], n = l.first[e + 1] - begin;
+    typename W::Row w[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        int c = c0 + 16 * t + (lane & 15);
+        c = c < p.Fo ? c : p.Fo - 1;
+        w[t] = W::row(p.w2, p.w2_scales, (int64_t)e * p.Fo + c, p.H);
+    }
+    typename X::Row x[M];
+    bool has[M];
+    int row[M];
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+        const int at = 16 * m + (lane & 15);
+        has[m] = at < n;
+        const int pair = has[m] ? l.pairs[begin + at] : 0;
+        x[m] = p.h + (int64_t)pair * p.Hp;
+        row[m] = pair / p.k;
+    }
+    f32x4 acc[2][M] = {};
+    multiply<W, X, M>(p, w, x, has, p.H, p.Hp, s0, s1, 1, acc);
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+        if (!has[m]) continue;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {  // (rows of an expert's pairs differ)
+            f32x4* to = reinterpret_cast<f32x4*>(&mine[row[m] * kLine + 16 * t + 4 * (lane >> 4)]);
+            *to += acc[t][m];
+        }
+    }
+}
+
+template <typename W, typename X>
+__global__ __launch_bounds__(kBlock) void expert_down(ExpertParams p) {
+    extern __shared__ int lds[];
+    __shared__ int s_last;
+    const Lists l = carve(lds, p.E, p.P);
+    float* sums = reinterpret_cast<float*>(lds + (list_words(p.E, p.P) + 3) / 4 * 4);
+    const int tid = threadIdx.x, wave = tid >> 6;
+    const int tile = blockIdx.x / p.splits, share = blockIdx.x - tile * p.splits, c0 = tile * kCols;
+    float* mine = sums + wave * p.N * kLine;
+    for (int i = tid; i < kWaves * p.N * kLine; i += kBlock) sums[i] = 0.f;
+    find_rows(p, l);
+    const int steps = p.Hp / kStep;
+    const int64_t items = (int64_t)*l.total * steps, runs = (int64_t)p.splits * kWaves;
+    const int64_t run = (int64_t)share * kWaves + wave;
+    const int64_t lo = items * run / runs, hi = items * (run + 1) / runs;
+    for (int64_t at = lo; at < hi;) {
+        const int slot = (int)(at / steps), s0 = (int)(at - (int64_t)slot * steps);
+        const int s1 = (int)(hi - at < steps - s0 ? s0 + (hi - at) : steps);
+        const int e = l.active[slot];
+        if (l.first[e + 1] - l.first[e] <= 16) down_rows<W, X, 1>(p, l, e, c0, s0, s1, mine);
+        else down_rows<W, X, 4>(p, l, e, c0, s0, s1, mine);
+        at += s1 - s0;
+    }
+    __syncthreads();
+    const int64_t size = (int64_t)p.N * kCols;
+    float* part = p.part + (int64_t)tile * p.splits * size;
+    for (int i = tid; i < p.N * kCols; i += kBlock) {
+        const int r = i / kCols, c = i % kCols;
+        float s = 0.f;
+#pragma unroll
+        for (int v = 0; v < kWaves; ++v) s += sums[(v * p.N + r) * kLine + c];
+        if (p.splits > 1) part[share * size + i] = s;
+        else sums[r * kLine + c] = s;  // (this thread's own)
+    }
+    if (p.splits > 1) {
+        // the last of a tile's workgroups adds the shares, in order
+        __threadfence();
+        __syncthreads();
+        if (tid == 0) s_last = atomicAdd(&p.arrived[tile], 1) == p.splits - 1;
+        __syncthreads();
+        if (!s_last) return;
+        __threadfence();
+    }
+    for (int i = tid; i < p.N * kCols; i += kBlock) {
+        const int r = i / kCols, c = i % kCols;
+        if (c0 + c >= p.Fo) continue;
+        float s = 0.f;
+        if (p.splits > 1) {
+            for (int v = 0; v < p.splits; ++v) s += part[v * size + i];
+        } else {
+            s = sums[r * kLine + c];
+        }
+        if (p.out_bf16) {
+            if (p.residual)
+                s += load_one<BF16>(static_cast<const uint16_t*>(p.residual) + r * p.ldr + c0 + c);
+            store_one<BF16>(static_cast<uint16_t*>(p.out) + (int64_t)r * p.Fo + c0 + c, s);
+        } else {
+            if (p.residual) s += static_cast<const float*>(p.residual)[r * p.ldr + c0 + c];
+            static_cast<float*>(p.out)[(int64_t)r * p.Fo + c0 + c] = s;
+        }
+    }
+}
+
+size_t list_bytes(const ExpertParams& p) {
+    return (size_t)(list_words(p.E, p.P) + 3) / 4 * 16;
+}
+
+template <typename W, typename X>
+void launch_up(const ExpertParams& p, hipStream_t s) {
+    const int tiles = (int)ceil_div(p.H, p.gated ? 16 : 32);
+    const dim3 g((unsigned)((p.E < p.P ? p.E : p.P) * tiles));
+    const size_t lds = list_bytes(p) + (size_t)kWaves * 2 * (p.N > 16 ? 4 : 1) * 4 * 64 * 4;
+    if (p.gated) hipLaunchKernelGGL((expert_up<W, X, true>), g, dim3(kBlock), lds, s, p, tiles);
+    else hipLaunchKernelGGL((expert_up<W, X, false>), g, dim3(kBlock), lds, s, p, tiles);
+}
+
+template <typename W>
+hipError_t launch(const ExpertParams& p, int rows, hipStream_t s) {
+    if (rows == kRowsMx8) launch_up<W, RowsMx8>(p, s);
+    else if (rows == kRowsBf16) launch_up<W, RowsBf16>(p, s);
+    else if (p.planes == 3) launch_up<W, RowsF32<3>>(p, s);
+    else launch_up<W, RowsF32<2>>(p, s);
+    const dim3 g((unsigned)(ceil_div(p.Fo, kCols) * p.splits));
+    const size_t lds = list_bytes(p) + (size_t)kWaves * p.N * kLine * 4;
+    if (p.planes == 3)
+        hipLaunchKernelGGL((expert_down<W, RowsOfH<3>>), g, dim3(kBlock), lds, s, p);
+    else
+        hipLaunchKernelGGL((expert_down<W, RowsOfH<2>>), g, dim3(kBlock), lds, s, p);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+// Workgroups that share the second product's work for a tile of columns.
+int expert_splits(int64_t Fo) {
+    const int64_t tiles = ceil_div(Fo, kCols);
+    int64_t n = ceil_div(512, tiles);
+    return (int)(n > 16 ? 16 : n);
+}
+
+hipError_t launch_experts(const ExpertParams& p, int rows, int mx4, hipStream_t s) {
+    return mx4 ? launch<WeightsMx4>(p, rows, s) : launch<WeightsBf16>(p, rows, s);
+}
+
+}  // namespace mp

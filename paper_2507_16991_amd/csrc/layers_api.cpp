@@ -130,6 +130,24 @@ size_t rms_bytes(int64_t N, int64_t F, int dtype) {
     return parts > 1 ? (size_t)parts * (size_t)F * 4 : 0;
 }
 
+// Workspace of the experts, in pieces that start on 256 bytes.
+struct ExpertSpace {
+    size_t h, part, arrived, bytes;
+};
+int expert_space(int64_t N, int64_t k, int64_t H, int64_t Fo, int out_dtype, ExpertSpace& m) {
+    if (!valid_dtype(out_dtype)) return MP_ERR_DTYPE;
+    if (N < 0 || N > 64 || k < 1 || k > 1024 || N * k > 1024 || H < 1 || H > kMaxF || Fo < 1 ||
+        Fo > kMaxF)
+        return MP_ERR_SIZE;
+    const size_t planes = out_dtype == MP_BF16 ? 2 : 3, tiles = (size_t)ceil_div(Fo, 32);
+    const size_t splits = (size_t)expert_splits(Fo);
+    m.h = 0;
+    m.part = align_up(planes * (size_t)(N * k) * align_up((size_t)H, 128) * 2, 256);
+    m.arrived = m.part + (splits > 1 ? align_up(tiles * splits * (size_t)N * 32 * 4, 256) : 0);
+    m.bytes = m.arrived + align_up(tiles * 4, 256);
+    return MP_OK;
+}
+
 // What both forms of the forward check and pass on.
 int rms_forward(RmsParams& P, const void* x, int dtype, int64_t N, int64_t F, int64_t ldx,
                 const void* residual, int64_t ldr, const float* weight, float eps, void* total,
@@ -567,6 +585,72 @@ int mp_rms_norm_backward(const void* total, int dtype, int64_t N, int64_t F, int
     P.dweight = dweight;
     P.part = static_cast<float*>(ws);
     return hip_status(launch_rms_backward(P, dtype, as_stream(stream)));
+}
+
+int mp_expert_mlp_workspace(int64_t N, int64_t k, int64_t H, int64_t Fo, int out_dtype,
+                            size_t* bytes) {
+    if (!bytes) return MP_ERR_NULL;
+    ExpertSpace m;
+    const int st = expert_space(N, k, H, Fo, out_dtype, m);
+    if (st != MP_OK) return st;
+    *bytes = m.bytes;
+    return MP_OK;
+}
+
+int mp_expert_mlp(const void* x, int x_dtype, const uint8_t* x_scales, int64_t N, int64_t K,
+                  int64_t ldx, const int32_t* idx, const float* weight, int64_t k, int64_t E,
+                  int64_t H, int64_t Fo, const void* w1, const uint8_t* w1_scales, const void* w2,
+                  const uint8_t* w2_scales, int act, int gated, const void* residual, int64_t ldr,
+                  void* out, int out_dtype, void* ws, size_t ws_bytes, void* stream) {
+    if (!x_scales && !valid_dtype(x_dtype)) return MP_ERR_DTYPE;
+    ExpertSpace m;
+    const int st = expert_space(N, k, H, Fo, out_dtype, m);
+    if (st != MP_OK) return st;
+    if (K < 1 || K > kMaxF || E < 1 || E > 1024 || k > E || (!x_scales && ldx < K) ||
+        (residual && ldr < Fo) || (residual && residual == out && ldr != Fo) ||
+        act < MP_ACT_NONE || act > MP_ACT_GELU)
+        return MP_ERR_SIZE;
+    if ((N > 0 && (!x || !idx || !weight || !out || !ws)) || !w1 || !w2 || !w1_scales != !w2_scales)
+        return MP_ERR_NULL;
+    const size_t xa = x_scales ? 16 : elem(x_dtype), wa = w1_scales ? 16 : 2;
+    if (!aligned(x, xa) || !aligned(idx, 4) || !aligned(weight, 4) || !aligned(w1, wa) ||
+        !aligned(w2, wa) || !aligned(residual, elem(out_dtype)) || !aligned(out, elem(out_dtype)) ||
+        !aligned(ws, 16))
+        return MP_ERR_ALIGN;
+    if (N == 0) return MP_OK;
+    if (ws_bytes < m.bytes) return MP_ERR_WORKSPACE;
+    char* w = static_cast<char*>(ws);
+    ExpertParams P{};
+    P.x = x;
+    P.x_scales = x_scales;
+    P.ldx = ldx;
+    P.N = (int)N;
+    P.k = (int)k;
+    P.P = (int)(N * k);
+    P.E = (int)E;
+    P.K = (int)K;
+    P.H = (int)H;
+    P.Fo = (int)Fo;
+    P.gated = gated != 0;
+    P.act = act;
+    P.idx = idx;
+    P.weight = weight;
+    P.w1 = w1;
+    P.w1_scales = w1_scales;
+    P.w2 = w2;
+    P.w2_scales = w2_scales;
+    P.residual = residual;
+    P.ldr = ldr;
+    P.out = out;
+    P.out_bf16 = out_dtype == MP_BF16;
+    P.splits = expert_splits(Fo);
+    P.planes = out_dtype == MP_BF16 ? 2 : 3;
+    P.h = reinterpret_cast<uint16_t*>(w + m.h);
+    P.Hp = (int)align_up((size_t)H, 128);
+    P.part = reinterpret_cast<float*>(w + m.part);
+    P.arrived = reinterpret_cast<int*>(w + m.arrived);
+    const int rows = x_scales ? kRowsMx8 : (x_dtype == MP_BF16 ? kRowsBf16 : kRowsF32);
+    return hip_status(launch_experts(P, rows, w1_scales != nullptr, as_stream(stream)));
 }
 
 }  // extern "C"

@@ -292,4 +292,32 @@ hipError_t launch_embed(const EmbedParams& p, int dtype, hipStream_t s);
 hipError_t launch_embed_keys(const EmbedParams& p, int32_t* key, int32_t* row, hipStream_t s);
 hipError_t launch_embed_backward(const EmbedParams& p, int dtype, hipStream_t s);
 
+// ---- the experts of few rows (experts.hip) ---------------------------------------------------
+struct ExpertParams {
+    const void* x;             // rows, or their 8-bit codes
+    const uint8_t* x_scales;
+    int64_t ldx;
+    int N, k, P, E, K, H, Fo;  // P = N k
+    int gated, act;
+    const int32_t* idx;        // [N, k]
+    const float* weight;       // [N, k]
+    const void* w1;            // [E, (1 + gated) H, K]: bf16, or 4-bit codes with scales
+    const uint8_t* w1_scales;
+    const void* w2;            // [E, Fo, H]
+    const uint8_t* w2_scales;
+    const void* residual;      // nullptr: none
+    int64_t ldr;
+    void* out;
+    int out_bf16;
+    int splits;                // of the second product's work
+    int planes;                // bf16 terms of an element of h
+    uint16_t* h;               // workspace [planes][P][Hp]
+    int Hp;                    // H in whole steps
+    float* part;               // workspace [column tiles][splits][N][32]
+    int* arrived;              // workspace [column tiles]
+};
+enum { kRowsF32 = 0, kRowsBf16 = 1, kRowsMx8 = 2 };
+int expert_splits(int64_t Fo);
+hipError_t launch_experts(const ExpertParams& p, int rows, int mx4, hipStream_t s);
+
 }  // namespace mp

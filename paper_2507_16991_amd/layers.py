@@ -25,7 +25,7 @@ __all__ = ["MP_ACT", "mp_group_norm_workspace", "mp_group_norm", "mp_group_norm_
            "mx_segment_matmul", "mp_embed", "mp_embed_backward_workspace", "mp_embed_backward", "embed",
            "embed_backward", "mp_rms_norm", "mp_rms_norm_mx8", "mp_rms_norm_backward_workspace",
            "mp_rms_norm_backward", "mp_mx8_dequantize", "rms_norm", "rms_norm_mx8", "rms_norm_backward",
-           "mx8_dequantize"]
+           "mx8_dequantize", "mp_expert_mlp_workspace", "mp_expert_mlp", "expert_mlp"]
 
 MP_ACT = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 
@@ -62,7 +62,10 @@ def _layers():
         L.mp_mx8_dequantize.argtypes = [p, p, i64, i64, p, i32, p]
         L.mp_rms_norm_backward_workspace.argtypes = [i64, i64, i32, psz]
         L.mp_rms_norm_backward.argtypes = [p, i32, i64, i64, i64, p, p, p, p, p, i32, p, p, sz, p]
-        for name in ("mp_embed", "mp_embed_backward_workspace", "mp_embed_backward", "mp_rms_norm",
+        L.mp_expert_mlp_workspace.argtypes = [i64, i64, i64, i64, i32, psz]
+        L.mp_expert_mlp.argtypes = [p, i32, p, i64, i64, i64, p, p, i64, i64, i64, i64, p, p, p, p, i32, i32,
+                                    p, i64, p, i32, p, sz, p]
+        for name in ("mp_expert_mlp_workspace", "mp_expert_mlp", "mp_embed", "mp_embed_backward_workspace", "mp_embed_backward", "mp_rms_norm",
                      "mp_rms_norm_mx8", "mp_mx8_dequantize", "mp_rms_norm_backward_workspace",
                      "mp_rms_norm_backward", "mp_mx_quantize", "mp_mx_dequantize", "mp_mx_segment_matmul_workspace",
                      "mp_mx_segment_matmul", "mp_group_norm_workspace", "mp_group_norm", "mp_group_norm_backward",
@@ -623,3 +626,93 @@ def rms_norm_backward(total, dout, rstd, weight=None, *, dtotal=None, dx_dtype=N
         mp_rms_norm_backward(tp, dt, N, F, ldt, dout, rstd, weight, dtotal, dx,
                              _dtype_code(dx.dtype) if want_dx else MP_F32, dw, ws, nb, stream)
     return dx, dw
+
+
+# ---- the experts of few rows ---------------------------------------------------------------------
+
+def mp_expert_mlp_workspace(N, k, H, Fo, out_dtype) -> int:
+    _layers()
+    return _bytes("mp_expert_mlp_workspace", N, k, H, Fo, out_dtype)
+
+
+def mp_expert_mlp(x, x_dtype, x_scales, N, K, ldx, idx, weight, k, E, H, Fo, w1, w1_scales, w2, w2_scales,
+                  act, gated, residual, ldr, out, out_dtype, ws, ws_bytes, stream=None):
+    """x and residual: tensors (rows may be strided) or raw addresses."""
+    xp, rp = (_rows_ptr(t)[0] if isinstance(t, torch.Tensor) else t for t in (x, residual))
+    _check("mp_expert_mlp", _layers().mp_expert_mlp(
+        xp, x_dtype, _ptr(x_scales), N, K, ldx, _ptr(idx), _ptr(weight), k, E, H, Fo, _ptr(w1),
+        _ptr(w1_scales), _ptr(w2), _ptr(w2_scales), act, gated, rp, ldr, _ptr(out), out_dtype, _ptr(ws),
+        ws_bytes, _stream(stream)))
+
+
+def _expert_weights(w, cols, name):
+    """codes (or bf16 weights) [E, rows, ...] and scales or None, for rows of `cols` values."""
+    if isinstance(w, torch.Tensor):
+        if w.dim() != 3 or w.dtype != torch.bfloat16 or w.shape[2] != cols:
+            raise ValueError(f"{name}: [E, rows, {cols}] bf16, or codes and scales of mx_quantize expected")
+        return w, None
+    codes, scales = w
+    _mx(codes, scales, cols)
+    if codes.dim() != 3:
+        raise ValueError(f"{name}: codes [E, rows, ...] expected")
+    return codes, scales
+
+
+def expert_mlp(x, idx, weight, w1, w2, *, act="silu", gated=True, residual=None, out_dtype=None, out=None,
+               stream=None):
+    """What the chosen experts make of few rows (at most 64): [N, Fo] of out_dtype,
+    out[r] = residual[r] + sum_j weight[r, j] * w2[e] h with e = idx[r, j] and h = act(w1[e] x[r]), or
+    with gated act(g) * u, where g and u are the two halves of w1[e] x[r].
+
+    x: [N, K] fp32 or bf16, or (codes, scales) of rms_norm_mx8.  idx [N, k] int32 and weight [N, k] fp32
+    are route's (idx -1: no choice).  w1 [E, (2 if gated else 1) * H, K] and w2 [E, Fo, H]: bf16 both, or
+    both as (codes, scales) of mx_quantize.  out_dtype: default x's, bf16 for rows in 8 bits.
+
+    For the many rows of a batch sort them by expert (coo_to_csr) and take mx_segment_matmul."""
+    a = _act(act)
+    if isinstance(x, torch.Tensor):
+        xs, K, dt = None, int(x.shape[1]), _dtype_code(x.dtype)
+        N = int(x.shape[0])
+        default = x.dtype
+    else:
+        x, xs = x
+        _mx8(x, xs, x.shape[1])
+        N, K, dt, default = int(x.shape[0]), int(x.shape[1]), MP_F32, torch.bfloat16
+    if xs is not None:
+        # blocks are whole: places past K hold zeros
+        K = int(w1.shape[2]) if isinstance(w1, torch.Tensor) else K
+        if _blocks(K) != xs.shape[1]:
+            raise ValueError("rows in 8 bits must have the blocks of w1's columns")
+    if isinstance(w1, torch.Tensor) != isinstance(w2, torch.Tensor):
+        raise ValueError("w1 and w2 must both be bf16 or both in 4 bits")
+    c1, s1 = _expert_weights(w1, K, "w1")
+    E, rows = int(c1.shape[0]), int(c1.shape[1])
+    if gated and rows % 2:
+        raise ValueError("w1 of gated experts has 2 H rows")
+    H = rows // 2 if gated else rows
+    c2, s2 = _expert_weights(w2, H, "w2")
+    Fo = int(c2.shape[1])
+    if int(c2.shape[0]) != E:
+        raise ValueError("w1 and w2 must be of as many experts")
+    if idx.dim() != 2 or int(idx.shape[0]) != N:
+        raise ValueError("idx [N, k] expected")
+    k = int(idx.shape[1])
+    _vector(idx, N * k, torch.int32, "idx")
+    _vector(weight, N * k, torch.float32, "weight")
+    if out is not None and tuple(out.shape) != (N, Fo):
+        raise ValueError("out must be [N, Fo]")
+    kind = out.dtype if out is not None else out_dtype or default
+    if residual is not None and (tuple(residual.shape) != (N, Fo) or residual.dtype != kind):
+        raise ValueError("residual must have the shape and dtype of out")
+    _on_gpu(x, xs, idx, weight, c1, s1, c2, s2, residual, out)
+    xp, ldx = _rows_ptr(x) if xs is None else (_ptr(x), K)
+    rp, ldr = _rows_ptr(residual) if residual is not None else (None, Fo)
+    od = _dtype_code(kind)
+    nb = _sized(mp_expert_mlp_workspace, N, k, H, Fo, od)
+    with _on(stream):
+        if out is None:
+            out = torch.empty(N, Fo, dtype=kind, device=x.device)
+        ws = _workspace(nb, x.device)
+        mp_expert_mlp(xp, dt, xs, N, K, ldx, idx, weight, k, E, H, Fo, c1, s1, c2, s2, a, int(bool(gated)), rp,
+                      ldr, out, od, ws, nb, stream)
+    return out
