@@ -323,7 +323,7 @@ int mp_rms_norm_backward(const void* total, int dtype, int64_t N, int64_t F, int
  * Sizes: 0 <= N <= 64, 1 <= k <= E <= 1024, N * k <= 1024, 1 <= K, H, Fo <= 65536.
  * ws 16-byte aligned; calls that may overlap need one each.
  * ------------------------------------------------------------------------- */
-int mp_expert_mlp_workspace(int64_t N, int64_t k, int64_t H, int64_t Fo, int out_dtype,
+int mp_expert_mlp_workspace(int64_t N, int64_t k, int64_t E, int64_t H, int64_t Fo, int out_dtype,
                             size_t* bytes);
 
 int mp_expert_mlp(const void* x, int x_dtype, const uint8_t* x_scales, int64_t N, int64_t K,

@@ -26,6 +26,7 @@ constexpr int kBlock = 256;
 constexpr int kWaves = kBlock / kWave;
 constexpr int kStep = 128;    // elements of K of a step, 32 for a quarter of the lanes
 constexpr int kCols = 32;     // weight rows of a workgroup
+constexpr int64_t kUpGrid = 1024;  // workgroups of the first launch, at most
 constexpr int kLine = 36;     // floats of a row's sums in LDS
 
 // 2^(s - 127) (s = 0 is subnormal); NaN for 255.
@@ -43,8 +44,10 @@ struct Lists {
     int* chosen;     // [P] expert of a pair, or -1
     int* pairs;      // [P] by expert
     int* total;      // [1] how many are active
+    float* given;    // [P] the choices' weights
+    float* weight;   // [P] a pair's: that of its choice and of later ones of its expert
 };
-__host__ __device__ inline int list_words(int E, int P) { return 3 * E + 2 * P + 2; }
+__host__ __device__ inline int list_words(int E, int P) { return 3 * E + 4 * P + 2; }
 
 __device__ inline Lists carve(int* lds, int E, int P) {
     Lists l;
@@ -54,6 +57,8 @@ __device__ inline Lists carve(int* lds, int E, int P) {
     l.chosen = l.active + E;
     l.pairs = l.chosen + P;
     l.total = l.pairs + P;
+    l.given = reinterpret_cast<float*>(l.total + 1);
+    l.weight = l.given + P;
     return l;
 }
 
@@ -62,14 +67,18 @@ __device__ inline void find_rows(const ExpertParams& p, const Lists& l) {
     for (int i = tid; i < p.P; i += kBlock) {
         const int e = p.idx[i];
         l.chosen[i] = e >= 0 && e < p.E ? e : -1;
+        l.given[i] = p.weight[i];
     }
     for (int e = tid; e < p.E; e += kBlock) l.cursor[e] = 0;
     __syncthreads();
     for (int i = tid; i < p.P; i += kBlock) {
-        const int e = l.chosen[i];
+        const int e = l.chosen[i], r0 = i - i % p.k;
         bool again = e < 0;
-        for (int j = i - i % p.k; j < i; ++j) again |= l.chosen[j] == e;
+        float weight = l.given[i];
+        for (int j = r0; j < i; ++j) again |= l.chosen[j] == e;
+        for (int j = i + 1; j < r0 + p.k; ++j) weight += l.chosen[j] == e ? l.given[j] : 0.f;
         l.pairs[i] = again ? -1 : e;
+        l.weight[i] = weight;
     }
     __syncthreads();
     for (int i = tid; i < p.P; i += kBlock) {
@@ -109,58 +118,43 @@ __device__ inline void find_rows(const ExpertParams& p, const Lists& l) {
     __syncthreads();
 }
 
+// Words of the lists that the second launch takes over.
+__host__ __device__ inline int kept_words(int E, int P) { return 2 * E + P + 2; }
+
+__device__ inline void keep_rows(const ExpertParams& p, const Lists& l) {
+    const int tid = threadIdx.x;
+    int* to = p.lists;
+    for (int e = tid; e <= p.E; e += kBlock) to[e] = l.first[e];
+    for (int a = tid; a < *l.total; a += kBlock) to[p.E + 1 + a] = l.active[a];
+    for (int i = tid; i < l.first[p.E]; i += kBlock) to[2 * p.E + 1 + i] = l.pairs[i];
+    if (tid == 0) to[2 * p.E + 1 + p.P] = *l.total;
+}
+
+// The kept lists in LDS: first, active, pairs and total, in this order.
+__device__ inline Lists take_rows(const ExpertParams& p, int* lds) {
+    for (int i = threadIdx.x; i < kept_words(p.E, p.P); i += kBlock) lds[i] = p.lists[i];
+    Lists l = {};
+    l.first = lds;
+    l.active = lds + p.E + 1;
+    l.pairs = l.active + p.E;
+    l.total = l.pairs + p.P;
+    return l;
+}
+
 // ---- operands ------------------------------------------------------------------------
 // A step's 128 elements of K lie on four quarters of the lanes; quarter q has, in its
 // i-th of four products, the elements at(i, q) .. + 7.  Any order will do that both
 // operands share: 4-bit weights take a whole block to a lane (16 bytes), bf16 ones
 // go through memory by whole lines.
-struct WeightsMx4 {
-    static constexpr int kSteps = 4;  // steps whose loads are under way
-    struct Raw {
-        uint32_t c[4];
-        uint32_t s;
-    };
-    struct Row {
-        const uint8_t* codes;
-        const uint8_t* scales;
-    };
-    __device__ static int at(int i, int q) { return 32 * q + 8 * i; }
-    __device__ static Row row(const void* w, const uint8_t* scales, int64_t r, int K) {
-        const int64_t KB = (K + 31) / 32;
-        return Row{static_cast<const uint8_t*>(w) + r * KB * 16, scales + r * KB};
-    }
-    __device__ static Raw load(const Row& w, int s, int q, int K) {
-        const int KB = (K + 31) / 32, b = 4 * s + q;
-        Raw r = {};
-        if (b < KB) {
-            __builtin_memcpy(r.c, w.codes + (int64_t)b * 16, 16);
-            if (4 * s + 4 <= KB) {
-                __builtin_memcpy(&r.s, w.scales + 4 * s, 4);
-                r.s = (r.s >> (8 * q)) & 255;
-            } else {
-                r.s = w.scales[b];
-            }
-        }
-        return r;
-    }
-    __device__ static void unpack(const Raw& r, bf16x8 (&v)[4]) {
-        const float f = scale_value(r.s);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            bf16x2 t[4];
-            t[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.c[i], f, 0);
-            t[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.c[i], f, 1);
-            t[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.c[i], f, 2);
-            t[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.c[i], f, 3);
-            __builtin_memcpy(&v[i], t, 16);
-        }
-    }
-};
+// FULL: the step ends within K.  Only such loads are many at a time, without branches
+// and without a use of what they load: a branch around a load, or a shift of a scale
+// in it, made each wait for the one before (70 us against 30 for 56 experts of 16 rows).
 
 // Eight bf16 elements k .. k+7 of a row of K, zero past its end.
+template <bool FULL>
 __device__ inline bf16x8 load_bf16(const uint16_t* p, int k, int K) {
     uint16_t u[8] = {};
-    if (k + 8 <= K) {
+    if (FULL || k + 8 <= K) {
         __builtin_memcpy(u, p + k, 16);
     } else {
 #pragma unroll
@@ -172,25 +166,76 @@ __device__ inline bf16x8 load_bf16(const uint16_t* p, int k, int K) {
     return v;
 }
 
+struct WeightsMx4 {
+    static constexpr int kSteps = 4;  // steps whose loads are under way
+    template <int U>
+    struct Raw {
+        uint32_t c[U][4];
+        uint32_t s[U];  // the scales of each step's blocks
+    };
+    struct Row {
+        const uint8_t* codes;
+        const uint8_t* scales;
+    };
+    __device__ static int at(int i, int q) { return 32 * q + 8 * i; }
+    __device__ static Row row(const void* w, const uint8_t* scales, int64_t r, int K) {
+        const int64_t KB = (K + 31) / 32;
+        return Row{static_cast<const uint8_t*>(w) + r * KB * 16, scales + r * KB};
+    }
+    // (the scales of U steps are one load: as many requests as rows)
+    template <int U, bool FULL>
+    __device__ static void load(Raw<U>& r, const Row& w, int s, int q, int K) {
+        const int KB = (K + 31) / 32, b = 4 * s + q;
+        if (FULL) {
+            __builtin_memcpy(r.s, w.scales + 4 * s, 4 * U);
+#pragma unroll
+            for (int u = 0; u < U; ++u) __builtin_memcpy(r.c[u], w.codes + (b + 4 * u) * 16, 16);
+        } else {
+            r = Raw<U>{};
+            if (b < KB) {
+                __builtin_memcpy(r.c[0], w.codes + b * 16, 16);
+                r.s[0] = (uint32_t)w.scales[b] << (8 * q);
+            }
+        }
+    }
+    template <int U>
+    __device__ static void unpack(const Raw<U>& r, int u, int q, bf16x8 (&v)[4]) {
+        const float f = scale_value((r.s[u] >> (8 * q)) & 255);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            bf16x2 t[4];
+            t[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.c[u][i], f, 0);
+            t[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.c[u][i], f, 1);
+            t[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.c[u][i], f, 2);
+            t[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.c[u][i], f, 3);
+            __builtin_memcpy(&v[i], t, 16);
+        }
+    }
+};
+
 struct WeightsBf16 {
     static constexpr int kSteps = 2;
+    template <int U>
     struct Raw {
-        bf16x8 v[4];
+        bf16x8 v[U][4];
     };
     typedef const uint16_t* Row;
     __device__ static int at(int i, int q) { return 32 * i + 8 * q; }
     __device__ static Row row(const void* w, const uint8_t*, int64_t r, int K) {
         return static_cast<const uint16_t*>(w) + r * K;
     }
-    __device__ static Raw load(const Row& w, int s, int q, int K) {
-        Raw r;
+    template <int U, bool FULL>
+    __device__ static void load(Raw<U>& r, const Row& w, int s, int q, int K) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r.v[i] = load_bf16(w, kStep * s + at(i, q), K);
-        return r;
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                r.v[u][i] = load_bf16<FULL>(w, kStep * (s + u) + at(i, q), K);
     }
-    __device__ static void unpack(const Raw& r, bf16x8 (&v)[4]) {
+    template <int U>
+    __device__ static void unpack(const Raw<U>& r, int u, int, bf16x8 (&v)[4]) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = r.v[i];
+        for (int i = 0; i < 4; ++i) v[i] = r.v[u][i];
     }
 };
 
@@ -217,34 +262,38 @@ __device__ inline void split(float x, uint16_t (&t)[T]) {
 template <int TERMS>
 struct RowsF32 {
     static constexpr int kTerms = TERMS;
+    template <int U>
     struct Raw {
-        float v[4][8];
+        float v[U][4][8];
     };
     typedef const float* Row;
     __device__ static Row row(const ExpertParams& p, int r) {
         return static_cast<const float*>(p.x) + r * p.ldx;
     }
-    template <typename W>
-    __device__ static void load(Raw& r, const ExpertParams&, Row x, int s, int q, int K) {
+    template <typename W, int U, bool FULL>
+    __device__ static void load(Raw<U>& r, const ExpertParams&, Row x, int s, int q, int K) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int k = kStep * s + W::at(i, q);
-            if (k + 8 <= K) {
-                __builtin_memcpy(r.v[i], x + k, 32);
-            } else {
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) r.v[i][j] = k + j < K ? x[k + j] : 0.f;
+            for (int i = 0; i < 4; ++i) {
+                const int k = kStep * (s + u) + W::at(i, q);
+                if (FULL) {
+                    __builtin_memcpy(r.v[u][i], x + k, 32);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) r.v[u][i][j] = k + j < K ? x[k + j] : 0.f;
+                }
             }
-        }
     }
-    __device__ static void unpack(const Raw& r, int i, bf16x8 (&v)[TERMS]) {
+    template <typename W, int U>
+    __device__ static void unpack(const Raw<U>& r, int u, int i, int, bf16x8 (&v)[TERMS]) {
         uint16_t t[TERMS][8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            uint16_t u[TERMS];
-            split<TERMS>(r.v[i][j], u);
+            uint16_t w[TERMS];
+            split<TERMS>(r.v[u][i][j], w);
 #pragma unroll
-            for (int m = 0; m < TERMS; ++m) t[m][j] = u[m];
+            for (int m = 0; m < TERMS; ++m) t[m][j] = w[m];
         }
 #pragma unroll
         for (int m = 0; m < TERMS; ++m) __builtin_memcpy(&v[m], t[m], 16);
@@ -253,26 +302,34 @@ struct RowsF32 {
 
 struct RowsBf16 {
     static constexpr int kTerms = 1;
+    template <int U>
     struct Raw {
-        bf16x8 v[4];
+        bf16x8 v[U][4];
     };
     typedef const uint16_t* Row;
     __device__ static Row row(const ExpertParams& p, int r) {
         return static_cast<const uint16_t*>(p.x) + r * p.ldx;
     }
-    template <typename W>
-    __device__ static void load(Raw& r, const ExpertParams&, Row x, int s, int q, int K) {
+    template <typename W, int U, bool FULL>
+    __device__ static void load(Raw<U>& r, const ExpertParams&, Row x, int s, int q, int K) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r.v[i] = load_bf16(x, kStep * s + W::at(i, q), K);
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                r.v[u][i] = load_bf16<FULL>(x, kStep * (s + u) + W::at(i, q), K);
     }
-    __device__ static void unpack(const Raw& r, int i, bf16x8 (&v)[1]) { v[0] = r.v[i]; }
+    template <typename W, int U>
+    __device__ static void unpack(const Raw<U>& r, int u, int i, int, bf16x8 (&v)[1]) {
+        v[0] = r.v[u][i];
+    }
 };
 
 struct RowsMx8 {
     static constexpr int kTerms = 1;
+    template <int U>
     struct Raw {
-        uint32_t c[4][2];
-        uint32_t s[4];
+        uint32_t c[U][4][2];
+        uint32_t s[U];  // the scales of each step's blocks
     };
     struct Row {
         const uint8_t* codes;
@@ -282,26 +339,31 @@ struct RowsMx8 {
         const int64_t KB = (p.K + 31) / 32;
         return Row{static_cast<const uint8_t*>(p.x) + r * KB * 32, p.x_scales + r * KB};
     }
-    template <typename W>
-    __device__ static void load(Raw& r, const ExpertParams&, const Row& x, int s, int q, int K) {
+    template <typename W, int U, bool FULL>
+    __device__ static void load(Raw<U>& r, const ExpertParams&, const Row& x, int s, int q, int K) {
         const int KB = (K + 31) / 32;
+        if (FULL) __builtin_memcpy(r.s, x.scales + 4 * s, 4 * U);
+        else r = Raw<U>{};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int k = kStep * s + W::at(i, q), b = k / 32;
-            r.c[i][0] = r.c[i][1] = r.s[i] = 0;
-            if (b < KB) {
-                __builtin_memcpy(r.c[i], x.codes + k, 8);
-                r.s[i] = x.scales[b];
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int k = kStep * (s + u) + W::at(i, q);
+                if (FULL || k / 32 < KB) __builtin_memcpy(r.c[u][i], x.codes + k, 8);
             }
+        if (!FULL) {
+            for (int i = 0; i < 4; ++i)
+                if (4 * s + i < KB) r.s[0] |= (uint32_t)x.scales[4 * s + i] << (8 * i);
         }
     }
-    __device__ static void unpack(const Raw& r, int i, bf16x8 (&v)[1]) {
-        const float f = scale_value(r.s[i]);
+    template <typename W, int U>
+    __device__ static void unpack(const Raw<U>& r, int u, int i, int q, bf16x8 (&v)[1]) {
+        const float f = scale_value((r.s[u] >> (W::at(i, q) / 32 * 8)) & 255);
         bf16x2 t[4];
-        t[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.c[i][0], f, false);
-        t[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.c[i][0], f, true);
-        t[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.c[i][1], f, false);
-        t[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.c[i][1], f, true);
+        t[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.c[u][i][0], f, false);
+        t[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.c[u][i][0], f, true);
+        t[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.c[u][i][1], f, false);
+        t[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.c[u][i][1], f, true);
         __builtin_memcpy(&v[0], t, 16);
     }
 };
@@ -310,77 +372,76 @@ struct RowsMx8 {
 template <int TERMS>
 struct RowsOfH {
     static constexpr int kTerms = TERMS;
+    template <int U>
     struct Raw {
-        bf16x8 v[TERMS][4];
+        bf16x8 v[U][TERMS][4];
     };
     typedef const uint16_t* Row;
-    template <typename W>
-    __device__ static void load(Raw& r, const ExpertParams& p, Row x, int s, int q, int) {
+    template <typename W, int U, bool FULL>
+    __device__ static void load(Raw<U>& r, const ExpertParams& p, Row x, int s, int q, int) {
 #pragma unroll
-        for (int m = 0; m < TERMS; ++m)
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                __builtin_memcpy(&r.v[m][i],
-                                 x + (int64_t)m * p.P * p.Hp + kStep * s + W::at(i, q), 16);
+            for (int m = 0; m < TERMS; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    __builtin_memcpy(&r.v[u][m][i],
+                                     x + (int64_t)m * p.P * p.Hp + kStep * (s + u) + W::at(i, q),
+                                     16);
     }
-    __device__ static void unpack(const Raw& r, int i, bf16x8 (&v)[TERMS]) {
+    template <typename W, int U>
+    __device__ static void unpack(const Raw<U>& r, int u, int i, int, bf16x8 (&v)[TERMS]) {
 #pragma unroll
-        for (int m = 0; m < TERMS; ++m) v[m] = r.v[m][i];
+        for (int m = 0; m < TERMS; ++m) v[m] = r.v[u][m][i];
     }
 };
 
 // acc[t][m] += weight rows w[t] (this lane's of each 16) times rows x[m] (this lane's
-// of each 16; `has` where there is one), steps s0, s0 + by, ... below s1.  K: of the
-// weights, KX: of the rows.
+// of each 16): U steps from s on.
+template <typename W, typename X, int M, int U, bool FULL>
+__device__ inline void multiply_steps(const ExpertParams& p, const typename W::Row (&w)[2],
+                                      const typename X::Row (&x)[M], int K, int s,
+                                      f32x4 (&acc)[2][M]) {
+    const int q = (threadIdx.x & 63) >> 4;
+    typename W::template Raw<U> rw[2];
+    typename X::template Raw<U> rx[M];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) W::template load<U, FULL>(rw[t], w[t], s, q, K);
+#pragma unroll
+    for (int m = 0; m < M; ++m) X::template load<W, U, FULL>(rx[m], p, x[m], s, q, K);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        bf16x8 a[2][4];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) W::template unpack<U>(rw[t], u, q, a[t]);
+#pragma unroll
+        for (int m = 0; m < M; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                bf16x8 b[X::kTerms];
+                X::template unpack<W, U>(rx[m], u, i, q, b);
+#pragma unroll
+                for (int c = X::kTerms - 1; c >= 0; --c)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+                        acc[t][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[t][i], b[c], acc[t][m],
+                                                                            0, 0, 0);
+            }
+    }
+}
+
+// Steps s .. s1-1 of K elements.
 template <typename W, typename X, int M>
 __device__ inline void multiply(const ExpertParams& p, const typename W::Row (&w)[2],
-                                const typename X::Row (&x)[M], const bool (&has)[M], int K, int KX,
-                                int s0, int s1, int by, f32x4 (&acc)[2][M]) {
-    // as many steps' loads under way as registers allow: rows of fp32 or of many
-    // are taken one step at a time
-    constexpr int U = M > 1 ? 1 : (sizeof(typename X::Raw) > 64 && W::kSteps > 2 ? 2 : W::kSteps);
-    const int q = (threadIdx.x & 63) >> 4;
-    for (int s = s0; s < s1; s += U * by) {
-        typename W::Raw rw[U][2];
-        typename X::Raw rx[U][M];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int at = s + u * by;
-            if (at < s1) {
-#pragma unroll
-                for (int t = 0; t < 2; ++t) rw[u][t] = W::load(w[t], at, q, K);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int at = s + u * by;
-#pragma unroll
-            for (int m = 0; m < M; ++m) {
-                rx[u][m] = typename X::Raw{};
-                if (at < s1 && has[m]) X::template load<W>(rx[u][m], p, x[m], at, q, KX);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (s + u * by >= s1) break;
-            bf16x8 a[2][4];
-            W::unpack(rw[u][0], a[0]);
-            W::unpack(rw[u][1], a[1]);
-#pragma unroll
-            for (int m = 0; m < M; ++m)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    bf16x8 b[X::kTerms];
-                    X::unpack(rx[u][m], i, b);
-#pragma unroll
-                    for (int c = X::kTerms - 1; c >= 0; --c)
-#pragma unroll
-                        for (int t = 0; t < 2; ++t)
-                            acc[t][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[t][i], b[c],
-                                                                                acc[t][m], 0, 0, 0);
-                }
-        }
-    }
+                                const typename X::Row (&x)[M], int K, int s, int s1,
+                                f32x4 (&acc)[2][M]) {
+    // as many steps' loads under way as registers allow
+    constexpr int U =
+        sizeof(typename X::template Raw<1>) * M > 128 ? W::kSteps / 2 : W::kSteps;
+    const int full = K / kStep < s1 ? K / kStep : s1;
+    for (; s + U <= full; s += U) multiply_steps<W, X, M, U, true>(p, w, x, K, s, acc);
+    for (; s < full; ++s) multiply_steps<W, X, M, 1, true>(p, w, x, K, s, acc);
+    if (s < s1) multiply_steps<W, X, M, 1, false>(p, w, x, K, s, acc);
 }
 
 // ---- up ---------------------------------------------------------------------------------
@@ -391,9 +452,9 @@ __device__ inline float activate(float z, int act) {
     return z;
 }
 
-// The pairs of expert e, at most 16 M of them, and the weight rows of a tile.
+// The pairs n0 .. n0 + 16 M - 1 of expert e and the weight rows of a tile.
 template <typename W, typename X, bool GATED, int M>
-__device__ inline void up_rows(const ExpertParams& p, const Lists& l, int e, int tile,
+__device__ inline void up_rows(const ExpertParams& p, const Lists& l, int e, int tile, int n0,
                                float* sums) {
     constexpr int COLS = GATED ? 16 : 32;  // columns of h
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -407,15 +468,14 @@ __device__ inline void up_rows(const ExpertParams& p, const Lists& l, int e, int
         w[t] = W::row(p.w1, p.w1_scales, e * rows + (GATED ? t * (int64_t)p.H : 0) + c, p.K);
     }
     typename X::Row x[M];
-    bool has[M];
 #pragma unroll
-    for (int m = 0; m < M; ++m) {
-        const int at = 16 * m + (lane & 15);
-        has[m] = at < n;
-        x[m] = X::row(p, has[m] ? l.pairs[begin + at] / p.k : 0);
+    for (int m = 0; m < M; ++m) {  // (lanes without a pair take the first one again)
+        const int at = n0 + 16 * m + (lane & 15);
+        x[m] = X::row(p, l.pairs[begin + (at < n ? at : n0)] / p.k);
     }
     f32x4 acc[2][M] = {};
-    multiply<W, X, M>(p, w, x, has, p.K, p.K, wave, (p.K + kStep - 1) / kStep, kWaves, acc);
+    const int steps = (p.K + kStep - 1) / kStep;
+    multiply<W, X, M>(p, w, x, p.K, steps * wave / kWaves, steps * (wave + 1) / kWaves, acc);
 
     // the wavefronts' sums: [wave][t][m][i][lane]
     __syncthreads();
@@ -430,18 +490,15 @@ __device__ inline void up_rows(const ExpertParams& p, const Lists& l, int e, int
     const int i = threadIdx.x >> 6;
 #pragma unroll
     for (int m = 0; m < M; ++m) {
-        const int at = 16 * m + (lane & 15);
+        const int at = n0 + 16 * m + (lane & 15);
         if (at >= n) continue;
-        const int pair = l.pairs[begin + at], j0 = pair % p.k, r0 = pair - j0;
+        const int pair = l.pairs[begin + at];
         float z[2] = {0.f, 0.f};
 #pragma unroll
         for (int t = 0; t < 2; ++t)
             for (int v = 0; v < kWaves; ++v)
                 z[t] += sums[((((v * 2 + t) * M + m) * 4 + i) << 6) + lane];
-        // the weight of this choice, and of later ones of the same expert
-        float weight = p.weight[pair];
-        for (int j = j0 + 1; j < p.k; ++j)
-            if (p.idx[r0 + j] == e) weight += p.weight[r0 + j];
+        const float weight = l.weight[pair];
         const int c = 4 * (lane >> 4) + i;
 #pragma unroll
         for (int t = 0; t < (GATED ? 1 : 2); ++t) {
@@ -466,34 +523,41 @@ __device__ inline void up_rows(const ExpertParams& p, const Lists& l, int e, int
     }
 }
 
-template <typename W, typename X, bool GATED>
+// M: products of 16 rows side by side (1 where there are no more rows).  Workgroups
+// go through the (expert, tile) items by the grid, so that finding the rows is paid
+// once by each.
+template <typename W, typename X, bool GATED, int M>
 __global__ __launch_bounds__(kBlock) void expert_up(ExpertParams p, int tiles) {
     extern __shared__ int lds[];
     const Lists l = carve(lds, p.E, p.P);
     float* sums = reinterpret_cast<float*>(lds + (list_words(p.E, p.P) + 3) / 4 * 4);
-    if (p.splits > 1 && blockIdx.x == 0)  // (for the second launch)
-        for (int c = threadIdx.x; c < (p.Fo + kCols - 1) / kCols; c += kBlock) p.arrived[c] = 0;
     find_rows(p, l);
-    const int slot = blockIdx.x / tiles, tile = blockIdx.x - slot * tiles;
-    if (slot >= *l.total) return;
-    const int e = l.active[slot], n = l.first[e + 1] - l.first[e];
-    if (n <= 16) {
-        up_rows<W, X, GATED, 1>(p, l, e, tile, sums);
-    } else {
-        up_rows<W, X, GATED, 4>(p, l, e, tile, sums);  // (no more than 64 rows)
+    if (blockIdx.x == 0) {  // (for the second launch)
+        keep_rows(p, l);
+        for (int c = threadIdx.x; c < (p.Fo + kCols - 1) / kCols; c += kBlock) p.arrived[c] = 0;
     }
-    if (tile == tiles - 1) {  // zeros fill the last step of the rows of h
-        const int more = p.Hp - p.H;
-        for (int i = threadIdx.x; i < n * more; i += kBlock)
-            for (int v = 0; v < p.planes; ++v)
-                p.h[((int64_t)v * p.P + l.pairs[l.first[e] + i / more]) * p.Hp + p.H + i % more] = 0;
+    const int items = *l.total * tiles;
+    for (int item = blockIdx.x; item < items; item += gridDim.x) {
+        const int slot = item / tiles, tile = item - slot * tiles;
+        const int e = l.active[slot], n = l.first[e + 1] - l.first[e];
+        // (the weights of more than 16 M rows are read again, from the caches)
+        int n0 = 0;
+        for (; n0 + 16 * (M - 1) < n; n0 += 16 * M) up_rows<W, X, GATED, M>(p, l, e, tile, n0, sums);
+        if (M > 1 && n0 < n) up_rows<W, X, GATED, 1>(p, l, e, tile, n0, sums);
+        if (tile == tiles - 1) {  // zeros fill the last step of the rows of h
+            const int more = p.Hp - p.H;
+            for (int i = threadIdx.x; i < n * more; i += kBlock)
+                for (int v = 0; v < p.planes; ++v)
+                    p.h[((int64_t)v * p.P + l.pairs[l.first[e] + i / more]) * p.Hp + p.H +
+                        i % more] = 0;
+        }
     }
 }
 
 // ---- down -----------------------------------------------------------------------------
-// The sums of this wavefront for the pairs of expert e, steps s0 .. s1-1.
+// The sums of this wavefront for the pairs n0 .. of expert e, steps s0 .. s1-1.
 template <typename W, typename X, int M>
-__device__ inline void down_rows(const ExpertParams& p, const Lists& l, int e, int c0, int s0,
+__device__ inline void down_rows(const ExpertParams& p, const Lists& l, int e, int n0, int c0, int s0,
                                  int s1, float* mine) {
     const int lane = threadIdx.x & 63;
     const int begin = l.first[e], n = l.first[e + 1] - begin;
@@ -509,14 +573,14 @@ __device__ inline void down_rows(const ExpertParams& p, const Lists& l, int e, i
     int row[M];
 #pragma unroll
     for (int m = 0; m < M; ++m) {
-        const int at = 16 * m + (lane & 15);
-        has[m] = at < n;
-        const int pair = has[m] ? l.pairs[begin + at] : 0;
+        const int at = n0 + 16 * m + (lane & 15);
+        has[m] = at < n;  // (others take the first one again)
+        const int pair = l.pairs[begin + (has[m] ? at : n0)];
         x[m] = p.h + (int64_t)pair * p.Hp;
         row[m] = pair / p.k;
     }
     f32x4 acc[2][M] = {};
-    multiply<W, X, M>(p, w, x, has, p.H, p.Hp, s0, s1, 1, acc);
+    multiply<W, X, M>(p, w, x, p.H, s0, s1, acc);
 #pragma unroll
     for (int m = 0; m < M; ++m) {
         if (!has[m]) continue;
@@ -528,17 +592,17 @@ __device__ inline void down_rows(const ExpertParams& p, const Lists& l, int e, i
     }
 }
 
-template <typename W, typename X>
+template <typename W, typename X, int M>
 __global__ __launch_bounds__(kBlock) void expert_down(ExpertParams p) {
     extern __shared__ int lds[];
     __shared__ int s_last;
-    const Lists l = carve(lds, p.E, p.P);
-    float* sums = reinterpret_cast<float*>(lds + (list_words(p.E, p.P) + 3) / 4 * 4);
+    const Lists l = take_rows(p, lds);
+    float* sums = reinterpret_cast<float*>(lds + (kept_words(p.E, p.P) + 3) / 4 * 4);
     const int tid = threadIdx.x, wave = tid >> 6;
     const int tile = blockIdx.x / p.splits, share = blockIdx.x - tile * p.splits, c0 = tile * kCols;
     float* mine = sums + wave * p.N * kLine;
     for (int i = tid; i < kWaves * p.N * kLine; i += kBlock) sums[i] = 0.f;
-    find_rows(p, l);
+    __syncthreads();
     const int steps = p.Hp / kStep;
     const int64_t items = (int64_t)*l.total * steps, runs = (int64_t)p.splits * kWaves;
     const int64_t run = (int64_t)share * kWaves + wave;
@@ -547,8 +611,10 @@ __global__ __launch_bounds__(kBlock) void expert_down(ExpertParams p) {
         const int slot = (int)(at / steps), s0 = (int)(at - (int64_t)slot * steps);
         const int s1 = (int)(hi - at < steps - s0 ? s0 + (hi - at) : steps);
         const int e = l.active[slot];
-        if (l.first[e + 1] - l.first[e] <= 16) down_rows<W, X, 1>(p, l, e, c0, s0, s1, mine);
-        else down_rows<W, X, 4>(p, l, e, c0, s0, s1, mine);
+        const int n = l.first[e + 1] - l.first[e];
+        int n0 = 0;
+        for (; n0 + 16 * (M - 1) < n; n0 += 16 * M) down_rows<W, X, M>(p, l, e, n0, c0, s0, s1, mine);
+        if (M > 1 && n0 < n) down_rows<W, X, 1>(p, l, e, n0, c0, s0, s1, mine);
         at += s1 - s0;
     }
     __syncthreads();
@@ -559,24 +625,33 @@ __global__ __launch_bounds__(kBlock) void expert_down(ExpertParams p) {
         float s = 0.f;
 #pragma unroll
         for (int v = 0; v < kWaves; ++v) s += sums[(v * p.N + r) * kLine + c];
-        if (p.splits > 1) part[share * size + i] = s;
+        if (p.splits > 1)
+            __hip_atomic_store(&part[share * size + i], s, __ATOMIC_RELAXED,
+                               __HIP_MEMORY_SCOPE_AGENT);
         else sums[r * kLine + c] = s;  // (this thread's own)
     }
     if (p.splits > 1) {
-        // the last of a tile's workgroups adds the shares, in order
-        __threadfence();
+        // The last of a tile's workgroups adds the shares, in order.  They are stored and
+        // loaded by agent-scope atomics, that is in memory that all XCDs see alike, and
+        // every thread waits for its stores before the workgroup is counted: so no
+        // fence has to write back and drop the L2 (with __threadfence on both sides
+        // this launch took 45 us for one row, now 7).
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        if (tid == 0) s_last = atomicAdd(&p.arrived[tile], 1) == p.splits - 1;
+        if (tid == 0)
+            s_last = __hip_atomic_fetch_add(&p.arrived[tile], 1, __ATOMIC_RELAXED,
+                                            __HIP_MEMORY_SCOPE_AGENT) == p.splits - 1;
         __syncthreads();
         if (!s_last) return;
-        __threadfence();
     }
     for (int i = tid; i < p.N * kCols; i += kBlock) {
         const int r = i / kCols, c = i % kCols;
         if (c0 + c >= p.Fo) continue;
         float s = 0.f;
         if (p.splits > 1) {
-            for (int v = 0; v < p.splits; ++v) s += part[v * size + i];
+            for (int v = 0; v < p.splits; ++v)
+                s += __hip_atomic_load(&part[v * size + i], __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_AGENT);
         } else {
             s = sums[r * kLine + c];
         }
@@ -591,31 +666,30 @@ __global__ __launch_bounds__(kBlock) void expert_down(ExpertParams p) {
     }
 }
 
-size_t list_bytes(const ExpertParams& p) {
-    return (size_t)(list_words(p.E, p.P) + 3) / 4 * 16;
-}
+size_t in_16(int words) { return (size_t)(words + 3) / 4 * 16; }
 
-template <typename W, typename X>
+template <typename W, typename X, int M>
 void launch_up(const ExpertParams& p, hipStream_t s) {
     const int tiles = (int)ceil_div(p.H, p.gated ? 16 : 32);
-    const dim3 g((unsigned)((p.E < p.P ? p.E : p.P) * tiles));
-    const size_t lds = list_bytes(p) + (size_t)kWaves * 2 * (p.N > 16 ? 4 : 1) * 4 * 64 * 4;
-    if (p.gated) hipLaunchKernelGGL((expert_up<W, X, true>), g, dim3(kBlock), lds, s, p, tiles);
-    else hipLaunchKernelGGL((expert_up<W, X, false>), g, dim3(kBlock), lds, s, p, tiles);
+    const int64_t items = (int64_t)(p.E < p.P ? p.E : p.P) * tiles;
+    const dim3 g((unsigned)(items < kUpGrid ? items : kUpGrid));
+    const size_t lds = in_16(list_words(p.E, p.P)) + (size_t)kWaves * 2 * M * 4 * 64 * 4;
+    if (p.gated) hipLaunchKernelGGL((expert_up<W, X, true, M>), g, dim3(kBlock), lds, s, p, tiles);
+    else hipLaunchKernelGGL((expert_up<W, X, false, M>), g, dim3(kBlock), lds, s, p, tiles);
 }
 
-template <typename W>
+template <typename W, int M>
 hipError_t launch(const ExpertParams& p, int rows, hipStream_t s) {
-    if (rows == kRowsMx8) launch_up<W, RowsMx8>(p, s);
-    else if (rows == kRowsBf16) launch_up<W, RowsBf16>(p, s);
-    else if (p.planes == 3) launch_up<W, RowsF32<3>>(p, s);
-    else launch_up<W, RowsF32<2>>(p, s);
+    if (rows == kRowsMx8) launch_up<W, RowsMx8, M>(p, s);
+    else if (rows == kRowsBf16) launch_up<W, RowsBf16, M>(p, s);
+    else if (p.planes == 3) launch_up<W, RowsF32<3>, M>(p, s);
+    else launch_up<W, RowsF32<2>, M>(p, s);
     const dim3 g((unsigned)(ceil_div(p.Fo, kCols) * p.splits));
-    const size_t lds = list_bytes(p) + (size_t)kWaves * p.N * kLine * 4;
+    const size_t lds = in_16(kept_words(p.E, p.P)) + (size_t)kWaves * p.N * kLine * 4;
     if (p.planes == 3)
-        hipLaunchKernelGGL((expert_down<W, RowsOfH<3>>), g, dim3(kBlock), lds, s, p);
+        hipLaunchKernelGGL((expert_down<W, RowsOfH<3>, M>), g, dim3(kBlock), lds, s, p);
     else
-        hipLaunchKernelGGL((expert_down<W, RowsOfH<2>>), g, dim3(kBlock), lds, s, p);
+        hipLaunchKernelGGL((expert_down<W, RowsOfH<2>, M>), g, dim3(kBlock), lds, s, p);
     return hipGetLastError();
 }
 
@@ -629,7 +703,10 @@ int expert_splits(int64_t Fo) {
 }
 
 hipError_t launch_experts(const ExpertParams& p, int rows, int mx4, hipStream_t s) {
-    return mx4 ? launch<WeightsMx4>(p, rows, s) : launch<WeightsBf16>(p, rows, s);
+    if (mx4) return p.N > 16 ? launch<WeightsMx4, 2>(p, rows, s) : launch<WeightsMx4, 1>(p, rows, s);
+    return p.N > 16 ? launch<WeightsBf16, 2>(p, rows, s) : launch<WeightsBf16, 1>(p, rows, s);
 }
+
+size_t expert_list_bytes(int64_t E, int64_t P) { return (size_t)kept_words((int)E, (int)P) * 4; }
 
 }  // namespace mp

@@ -132,11 +132,11 @@ size_t rms_bytes(int64_t N, int64_t F, int dtype) {
 
 // Workspace of the experts, in pieces that start on 256 bytes.
 struct ExpertSpace {
-    size_t h, part, arrived, bytes;
+    size_t h, part, arrived, lists, bytes;
 };
-int expert_space(int64_t N, int64_t k, int64_t H, int64_t Fo, int out_dtype, ExpertSpace& m) {
+int expert_space(int64_t N, int64_t k, int64_t E, int64_t H, int64_t Fo, int out_dtype, ExpertSpace& m) {
     if (!valid_dtype(out_dtype)) return MP_ERR_DTYPE;
-    if (N < 0 || N > 64 || k < 1 || k > 1024 || N * k > 1024 || H < 1 || H > kMaxF || Fo < 1 ||
+    if (N < 0 || N > 64 || k < 1 || k > E || E > 1024 || N * k > 1024 || H < 1 || H > kMaxF || Fo < 1 ||
         Fo > kMaxF)
         return MP_ERR_SIZE;
     const size_t planes = out_dtype == MP_BF16 ? 2 : 3, tiles = (size_t)ceil_div(Fo, 32);
@@ -144,7 +144,8 @@ int expert_space(int64_t N, int64_t k, int64_t H, int64_t Fo, int out_dtype, Exp
     m.h = 0;
     m.part = align_up(planes * (size_t)(N * k) * align_up((size_t)H, 128) * 2, 256);
     m.arrived = m.part + (splits > 1 ? align_up(tiles * splits * (size_t)N * 32 * 4, 256) : 0);
-    m.bytes = m.arrived + align_up(tiles * 4, 256);
+    m.lists = m.arrived + align_up(tiles * 4, 256);
+    m.bytes = m.lists + align_up(expert_list_bytes(E, N * k), 256);
     return MP_OK;
 }
 
@@ -587,11 +588,11 @@ int mp_rms_norm_backward(const void* total, int dtype, int64_t N, int64_t F, int
     return hip_status(launch_rms_backward(P, dtype, as_stream(stream)));
 }
 
-int mp_expert_mlp_workspace(int64_t N, int64_t k, int64_t H, int64_t Fo, int out_dtype,
+int mp_expert_mlp_workspace(int64_t N, int64_t k, int64_t E, int64_t H, int64_t Fo, int out_dtype,
                             size_t* bytes) {
     if (!bytes) return MP_ERR_NULL;
     ExpertSpace m;
-    const int st = expert_space(N, k, H, Fo, out_dtype, m);
+    const int st = expert_space(N, k, E, H, Fo, out_dtype, m);
     if (st != MP_OK) return st;
     *bytes = m.bytes;
     return MP_OK;
@@ -604,9 +605,9 @@ int mp_expert_mlp(const void* x, int x_dtype, const uint8_t* x_scales, int64_t N
                   void* out, int out_dtype, void* ws, size_t ws_bytes, void* stream) {
     if (!x_scales && !valid_dtype(x_dtype)) return MP_ERR_DTYPE;
     ExpertSpace m;
-    const int st = expert_space(N, k, H, Fo, out_dtype, m);
+    const int st = expert_space(N, k, E, H, Fo, out_dtype, m);
     if (st != MP_OK) return st;
-    if (K < 1 || K > kMaxF || E < 1 || E > 1024 || k > E || (!x_scales && ldx < K) ||
+    if (K < 1 || K > kMaxF || (!x_scales && ldx < K) ||
         (residual && ldr < Fo) || (residual && residual == out && ldr != Fo) ||
         act < MP_ACT_NONE || act > MP_ACT_GELU)
         return MP_ERR_SIZE;
@@ -649,6 +650,7 @@ int mp_expert_mlp(const void* x, int x_dtype, const uint8_t* x_scales, int64_t N
     P.Hp = (int)align_up((size_t)H, 128);
     P.part = reinterpret_cast<float*>(w + m.part);
     P.arrived = reinterpret_cast<int*>(w + m.arrived);
+    P.lists = reinterpret_cast<int*>(w + m.lists);
     const int rows = x_scales ? kRowsMx8 : (x_dtype == MP_BF16 ? kRowsBf16 : kRowsF32);
     return hip_status(launch_experts(P, rows, w1_scales != nullptr, as_stream(stream)));
 }

@@ -315,9 +315,11 @@ struct ExpertParams {
     int Hp;                    // H in whole steps
     float* part;               // workspace [column tiles][splits][N][32]
     int* arrived;              // workspace [column tiles]
+    int* lists;                // workspace: which rows chose which experts
 };
 enum { kRowsF32 = 0, kRowsBf16 = 1, kRowsMx8 = 2 };
 int expert_splits(int64_t Fo);
+size_t expert_list_bytes(int64_t E, int64_t P);
 hipError_t launch_experts(const ExpertParams& p, int rows, int mx4, hipStream_t s);
 
 }  // namespace mp

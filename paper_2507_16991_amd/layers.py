@@ -62,7 +62,7 @@ def _layers():
         L.mp_mx8_dequantize.argtypes = [p, p, i64, i64, p, i32, p]
         L.mp_rms_norm_backward_workspace.argtypes = [i64, i64, i32, psz]
         L.mp_rms_norm_backward.argtypes = [p, i32, i64, i64, i64, p, p, p, p, p, i32, p, p, sz, p]
-        L.mp_expert_mlp_workspace.argtypes = [i64, i64, i64, i64, i32, psz]
+        L.mp_expert_mlp_workspace.argtypes = [i64, i64, i64, i64, i64, i32, psz]
         L.mp_expert_mlp.argtypes = [p, i32, p, i64, i64, i64, p, p, i64, i64, i64, i64, p, p, p, p, i32, i32,
                                     p, i64, p, i32, p, sz, p]
         for name in ("mp_expert_mlp_workspace", "mp_expert_mlp", "mp_embed", "mp_embed_backward_workspace", "mp_embed_backward", "mp_rms_norm",
@@ -90,8 +90,13 @@ def _on(stream):
 
 def _on_gpu(*tensors):
     """Kernels run on the current GPU: an operand elsewhere is refused."""
+    here = None
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != torch.cuda.current_device()):
+        if t is None:
+            continue
+        if here is None and t.is_cuda:
+            here = torch.cuda.current_device()
+        if not t.is_cuda or t.get_device() != here:
             raise ValueError(f"operands must be on the current GPU, got one on {t.device}")
 
 
@@ -630,9 +635,9 @@ def rms_norm_backward(total, dout, rstd, weight=None, *, dtotal=None, dx_dtype=N
 
 # ---- the experts of few rows ---------------------------------------------------------------------
 
-def mp_expert_mlp_workspace(N, k, H, Fo, out_dtype) -> int:
+def mp_expert_mlp_workspace(N, k, E, H, Fo, out_dtype) -> int:
     _layers()
-    return _bytes("mp_expert_mlp_workspace", N, k, H, Fo, out_dtype)
+    return _bytes("mp_expert_mlp_workspace", N, k, E, H, Fo, out_dtype)
 
 
 def mp_expert_mlp(x, x_dtype, x_scales, N, K, ldx, idx, weight, k, E, H, Fo, w1, w1_scales, w2, w2_scales,
@@ -708,7 +713,7 @@ def expert_mlp(x, idx, weight, w1, w2, *, act="silu", gated=True, residual=None,
     xp, ldx = _rows_ptr(x) if xs is None else (_ptr(x), K)
     rp, ldr = _rows_ptr(residual) if residual is not None else (None, Fo)
     od = _dtype_code(kind)
-    nb = _sized(mp_expert_mlp_workspace, N, k, H, Fo, od)
+    nb = _sized(mp_expert_mlp_workspace, N, k, E, H, Fo, od)
     with _on(stream):
         if out is None:
             out = torch.empty(N, Fo, dtype=kind, device=x.device)
