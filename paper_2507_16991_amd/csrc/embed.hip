@@ -11,11 +11,14 @@
 // so that a chunk has parts of two such ids at most.
 #include "layers_internal.hpp"
 
+#ifndef MP_ROWS
+#define MP_ROWS 4
+#endif
 namespace mp {
 namespace {
 
 constexpr int kBlock = 256;
-constexpr int kRows = 4;  // rows of a thread, forward
+constexpr int kRows = MP_ROWS;  // rows of a thread
 constexpr int64_t kMaxGrid = int64_t(1) << 22;  // (a launch has fewer than 2^32 threads)
 
 __device__ inline int64_t id_at(const EmbedParams& P, int64_t r) {
@@ -118,6 +121,50 @@ __device__ inline void add_rows(const EmbedParams& P, int64_t b, int64_t e, int 
     }
 }
 
+// Rows v0, v0 + slots ... of the gradient, kRows of them, but for ids of more than C
+// positions.  Most ids have few: the offsets, the first row's number and the first
+// row of all of them go out together.
+template <typename T, int V>
+__device__ inline void sum_rows(const EmbedParams& P, int64_t v0, int first, int per, int slots,
+                                int64_t C, bool failed) {
+    const int F = (int)P.F;
+    int32_t b[kRows], e[kRows], r[kRows];
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+        const int64_t v = v0 + (int64_t)u * slots;
+        const bool on = v < P.V && !failed;
+        b[u] = on ? P.rowptr[v] : 0;
+        e[u] = on ? P.rowptr[v + 1] : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) r[u] = b[u] < e[u] ? P.row[b[u]] : -1;
+    for (int j = first; j < per; j += kBlock) {
+        const int c = chunk_at<V>(j, F);
+        float acc[kRows][V];
+#pragma unroll
+        for (int u = 0; u < kRows; ++u) {
+            if (r[u] >= 0) {
+                load_floats<T, V>(static_cast<const typename T::raw*>(P.in) + r[u] * P.ld + c,
+                                  acc[u]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[u][i] = 0.f;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kRows; ++u) {
+            const int64_t v = v0 + (int64_t)u * slots;
+            if (v >= P.V) break;
+            if (e[u] - b[u] > C) continue;
+            if (e[u] - b[u] > 1) add_rows<T, V>(P, b[u] + 1, e[u], 1, c, acc[u]);
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                acc[u][i] = failed ? __builtin_nanf("") : acc[u][i] * P.scale;
+            store_as<V>(P.out, P.out_bf16, v * P.F + c, acc[u]);
+        }
+    }
+}
+
 // acc of a workgroup's slots added in order, the result in slot 0.
 template <int V>
 __device__ inline void add_slots(float (&acc)[V], int per, int slots, int slot, float* lds) {
@@ -146,20 +193,10 @@ __global__ __launch_bounds__(kBlock) void embed_grad(EmbedParams P, int per, int
     const bool failed = *P.status != MP_OK;  // (then rowptr is not written)
     if ((int64_t)blockIdx.x >= chunks) {
         if (slot >= slots) return;
-        const int64_t step = (gridDim.x - chunks) * slots;
-        for (int64_t v = ((int64_t)blockIdx.x - chunks) * slots + slot; v < P.V; v += step) {
-            const int64_t b = failed ? 0 : P.rowptr[v], e = failed ? 0 : P.rowptr[v + 1];
-            if (e - b > C) continue;
-            for (int j = first; j < per; j += kBlock) {
-                const int c = chunk_at<V>(j, F);
-                float acc[V] = {};
-                add_rows<T, V>(P, b, e, 1, c, acc);
-#pragma unroll
-                for (int i = 0; i < V; ++i)
-                    acc[i] = failed ? __builtin_nanf("") : acc[i] * P.scale;
-                store_as<V>(P.out, P.out_bf16, v * P.F + c, acc);
-            }
-        }
+        const int64_t step = (gridDim.x - chunks) * slots * kRows;
+        for (int64_t v0 = ((int64_t)blockIdx.x - chunks) * slots * kRows + slot; v0 < P.V;
+             v0 += step)
+            sum_rows<T, V>(P, v0, first, per, slots, C, failed);
         return;
     }
     if (failed) return;
@@ -222,13 +259,14 @@ __global__ __launch_bounds__(kBlock) void embed_join(EmbedParams P, int per, int
 
 int64_t at_most(int64_t blocks) { return blocks < kMaxGrid ? blocks : kMaxGrid; }
 
-// Elements of a chunk, chunks of a row and rows side by side in a workgroup.
+// Elements of a chunk, chunks of a row and rows side by side in a workgroup.  bf16
+// rows of a multiple of 4 but not of 8 are taken 4 at a time: 
 struct EmbedShape {
     int V, per, slots;
 };
 EmbedShape embed_shape(int64_t F, int dtype) {
     EmbedShape h;
-    h.V = dtype == MP_BF16 ? 8 : 4;
+    h.V = dtype == MP_BF16 && (F % 8 == 0 || F % 4 != 0) ? 8 : 4;
     if (F < h.V) h.V = 1;
     h.per = (int)ceil_div(F, h.V);
     h.slots = h.per < kBlock ? kBlock / h.per : 1;
@@ -244,7 +282,7 @@ void launch_rows(const EmbedParams& p, const EmbedShape& h, hipStream_t s) {
 template <typename T, int V>
 void launch_grad(const EmbedParams& p, const EmbedShape& h, hipStream_t s) {
     const int64_t C = embed_chunk(p.N), chunks = p.N > C ? ceil_div(p.N, C) : 0;
-    hipLaunchKernelGGL((embed_grad<T, V>), dim3((unsigned)(chunks + at_most(ceil_div(p.V, h.slots)))),
+    hipLaunchKernelGGL((embed_grad<T, V>), dim3((unsigned)(chunks + at_most(ceil_div(p.V, h.slots * kRows)))),
                        dim3(kBlock), 0, s, p, h.per, h.slots, C, chunks);
     if (chunks)
         hipLaunchKernelGGL((embed_join<V>), dim3((unsigned)chunks), dim3(kBlock), 0, s, p, h.per,
@@ -267,8 +305,9 @@ hipError_t launch_embed(const EmbedParams& p, int dtype, hipStream_t s) {
         if (dtype == MP_BF16) launch_rows<BF16, 1>(p, h, s);
         else launch_rows<F32, 1>(p, h, s);
     } else {
-        if (dtype == MP_BF16) launch_rows<BF16, 8>(p, h, s);
-        else launch_rows<F32, 4>(p, h, s);
+        if (dtype == MP_F32) launch_rows<F32, 4>(p, h, s);
+        else if (h.V == 8) launch_rows<BF16, 8>(p, h, s);
+        else launch_rows<BF16, 4>(p, h, s);
     }
     return hipGetLastError();
 }
@@ -286,8 +325,9 @@ hipError_t launch_embed_backward(const EmbedParams& p, int dtype, hipStream_t s)
         if (dtype == MP_BF16) launch_grad<BF16, 1>(p, h, s);
         else launch_grad<F32, 1>(p, h, s);
     } else {
-        if (dtype == MP_BF16) launch_grad<BF16, 8>(p, h, s);
-        else launch_grad<F32, 4>(p, h, s);
+        if (dtype == MP_F32) launch_grad<F32, 4>(p, h, s);
+        else if (h.V == 8) launch_grad<BF16, 8>(p, h, s);
+        else launch_grad<BF16, 4>(p, h, s);
     }
     return hipGetLastError();
 }

@@ -13,7 +13,8 @@
 // Products run on v_mfma_f32_16x16x32_bf16, weights first, so that a lane's
 // accumulators are neighbouring columns of one row.  4-bit weights are exact in
 // bf16, and so are 8-bit rows; fp32 values are taken as sums of bf16 terms, three
-// of which are exact (two, off by 2^-16, where the result is bf16).
+// of which are exact (two, off by 2^-16, where the result is bf16).  8-bit rows
+// times 4-bit weights are v_mfma_scale_f32_16x16x128_f8f6f4's, as they are.
 #include "layers_internal.hpp"
 
 namespace mp {
@@ -21,10 +22,12 @@ namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kBlock = 256;
 constexpr int kWaves = kBlock / kWave;
 constexpr int kStep = 128;    // elements of K of a step, 32 for a quarter of the lanes
+constexpr int kE4M3 = 0, kE2M1 = 4;  // operand formats of the scaled products
 constexpr int kCols = 32;     // weight rows of a workgroup
 constexpr int64_t kUpGrid = 1024;  // workgroups of the first launch, at most
 constexpr int kLine = 36;     // floats of a row's sums in LDS
@@ -131,8 +134,9 @@ __device__ inline void keep_rows(const ExpertParams& p, const Lists& l) {
 }
 
 // The kept lists in LDS: first, active, pairs and total, in this order.
+template <int BLOCK>
 __device__ inline Lists take_rows(const ExpertParams& p, int* lds) {
-    for (int i = threadIdx.x; i < kept_words(p.E, p.P); i += kBlock) lds[i] = p.lists[i];
+    for (int i = threadIdx.x; i < kept_words(p.E, p.P); i += BLOCK) lds[i] = p.lists[i];
     Lists l = {};
     l.first = lds;
     l.active = lds + p.E + 1;
@@ -167,7 +171,7 @@ __device__ inline bf16x8 load_bf16(const uint16_t* p, int k, int K) {
 }
 
 struct WeightsMx4 {
-    static constexpr int kSteps = 4;  // steps whose loads are under way
+    static constexpr bool kMx4 = true;
     template <int U>
     struct Raw {
         uint32_t c[U][4];
@@ -214,7 +218,7 @@ struct WeightsMx4 {
 };
 
 struct WeightsBf16 {
-    static constexpr int kSteps = 2;
+    static constexpr bool kMx4 = false;
     template <int U>
     struct Raw {
         bf16x8 v[U][4];
@@ -262,6 +266,8 @@ __device__ inline void split(float x, uint16_t (&t)[T]) {
 template <int TERMS>
 struct RowsF32 {
     static constexpr int kTerms = TERMS;
+    template <typename W>
+    static constexpr bool kScaled = false;
     template <int U>
     struct Raw {
         float v[U][4][8];
@@ -302,6 +308,8 @@ struct RowsF32 {
 
 struct RowsBf16 {
     static constexpr int kTerms = 1;
+    template <typename W>
+    static constexpr bool kScaled = false;
     template <int U>
     struct Raw {
         bf16x8 v[U][4];
@@ -326,6 +334,9 @@ struct RowsBf16 {
 
 struct RowsMx8 {
     static constexpr int kTerms = 1;
+    // Whether products with these weights take codes and scales as they are.
+    template <typename W>
+    static constexpr bool kScaled = W::kMx4;
     template <int U>
     struct Raw {
         uint32_t c[U][4][2];
@@ -346,10 +357,19 @@ struct RowsMx8 {
         else r = Raw<U>{};
 #pragma unroll
         for (int u = 0; u < U; ++u)
+            if constexpr (kScaled<W>) {
+                // 8-bit codes k = 16 q .. + 15 and 64 + 16 q .. + 15
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int k = kStep * (s + u) + W::at(i, q);
-                if (FULL || k / 32 < KB) __builtin_memcpy(r.c[u][i], x.codes + k, 8);
+                for (int i = 0; i < 4; i += 2) {
+                    const int k = kStep * (s + u) + 32 * i + 16 * q;
+                    if (FULL || k / 32 < KB) __builtin_memcpy(r.c[u][i], x.codes + k, 16);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int k = kStep * (s + u) + W::at(i, q);
+                    if (FULL || k / 32 < KB) __builtin_memcpy(r.c[u][i], x.codes + k, 8);
+                }
             }
         if (!FULL) {
             for (int i = 0; i < 4; ++i)
@@ -372,6 +392,8 @@ struct RowsMx8 {
 template <int TERMS>
 struct RowsOfH {
     static constexpr int kTerms = TERMS;
+    template <typename W>
+    static constexpr bool kScaled = false;
     template <int U>
     struct Raw {
         bf16x8 v[U][TERMS][4];
@@ -396,6 +418,14 @@ struct RowsOfH {
     }
 };
 
+// Steps whose loads are under way together: as many as about 104 registers hold.
+template <typename W, typename X, int M>
+constexpr int steps_at_once() {
+    constexpr int bytes = (int)(2 * sizeof(typename W::template Raw<1>) +
+                                M * sizeof(typename X::template Raw<1>));
+    return 4 * bytes <= 416 ? 4 : (2 * bytes <= 416 ? 2 : 1);
+}
+
 // acc[t][m] += weight rows w[t] (this lane's of each 16) times rows x[m] (this lane's
 // of each 16): U steps from s on.
 template <typename W, typename X, int M, int U, bool FULL>
@@ -409,6 +439,24 @@ __device__ inline void multiply_steps(const ExpertParams& p, const typename W::R
     for (int t = 0; t < 2; ++t) W::template load<U, FULL>(rw[t], w[t], s, q, K);
 #pragma unroll
     for (int m = 0; m < M; ++m) X::template load<W, U, FULL>(rx[m], p, x[m], s, q, K);
+    __builtin_amdgcn_sched_barrier(0);  // (the compiler would spread them to save registers)
+    if constexpr (X::template kScaled<W>) {
+        // lane quarter q has the scales of block q
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int m = 0; m < M; ++m)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const uint32_t* c = rw[t].c[u];
+                    i32x8 a = {(int)c[0], (int)c[1], (int)c[2], (int)c[3], 0, 0, 0, 0}, b;
+                    __builtin_memcpy(&b, rx[m].c[u], 32);
+                    acc[t][m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                        a, b, acc[t][m], kE2M1, kE4M3, 0, (int)(rw[t].s[u] >> (8 * q)), 0,
+                        (int)(rx[m].s[u] >> (8 * q)));
+                }
+        return;
+    }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         bf16x8 a[2][4];
@@ -435,12 +483,16 @@ template <typename W, typename X, int M>
 __device__ inline void multiply(const ExpertParams& p, const typename W::Row (&w)[2],
                                 const typename X::Row (&x)[M], int K, int s, int s1,
                                 f32x4 (&acc)[2][M]) {
-    // as many steps' loads under way as registers allow
-    constexpr int U =
-        sizeof(typename X::template Raw<1>) * M > 128 ? W::kSteps / 2 : W::kSteps;
+    constexpr int U = steps_at_once<W, X, M>();
     const int full = K / kStep < s1 ? K / kStep : s1;
     for (; s + U <= full; s += U) multiply_steps<W, X, M, U, true>(p, w, x, K, s, acc);
-    for (; s < full; ++s) multiply_steps<W, X, M, 1, true>(p, w, x, K, s, acc);
+    if constexpr (U > 2) {
+        if (s + 2 <= full) {
+            multiply_steps<W, X, M, 2, true>(p, w, x, K, s, acc);
+            s += 2;
+        }
+    }
+    if (U > 1 && s < full) multiply_steps<W, X, M, 1, true>(p, w, x, K, s++, acc);
     if (s < s1) multiply_steps<W, X, M, 1, false>(p, w, x, K, s, acc);
 }
 
@@ -592,39 +644,42 @@ __device__ inline void down_rows(const ExpertParams& p, const Lists& l, int e, i
     }
 }
 
-template <typename W, typename X, int M>
-__global__ __launch_bounds__(kBlock) void expert_down(ExpertParams p) {
+template <typename W, typename X, int M, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void expert_down(ExpertParams p) {
+    constexpr int BLOCK = WAVES * 64;
     extern __shared__ int lds[];
     __shared__ int s_last;
-    const Lists l = take_rows(p, lds);
+    const Lists l = take_rows<BLOCK>(p, lds);
     float* sums = reinterpret_cast<float*>(lds + (kept_words(p.E, p.P) + 3) / 4 * 4);
     const int tid = threadIdx.x, wave = tid >> 6;
     const int tile = blockIdx.x / p.splits, share = blockIdx.x - tile * p.splits, c0 = tile * kCols;
     float* mine = sums + wave * p.N * kLine;
-    for (int i = tid; i < kWaves * p.N * kLine; i += kBlock) sums[i] = 0.f;
+    for (int i = tid; i < WAVES * p.N * kLine; i += BLOCK) sums[i] = 0.f;
     __syncthreads();
-    const int steps = p.Hp / kStep;
-    const int64_t items = (int64_t)*l.total * steps, runs = (int64_t)p.splits * kWaves;
-    const int64_t run = (int64_t)share * kWaves + wave;
-    const int64_t lo = items * run / runs, hi = items * (run + 1) / runs;
-    for (int64_t at = lo; at < hi;) {
-        const int slot = (int)(at / steps), s0 = (int)(at - (int64_t)slot * steps);
-        const int s1 = (int)(hi - at < steps - s0 ? s0 + (hi - at) : steps);
+    // items: an expert and as many steps as are loaded at once
+    constexpr int U = steps_at_once<W, X, M>();
+    const int steps = p.Hp / kStep, per = (steps + U - 1) / U;
+    const int items = *l.total * per, runs = p.splits * WAVES, run = share * WAVES + wave;
+    const int hi = (int)((int64_t)items * (run + 1) / runs);
+    for (int at = (int)((int64_t)items * run / runs); at < hi;) {
+        const int slot = at / per, i0 = at - slot * per;
+        const int i1 = hi - at < per - i0 ? i0 + (hi - at) : per;
+        const int s0 = i0 * U, s1 = i1 * U < steps ? i1 * U : steps;
         const int e = l.active[slot];
         const int n = l.first[e + 1] - l.first[e];
         int n0 = 0;
         for (; n0 + 16 * (M - 1) < n; n0 += 16 * M) down_rows<W, X, M>(p, l, e, n0, c0, s0, s1, mine);
         if (M > 1 && n0 < n) down_rows<W, X, 1>(p, l, e, n0, c0, s0, s1, mine);
-        at += s1 - s0;
+        at += i1 - i0;
     }
     __syncthreads();
     const int64_t size = (int64_t)p.N * kCols;
     float* part = p.part + (int64_t)tile * p.splits * size;
-    for (int i = tid; i < p.N * kCols; i += kBlock) {
+    for (int i = tid; i < p.N * kCols; i += BLOCK) {
         const int r = i / kCols, c = i % kCols;
         float s = 0.f;
 #pragma unroll
-        for (int v = 0; v < kWaves; ++v) s += sums[(v * p.N + r) * kLine + c];
+        for (int v = 0; v < WAVES; ++v) s += sums[(v * p.N + r) * kLine + c];
         if (p.splits > 1)
             __hip_atomic_store(&part[share * size + i], s, __ATOMIC_RELAXED,
                                __HIP_MEMORY_SCOPE_AGENT);
@@ -644,7 +699,7 @@ __global__ __launch_bounds__(kBlock) void expert_down(ExpertParams p) {
         __syncthreads();
         if (!s_last) return;
     }
-    for (int i = tid; i < p.N * kCols; i += kBlock) {
+    for (int i = tid; i < p.N * kCols; i += BLOCK) {
         const int r = i / kCols, c = i % kCols;
         if (c0 + c >= p.Fo) continue;
         float s = 0.f;
@@ -685,11 +740,12 @@ hipError_t launch(const ExpertParams& p, int rows, hipStream_t s) {
     else if (p.planes == 3) launch_up<W, RowsF32<3>, M>(p, s);
     else launch_up<W, RowsF32<2>, M>(p, s);
     const dim3 g((unsigned)(ceil_div(p.Fo, kCols) * p.splits));
-    const size_t lds = in_16(kept_words(p.E, p.P)) + (size_t)kWaves * p.N * kLine * 4;
+    constexpr int D = M == 1 ? 8 : 4;  // wavefronts of a workgroup: their sums fit into LDS
+    const size_t lds = in_16(kept_words(p.E, p.P)) + (size_t)D * p.N * kLine * 4;
     if (p.planes == 3)
-        hipLaunchKernelGGL((expert_down<W, RowsOfH<3>, M>), g, dim3(kBlock), lds, s, p);
+        hipLaunchKernelGGL((expert_down<W, RowsOfH<3>, M, D>), g, dim3(D * 64), lds, s, p);
     else
-        hipLaunchKernelGGL((expert_down<W, RowsOfH<2>, M>), g, dim3(kBlock), lds, s, p);
+        hipLaunchKernelGGL((expert_down<W, RowsOfH<2>, M, D>), g, dim3(D * 64), lds, s, p);
     return hipGetLastError();
 }
 
@@ -698,7 +754,7 @@ hipError_t launch(const ExpertParams& p, int rows, hipStream_t s) {
 // Workgroups that share the second product's work for a tile of columns.
 int expert_splits(int64_t Fo) {
     const int64_t tiles = ceil_div(Fo, kCols);
-    int64_t n = ceil_div(512, tiles);
+    int64_t n = ceil_div(256, tiles);
     return (int)(n > 16 ? 16 : n);
 }
 
