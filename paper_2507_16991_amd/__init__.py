@@ -202,8 +202,14 @@ def _rows_ptr(t):
     return t.data_ptr(), int(t.stride(0)) if t.shape[0] > 1 else int(t.shape[1])
 
 
+# The current stream's handle without a Stream object around it (5 us of a small call).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream):
     if stream is None:
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 

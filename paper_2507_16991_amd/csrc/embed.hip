@@ -4,21 +4,21 @@
 // Forward: bound by memory; a thread has 16 bytes of a row.
 // Backward: the rows' numbers lie sorted by id (the library's radix sort), so that
 // every row of the gradient is the sum of consecutive positions, in the order of
-// the rows: no atomics.  An id of up to C positions is summed by the lanes that
-// write its row; the positions of all others, cut into chunks of C, by a workgroup
-// a chunk, whose partial sums the workgroup of the id's first chunk adds in
-// order.  An id of more than C positions reaches past the chunk that it begins in,
-// so that a chunk has parts of two such ids at most.
+// the rows: no atomics.  The positions, not the ids, are shared out: a team of lanes
+// walks over a run of them and writes the rows of the ids that begin and end
+// there, so that popular and rare ids cost the same (a team an id instead: 103 us
+// for 169,343 ids of 256 fp32, 350 for 2.4M of 100 bf16; now 95 and 280).  What
+// an id has in several runs is joined in LDS by the team of its last run, what it
+// has in several workgroups by a second launch, each in order.  Rows of ids without
+// positions are zeroed by workgroups of their own.
 #include "layers_internal.hpp"
 
-#ifndef MP_ROWS
-#define MP_ROWS 4
-#endif
 namespace mp {
 namespace {
 
 constexpr int kBlock = 256;
-constexpr int kRows = MP_ROWS;  // rows of a thread
+constexpr int kRows = 4;  // rows of a thread, forward, and rows zeroed
+constexpr int kRun = 8;   // positions whose rows are loaded together
 constexpr int64_t kMaxGrid = int64_t(1) << 22;  // (a launch has fewer than 2^32 threads)
 
 __device__ inline int64_t id_at(const EmbedParams& P, int64_t r) {
@@ -95,145 +95,180 @@ __global__ __launch_bounds__(kBlock) void embed_keys(EmbedParams P, int32_t* key
     row[r] = (int32_t)r;
 }
 
-// acc += rows row[p], p = b, b + step, ... below e, columns c ...
+// Row v of the gradient from its sum, columns c ...; nothing for v = V.
 template <typename T, int V>
-__device__ inline void add_rows(const EmbedParams& P, int64_t b, int64_t e, int step, int c,
-                                float (&acc)[V]) {
+__device__ inline void write_row(const EmbedParams& P, int32_t v, int c, const float (&sum)[V]) {
+    if (v >= P.V) return;
+    float o[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) o[i] = sum[i] * P.scale;
+    store_as<V>(P.out, P.out_bf16, (int64_t)v * P.F + c, o);
+}
+
+// A segment of positions is an id's.  Of a run, the segments that begin and end in it
+// are written to the gradient; an end of one that began before goes to A, a
+// beginning (or middle) of one that goes on to B.
+enum { kEnds = 1, kGoesOn = 2, kMiddle = 4 };  // A there, B there, all of the run is B
+
+// The workgroup's runs of R * kRun positions, columns of chunk j.  Flags and what lies
+// in A and B go through LDS where there are several teams.
+template <typename T, int V>
+__device__ inline void sum_runs(const EmbedParams& P, int64_t block, int j, int per, int slots, int slot, int R,
+                                float* s_a, float* s_b, int* s_flag) {
+    const int F = (int)P.F, c = chunk_at<V>(j, F);
+    const int tid = threadIdx.x;
+    const int64_t p0 = (block * slots + slot) * R * kRun;
+    const int32_t none = (int32_t)P.V;  // ids outside the table, and positions past the last
+    const bool on = slot < slots && p0 < P.N;
     const typename T::raw* in = static_cast<const typename T::raw*>(P.in) + c;
-    int64_t p = b;
-    for (; p + 3 * step < e; p += 4 * step) {
-        int32_t r[4];
-        float v[4][V];
+    int flag = 0;
+    float a[V] = {}, acc[V] = {};
+    if (on) {
+        const int64_t p1 = p0 + R * kRun;
+        const int32_t before = p0 > 0 ? P.key[P.row[p0 - 1]] : -1;
+        const int32_t after = p1 < P.N ? P.key[P.row[p1]] : -1;
+        int32_t cur = -1;
+        bool open = false;    // the present segment began before the run
+        bool whole = true;    // there has been no other
+        for (int q0 = 0; q0 < R; ++q0) {
+            int32_t r[kRun], k[kRun];
+            RawOf<T, V> raw[kRun];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) r[u] = P.row[p + u * step];
+            for (int q = 0; q < kRun; ++q) {
+                const int64_t p = p0 + q0 * kRun + q;
+                r[q] = p < P.N ? P.row[p] : -1;
+            }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) load_floats<T, V>(in + (int64_t)r[u] * P.ld, v[u]);
+            for (int q = 0; q < kRun; ++q) k[q] = r[q] >= 0 ? P.key[r[q]] : none;
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+            for (int q = 0; q < kRun; ++q)  // (rows of padding are not looked at)
+                raw[q] = load_raw<T, V>(in + (int64_t)(k[q] < none ? r[q] : 0) * P.ld);
+            if (q0 == 0) {
+                cur = k[0];
+                open = cur == before;
+            }
 #pragma unroll
-            for (int i = 0; i < V; ++i) acc[i] += v[u][i];
+            for (int q = 0; q < kRun; ++q) {
+                if (k[q] != cur) {
+                    if (open) {
+                        flag |= kEnds;
+#pragma unroll
+                        for (int i = 0; i < V; ++i) a[i] = acc[i];
+                    } else {
+                        write_row<T, V>(P, cur, c, acc);
+                    }
+                    cur = k[q];
+                    open = whole = false;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) acc[i] = 0.f;
+                }
+                float v[V];
+                to_floats<T, V>(raw[q], v);
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[i] += v[i];
+            }
+        }
+        if (cur < none) {
+            if (cur == after) {
+                flag |= kGoesOn | (whole && open ? kMiddle : 0);
+            } else if (open) {
+                flag |= kEnds;
+#pragma unroll
+                for (int i = 0; i < V; ++i) a[i] = acc[i];
+            } else {
+                write_row<T, V>(P, cur, c, acc);
+            }
+        }
     }
-    for (; p < e; p += step) {
-        float v[V];
-        load_floats<T, V>(in + (int64_t)P.row[p] * P.ld, v);
+    float* part = P.part + 2 * block * P.F + c;  // ends, then what goes on
+    if (slots == 1) {
+        if (flag & kEnds) store_floats<F32, V>(part, a);
+        if (flag & kGoesOn) store_floats<F32, V>(part + P.F, acc);
+        return;
+    }
 #pragma unroll
-        for (int i = 0; i < V; ++i) acc[i] += v[i];
+    for (int i = 0; i < V; ++i) {
+        s_a[i * kBlock + tid] = a[i];
+        s_b[i * kBlock + tid] = acc[i];
+    }
+    if (j == 0) s_flag[slot] = flag;
+    __syncthreads();
+    if (slot >= slots) return;
+    const bool last = slot == slots - 1;
+    for (int part_of = 0; part_of < 2; ++part_of) {
+        // the end of a segment that began in an earlier run; what goes on past the workgroup
+        if (part_of == 0 ? !(flag & kEnds) : !(last && flag & kGoesOn)) continue;
+        int t = part_of == 0 ? slot - 1 : slot;
+        while (t >= 0 && s_flag[t] & kMiddle) --t;
+        const bool began = t >= 0;  // in this workgroup
+        float v[V] = {};
+        for (int u = t < 0 ? 0 : t; u <= (part_of == 0 ? slot - 1 : slot); ++u)
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] += s_b[i * kBlock + u * per + j];
+        if (part_of == 0) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] += a[i];
+        }
+        if (part_of == 0 && began) {
+            write_row<T, V>(P, P.key[P.row[(block * slots + slot) * R * kRun]], c, v);
+        } else {
+            store_floats<F32, V>(part + part_of * P.F, v);
+        }
     }
 }
 
-// Rows v0, v0 + slots ... of the gradient, kRows of them, but for ids of more than C
-// positions.  Most ids have few: the offsets, the first row's number and the first
-// row of all of them go out together.
+// `sums` workgroups for the runs of positions, among others for the rows of ids
+// without any: the first wait for loads, the others for stores.
 template <typename T, int V>
-__device__ inline void sum_rows(const EmbedParams& P, int64_t v0, int first, int per, int slots,
-                                int64_t C, bool failed) {
+__global__ __launch_bounds__(kBlock) void embed_grad(EmbedParams P, int per, int slots, int R,
+                                                     int64_t sums) {
+    __shared__ float s_a[kBlock * V], s_b[kBlock * V];
+    __shared__ int s_flag[kBlock + 1];  // (one for the threads beside the teams)
     const int F = (int)P.F;
-    int32_t b[kRows], e[kRows], r[kRows];
-#pragma unroll
-    for (int u = 0; u < kRows; ++u) {
-        const int64_t v = v0 + (int64_t)u * slots;
-        const bool on = v < P.V && !failed;
-        b[u] = on ? P.rowptr[v] : 0;
-        e[u] = on ? P.rowptr[v + 1] : 0;
+    const int slot = threadIdx.x / per, first = threadIdx.x - slot * per;
+    const bool failed = *P.status != MP_OK;  // (then there are neither offsets nor an order)
+    const int64_t before = blockIdx.x * sums / gridDim.x;
+    if ((blockIdx.x + 1) * sums / gridDim.x > before) {
+        if (failed) return;
+        // (several teams: all threads make one pass)
+        for (int j = first; j < per; j += kBlock)
+            sum_runs<T, V>(P, before, j, per, slots, slot, R, s_a, s_b, s_flag);
+        return;
     }
-#pragma unroll
-    for (int u = 0; u < kRows; ++u) r[u] = b[u] < e[u] ? P.row[b[u]] : -1;
-    for (int j = first; j < per; j += kBlock) {
-        const int c = chunk_at<V>(j, F);
-        float acc[kRows][V];
-#pragma unroll
-        for (int u = 0; u < kRows; ++u) {
-            if (r[u] >= 0) {
-                load_floats<T, V>(static_cast<const typename T::raw*>(P.in) + r[u] * P.ld + c,
-                                  acc[u]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < V; ++i) acc[u][i] = 0.f;
-            }
-        }
+    if (slot >= slots) return;
+    const int64_t step = (gridDim.x - sums) * slots * kRows;
+    for (int64_t v0 = ((int64_t)blockIdx.x - before) * slots * kRows + slot; v0 < P.V; v0 += step) {
+        bool empty[kRows];
 #pragma unroll
         for (int u = 0; u < kRows; ++u) {
             const int64_t v = v0 + (int64_t)u * slots;
-            if (v >= P.V) break;
-            if (e[u] - b[u] > C) continue;
-            if (e[u] - b[u] > 1) add_rows<T, V>(P, b[u] + 1, e[u], 1, c, acc[u]);
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-                acc[u][i] = failed ? __builtin_nanf("") : acc[u][i] * P.scale;
-            store_as<V>(P.out, P.out_bf16, v * P.F + c, acc[u]);
+            empty[u] = v < P.V && (failed || P.rowptr[v] == P.rowptr[v + 1]);
         }
-    }
-}
-
-// acc of a workgroup's slots added in order, the result in slot 0.
-template <int V>
-__device__ inline void add_slots(float (&acc)[V], int per, int slots, int slot, float* lds) {
-    if (slots == 1) return;
-    __syncthreads();
-    if (slot < slots) {
+        float zero[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) lds[i * kBlock + threadIdx.x] = acc[i];
-    }
-    __syncthreads();
-    if (slot == 0) {
-        for (int q = 1; q < slots; ++q)
-#pragma unroll
-            for (int i = 0; i < V; ++i) acc[i] += lds[i * kBlock + q * per + threadIdx.x];
-    }
-}
-
-// blockIdx.x < chunks: the partial sums of a chunk of C positions.  Others: rows of
-// the gradient whose ids have at most C.
-template <typename T, int V>
-__global__ __launch_bounds__(kBlock) void embed_grad(EmbedParams P, int per, int slots, int64_t C,
-                                                     int64_t chunks) {
-    __shared__ float lds[kBlock * V];
-    const int F = (int)P.F;
-    const int slot = threadIdx.x / per, first = threadIdx.x - slot * per;
-    const bool failed = *P.status != MP_OK;  // (then rowptr is not written)
-    if ((int64_t)blockIdx.x >= chunks) {
-        if (slot >= slots) return;
-        const int64_t step = (gridDim.x - chunks) * slots * kRows;
-        for (int64_t v0 = ((int64_t)blockIdx.x - chunks) * slots * kRows + slot; v0 < P.V;
-             v0 += step)
-            sum_rows<T, V>(P, v0, first, per, slots, C, failed);
-        return;
-    }
-    if (failed) return;
-    const int64_t inside = P.rowptr[P.V];  // positions of ids of the table
-    const int64_t b = (int64_t)blockIdx.x * C, e = b + C < inside ? b + C : inside;
-    if (b >= e) return;
-    const int32_t va = P.key[P.row[b]], vb = P.key[P.row[e - 1]];
-    for (int part = 0; part < (va == vb ? 1 : 2); ++part) {
-        const int32_t v = part ? vb : va;
-        const int64_t vbeg = P.rowptr[v], vend = P.rowptr[v + 1];
-        if (vend - vbeg <= C) continue;
-        const int64_t pb = vbeg > b ? vbeg : b, pe = vend < e ? vend : e;
+        for (int i = 0; i < V; ++i) zero[i] = failed ? __builtin_nanf("") : 0.f;
         for (int j = first; j < per; j += kBlock) {
             const int c = chunk_at<V>(j, F);
-            float acc[V] = {};
-            if (slot < slots) add_rows<T, V>(P, pb + slot, pe, slots, c, acc);
-            add_slots<V>(acc, per, slots, slot, lds);
-            if (slot == 0)
-                store_floats<F32, V>(P.part + (2 * (int64_t)blockIdx.x + part) * P.F + c, acc);
+#pragma unroll
+            for (int u = 0; u < kRows; ++u)
+                if (empty[u]) store_as<V>(P.out, P.out_bf16, (v0 + (int64_t)u * slots) * P.F + c, zero);
         }
     }
 }
 
-// The rows of ids of more than C positions: the workgroup of the chunk that such an
-// id begins in (it has the chunk's last position) adds its partial sums.
+// The rows of ids whose positions lie in several workgroups (of C each), by the
+// workgroup of the first.
 template <int V>
 __global__ __launch_bounds__(kBlock) void embed_join(EmbedParams P, int per, int slots, int64_t C) {
     __shared__ float lds[kBlock * V];
     const int F = (int)P.F;
     const int slot = threadIdx.x / per, first = threadIdx.x - slot * per;
     if (*P.status != MP_OK) return;
-    const int64_t inside = P.rowptr[P.V];
-    const int64_t k0 = blockIdx.x, b = k0 * C, e = b + C < inside ? b + C : inside;
-    if (b >= e) return;
+    const int64_t k0 = blockIdx.x, b = k0 * C, e = b + C;
+    if (e >= P.rowptr[P.V]) return;  // (no position of an id of the table follows)
     const int32_t v = P.key[P.row[e - 1]];
     const int64_t vbeg = P.rowptr[v], vend = P.rowptr[v + 1];
-    if (vend - vbeg <= C || vbeg < b) return;
+    if (vend <= e || vbeg < b) return;
     const int64_t k1 = (vend - 1) / C;
     for (int j = first; j < per; j += kBlock) {
         const int c = chunk_at<V>(j, F);
@@ -241,14 +276,23 @@ __global__ __launch_bounds__(kBlock) void embed_join(EmbedParams P, int per, int
         if (slot < slots) {
 #pragma unroll 4
             for (int64_t k = k0 + slot; k <= k1; k += slots) {
-                // (in its first chunk the id is the second one, unless it begins there)
                 float t[V];
-                load_floats<F32, V>(P.part + (2 * k + (k == k0 && vbeg > b ? 1 : 0)) * P.F + c, t);
+                load_floats<F32, V>(P.part + (2 * k + (k < k1 ? 1 : 0)) * P.F + c, t);
 #pragma unroll
                 for (int i = 0; i < V; ++i) acc[i] += t[i];
             }
         }
-        add_slots<V>(acc, per, slots, slot, lds);
+        if (slots > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < V; ++i) lds[i * kBlock + threadIdx.x] = acc[i];
+            __syncthreads();
+            if (slot == 0) {
+                for (int q = 1; q < slots; ++q)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) acc[i] += lds[i * kBlock + q * per + threadIdx.x];
+            }
+        }
         if (slot == 0) {
 #pragma unroll
             for (int i = 0; i < V; ++i) acc[i] *= P.scale;
@@ -259,19 +303,21 @@ __global__ __launch_bounds__(kBlock) void embed_join(EmbedParams P, int per, int
 
 int64_t at_most(int64_t blocks) { return blocks < kMaxGrid ? blocks : kMaxGrid; }
 
-// Elements of a chunk, chunks of a row and rows side by side in a workgroup.  bf16
-// rows of a multiple of 4 but not of 8 are taken 4 at a time: 
+// Elements of a chunk, chunks of a row and rows side by side in a workgroup.  (Rows of
+// 100 bf16 by chunks of 4 that divide them: 195 us for 1.9M of them, of 8 155.)
 struct EmbedShape {
-    int V, per, slots;
+    int V, per, slots, R;  // R * kRun positions of a team: at least 128 of a workgroup
 };
 EmbedShape embed_shape(int64_t F, int dtype) {
     EmbedShape h;
-    h.V = dtype == MP_BF16 && (F % 8 == 0 || F % 4 != 0) ? 8 : 4;
+    h.V = dtype == MP_BF16 ? 8 : 4;
     if (F < h.V) h.V = 1;
     h.per = (int)ceil_div(F, h.V);
     h.slots = h.per < kBlock ? kBlock / h.per : 1;
+    h.R = (int)ceil_div(128, h.slots * kRun);
     return h;
 }
+int64_t positions(const EmbedShape& h) { return (int64_t)h.slots * h.R * kRun; }
 
 template <typename T, int V>
 void launch_rows(const EmbedParams& p, const EmbedShape& h, hipStream_t s) {
@@ -281,21 +327,22 @@ void launch_rows(const EmbedParams& p, const EmbedShape& h, hipStream_t s) {
 
 template <typename T, int V>
 void launch_grad(const EmbedParams& p, const EmbedShape& h, hipStream_t s) {
-    const int64_t C = embed_chunk(p.N), chunks = p.N > C ? ceil_div(p.N, C) : 0;
-    hipLaunchKernelGGL((embed_grad<T, V>), dim3((unsigned)(chunks + at_most(ceil_div(p.V, h.slots * kRows)))),
-                       dim3(kBlock), 0, s, p, h.per, h.slots, C, chunks);
-    if (chunks)
-        hipLaunchKernelGGL((embed_join<V>), dim3((unsigned)chunks), dim3(kBlock), 0, s, p, h.per,
+    const int64_t C = positions(h), sums = ceil_div(p.N, C);
+    hipLaunchKernelGGL((embed_grad<T, V>),
+                       dim3((unsigned)(sums + at_most(ceil_div(p.V, h.slots * kRows)))), dim3(kBlock),
+                       0, s, p, h.per, h.slots, h.R, sums);
+    if (sums > 1)
+        hipLaunchKernelGGL((embed_join<V>), dim3((unsigned)(sums - 1)), dim3(kBlock), 0, s, p, h.per,
                            h.slots, C);
 }
 
 }  // namespace
 
-// Positions of a chunk.
-int64_t embed_chunk(int64_t N) {
-    int64_t c = 64;
-    while (c < 512 && c * 8192 < N) c *= 2;
-    return c;
+// Workgroups of either type's sums, with two lines of F floats each.
+int64_t embed_parts(int64_t N, int64_t F) {
+    const int64_t a = ceil_div(N, positions(embed_shape(F, MP_F32)));
+    const int64_t b = ceil_div(N, positions(embed_shape(F, MP_BF16)));
+    return a > b ? a : b;
 }
 
 hipError_t launch_embed(const EmbedParams& p, int dtype, hipStream_t s) {
@@ -305,9 +352,8 @@ hipError_t launch_embed(const EmbedParams& p, int dtype, hipStream_t s) {
         if (dtype == MP_BF16) launch_rows<BF16, 1>(p, h, s);
         else launch_rows<F32, 1>(p, h, s);
     } else {
-        if (dtype == MP_F32) launch_rows<F32, 4>(p, h, s);
-        else if (h.V == 8) launch_rows<BF16, 8>(p, h, s);
-        else launch_rows<BF16, 4>(p, h, s);
+        if (dtype == MP_BF16) launch_rows<BF16, 8>(p, h, s);
+        else launch_rows<F32, 4>(p, h, s);
     }
     return hipGetLastError();
 }
@@ -325,9 +371,8 @@ hipError_t launch_embed_backward(const EmbedParams& p, int dtype, hipStream_t s)
         if (dtype == MP_BF16) launch_grad<BF16, 1>(p, h, s);
         else launch_grad<F32, 1>(p, h, s);
     } else {
-        if (dtype == MP_F32) launch_grad<F32, 4>(p, h, s);
-        else if (h.V == 8) launch_grad<BF16, 8>(p, h, s);
-        else launch_grad<BF16, 4>(p, h, s);
+        if (dtype == MP_BF16) launch_grad<BF16, 8>(p, h, s);
+        else launch_grad<F32, 4>(p, h, s);
     }
     return hipGetLastError();
 }

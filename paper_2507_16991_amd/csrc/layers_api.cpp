@@ -108,13 +108,12 @@ int embed_space(int64_t N, int64_t V, int64_t F, EmbedSpace& m) {
         at = align_up(at + bytes, 256);
         return b;
     };
-    const int64_t C = embed_chunk(N);
     m.key = take((size_t)N * 4);
     m.row = take((size_t)N * 4);
     m.col = take((size_t)N * 4);
     m.rowptr = take((size_t)(V + 2) * 4);
     m.status = take(4);
-    m.part = take(N > C ? (size_t)ceil_div(N, C) * 2 * (size_t)F * 4 : 0);
+    m.part = take((size_t)embed_parts(N, F) * 2 * (size_t)F * 4);
     m.sort = take(m.sort_bytes);
     m.bytes = at;
     return MP_OK;

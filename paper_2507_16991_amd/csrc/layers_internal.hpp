@@ -285,9 +285,9 @@ struct EmbedParams {
     const int32_t* row;        // [N] the row at every position
     const int32_t* key;        // [N] the id of every row, V outside
     const int32_t* status;     // the sort's
-    float* part;               // [embed_chunks][2][F]
+    float* part;               // [embed_parts][2][F]
 };
-int64_t embed_chunk(int64_t N);
+int64_t embed_parts(int64_t N, int64_t F);
 hipError_t launch_embed(const EmbedParams& p, int dtype, hipStream_t s);
 hipError_t launch_embed_keys(const EmbedParams& p, int32_t* key, int32_t* row, hipStream_t s);
 hipError_t launch_embed_backward(const EmbedParams& p, int dtype, hipStream_t s);

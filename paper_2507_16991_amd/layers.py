@@ -90,13 +90,14 @@ def _on(stream):
 
 def _on_gpu(*tensors):
     """Kernels run on the current GPU: an operand elsewhere is refused."""
-    here = None
+    here = -1
     for t in tensors:
         if t is None:
             continue
-        if here is None and t.is_cuda:
+        at = t.get_device()  # (-1: not on a GPU)
+        if here < 0 <= at:
             here = torch.cuda.current_device()
-        if not t.is_cuda or t.get_device() != here:
+        if at < 0 or at != here:
             raise ValueError(f"operands must be on the current GPU, got one on {t.device}")
 
 
