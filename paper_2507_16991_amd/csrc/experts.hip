@@ -150,24 +150,67 @@ __device__ inline Lists take_rows(const ExpertParams& p, int* lds) {
 // i-th of four products, the elements at(i, q) .. + 7.  Any order will do that both
 // operands share: 4-bit weights take a whole block to a lane (16 bytes), bf16 ones
 // go through memory by whole lines.
-// FULL: the step ends within K.  Only such loads are many at a time, without branches
-// and without a use of what they load: a branch around a load, or a shift of a scale
-// in it, made each wait for the one before (70 us against 30 for 56 experts of 16 rows).
+// kFull: all steps of a load end below `end`, which no row is shorter than.  kEnd:
+// places past the row read its last whole 8 elements (or its last block) instead, to
+// be shifted into place or dropped once they are there.  kShort: rows of fewer than
+// 8 elements, one by one.  But for those no load has a branch around it, or a use of
+// what it loads: either made each wait for the one before (70 us against 36 for 56
+// experts of 16 rows).
+enum Reach { kFull, kEnd, kShort };
 
-// Eight bf16 elements k .. k+7 of a row of K, zero past its end.
-template <bool FULL>
-__device__ inline bf16x8 load_bf16(const uint16_t* p, int k, int K) {
-    uint16_t u[8] = {};
-    if (FULL || k + 8 <= K) {
-        __builtin_memcpy(u, p + k, 16);
-    } else {
+// What a lane keeps of 8 elements from k on that were read from min(k, K - 8) on:
+// `skip` of them are before k, and all are dropped from `end` on.
+struct Place {
+    int start, skip;
+};
+__device__ inline Place place(int k, int end, int K) {
+    const int last = K - 8;
+    Place p;
+    p.start = k < last ? k : last;
+    p.skip = k < end ? k - p.start : 8;
+    return p;
+}
+// Elements skip .. skip+7 of 8 words, zeros after the last.
+__device__ inline void shift_words(uint32_t (&w)[8], int skip) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (k + i < K) u[i] = p[k + i];
+    for (int by = 4; by; by >>= 1)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = skip & by ? (i + by < 8 ? w[i + by] : 0u) : w[i];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = skip >= 8 ? 0u : w[i];
+}
+// The same of 8 halves in 4 words.
+__device__ inline void shift_halves(uint32_t (&w)[4], int skip) {
+#pragma unroll
+    for (int by = 2; by; by >>= 1)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = skip & (2 * by) ? (i + by < 4 ? w[i + by] : 0u) : w[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t next = i < 3 ? w[i + 1] : 0u;
+        w[i] = skip & 1 ? (w[i] >> 16) | (next << 16) : w[i];
     }
-    bf16x8 v;
-    __builtin_memcpy(&v, u, 16);
-    return v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = skip >= 8 ? 0u : w[i];
+}
+
+// Eight bf16 elements from k on; of rows shorter than 8 one by one.
+template <Reach R>
+__device__ inline void load_bf16(uint32_t (&w)[4], const uint16_t* p, int k, int end, int K) {
+    if constexpr (R != kShort) {
+        __builtin_memcpy(w, p + (R == kFull ? k : place(k, end, K).start), 16);
+    } else {
+        uint16_t u[8] = {};
+        for (int i = 0; i < 8; ++i)
+            if (k + i < end) u[i] = p[k + i];
+        __builtin_memcpy(w, u, 16);
+    }
+}
+template <Reach R>
+__device__ inline bf16x8 take_bf16(const uint32_t (&w)[4], int k, int end, int K) {
+    uint32_t t[4] = {w[0], w[1], w[2], w[3]};
+    if (R == kEnd) shift_halves(t, place(k, end, K).skip);
+    return __builtin_bit_cast(bf16x8, t);
 }
 
 struct WeightsMx4 {
@@ -186,32 +229,45 @@ struct WeightsMx4 {
         const int64_t KB = (K + 31) / 32;
         return Row{static_cast<const uint8_t*>(w) + r * KB * 16, scales + r * KB};
     }
-    // (the scales of U steps are one load: as many requests as rows)
-    template <int U, bool FULL>
-    __device__ static void load(Raw<U>& r, const Row& w, int s, int q, int K) {
-        const int KB = (K + 31) / 32, b = 4 * s + q;
-        if (FULL) {
-            __builtin_memcpy(r.s, w.scales + 4 * s, 4 * U);
+    // (the scales of U whole steps are one load: as many requests as rows)
+    template <int U, Reach R>
+    __device__ static void load(Raw<U>& r, const Row& w, int s, int q, int end, int K) {
+        const int last = (K + 31) / 32 - 1;
+        if (R == kFull) __builtin_memcpy(r.s, w.scales + 4 * s, 4 * U);
 #pragma unroll
-            for (int u = 0; u < U; ++u) __builtin_memcpy(r.c[u], w.codes + (b + 4 * u) * 16, 16);
-        } else {
-            r = Raw<U>{};
-            if (b < KB) {
-                __builtin_memcpy(r.c[0], w.codes + b * 16, 16);
-                r.s[0] = (uint32_t)w.scales[b] << (8 * q);
+        for (int u = 0; u < U; ++u) {
+            int b = 4 * (s + u) + q;
+            if (R != kFull) {
+                b = b < last ? b : last;
+                r.s[u] = w.scales[b];
             }
+            __builtin_memcpy(r.c[u], w.codes + b * 16, 16);
         }
     }
-    template <int U>
-    __device__ static void unpack(const Raw<U>& r, int u, int q, bf16x8 (&v)[4]) {
-        const float f = scale_value((r.s[u] >> (8 * q)) & 255);
+    // (blocks from `end` on are dropped)
+    template <int U, Reach R>
+    __device__ static uint32_t scale(const Raw<U>& r, int u, int s, int q, int end) {
+        return R == kFull ? (r.s[u] >> (8 * q)) & 255 : (kStep * (s + u) + 32 * q < end ? r.s[u] : 0u);
+    }
+    template <int U, Reach R>
+    __device__ static void codes(const Raw<U>& r, int u, int s, int q, int end, uint32_t (&c)[4]) {
+        const bool on = R == kFull || kStep * (s + u) + 32 * q < end;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c[i] = on ? r.c[u][i] : 0u;
+    }
+    template <int U, Reach R>
+    __device__ static void unpack(const Raw<U>& r, int u, int s, int q, int end, int,
+                                  bf16x8 (&v)[4]) {
+        const float f = scale_value(scale<U, R>(r, u, s, q, end));
+        uint32_t c[4];
+        codes<U, R>(r, u, s, q, end, c);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             bf16x2 t[4];
-            t[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.c[u][i], f, 0);
-            t[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.c[u][i], f, 1);
-            t[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.c[u][i], f, 2);
-            t[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.c[u][i], f, 3);
+            t[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[i], f, 0);
+            t[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[i], f, 1);
+            t[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[i], f, 2);
+            t[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[i], f, 3);
             __builtin_memcpy(&v[i], t, 16);
         }
     }
@@ -221,25 +277,27 @@ struct WeightsBf16 {
     static constexpr bool kMx4 = false;
     template <int U>
     struct Raw {
-        bf16x8 v[U][4];
+        uint32_t v[U][4][4];
     };
     typedef const uint16_t* Row;
     __device__ static int at(int i, int q) { return 32 * i + 8 * q; }
     __device__ static Row row(const void* w, const uint8_t*, int64_t r, int K) {
         return static_cast<const uint16_t*>(w) + r * K;
     }
-    template <int U, bool FULL>
-    __device__ static void load(Raw<U>& r, const Row& w, int s, int q, int K) {
+    template <int U, Reach R>
+    __device__ static void load(Raw<U>& r, const Row& w, int s, int q, int end, int K) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                r.v[u][i] = load_bf16<FULL>(w, kStep * (s + u) + at(i, q), K);
+                load_bf16<R>(r.v[u][i], w, kStep * (s + u) + at(i, q), end, K);
     }
-    template <int U>
-    __device__ static void unpack(const Raw<U>& r, int u, int, bf16x8 (&v)[4]) {
+    template <int U, Reach R>
+    __device__ static void unpack(const Raw<U>& r, int u, int s, int q, int end, int K,
+                                  bf16x8 (&v)[4]) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = r.v[u][i];
+        for (int i = 0; i < 4; ++i)
+            v[i] = take_bf16<R>(r.v[u][i], kStep * (s + u) + at(i, q), end, K);
     }
 };
 
@@ -270,34 +328,41 @@ struct RowsF32 {
     static constexpr bool kScaled = false;
     template <int U>
     struct Raw {
-        float v[U][4][8];
+        uint32_t v[U][4][8];
     };
     typedef const float* Row;
     __device__ static Row row(const ExpertParams& p, int r) {
         return static_cast<const float*>(p.x) + r * p.ldx;
     }
-    template <typename W, int U, bool FULL>
-    __device__ static void load(Raw<U>& r, const ExpertParams&, Row x, int s, int q, int K) {
+    template <typename W, int U, Reach R>
+    __device__ static void load(Raw<U>& r, const ExpertParams&, Row x, int s, int q, int end,
+                                int K) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int k = kStep * (s + u) + W::at(i, q);
-                if (FULL) {
-                    __builtin_memcpy(r.v[u][i], x + k, 32);
+                if constexpr (R != kShort) {
+                    __builtin_memcpy(r.v[u][i], x + (R == kFull ? k : place(k, end, K).start), 32);
                 } else {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) r.v[u][i][j] = k + j < K ? x[k + j] : 0.f;
+                    for (int j = 0; j < 8; ++j)
+                        r.v[u][i][j] = k + j < end ? __float_as_uint(x[k + j]) : 0u;
                 }
             }
     }
-    template <typename W, int U>
-    __device__ static void unpack(const Raw<U>& r, int u, int i, int, bf16x8 (&v)[TERMS]) {
+    template <typename W, int U, Reach R>
+    __device__ static void unpack(const Raw<U>& r, int u, int i, int s, int q, int end, int K,
+                                  bf16x8 (&v)[TERMS]) {
+        uint32_t f[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = r.v[u][i][j];
+        if (R == kEnd)
+            shift_words(f, place(kStep * (s + u) + W::at(i, q), end, K).skip);
         uint16_t t[TERMS][8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             uint16_t w[TERMS];
-            split<TERMS>(r.v[u][i][j], w);
+            split<TERMS>(__uint_as_float(f[j]), w);
 #pragma unroll
             for (int m = 0; m < TERMS; ++m) t[m][j] = w[m];
         }
@@ -312,23 +377,25 @@ struct RowsBf16 {
     static constexpr bool kScaled = false;
     template <int U>
     struct Raw {
-        bf16x8 v[U][4];
+        uint32_t v[U][4][4];
     };
     typedef const uint16_t* Row;
     __device__ static Row row(const ExpertParams& p, int r) {
         return static_cast<const uint16_t*>(p.x) + r * p.ldx;
     }
-    template <typename W, int U, bool FULL>
-    __device__ static void load(Raw<U>& r, const ExpertParams&, Row x, int s, int q, int K) {
+    template <typename W, int U, Reach R>
+    __device__ static void load(Raw<U>& r, const ExpertParams&, Row x, int s, int q, int end,
+                                int K) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                r.v[u][i] = load_bf16<FULL>(x, kStep * (s + u) + W::at(i, q), K);
+                load_bf16<R>(r.v[u][i], x, kStep * (s + u) + W::at(i, q), end, K);
     }
-    template <typename W, int U>
-    __device__ static void unpack(const Raw<U>& r, int u, int i, int, bf16x8 (&v)[1]) {
-        v[0] = r.v[u][i];
+    template <typename W, int U, Reach R>
+    __device__ static void unpack(const Raw<U>& r, int u, int i, int s, int q, int end, int K,
+                                  bf16x8 (&v)[1]) {
+        v[0] = take_bf16<R>(r.v[u][i], kStep * (s + u) + W::at(i, q), end, K);
     }
 };
 
@@ -350,40 +417,47 @@ struct RowsMx8 {
         const int64_t KB = (p.K + 31) / 32;
         return Row{static_cast<const uint8_t*>(p.x) + r * KB * 32, p.x_scales + r * KB};
     }
-    template <typename W, int U, bool FULL>
-    __device__ static void load(Raw<U>& r, const ExpertParams&, const Row& x, int s, int q, int K) {
-        const int KB = (K + 31) / 32;
-        if (FULL) __builtin_memcpy(r.s, x.scales + 4 * s, 4 * U);
-        else r = Raw<U>{};
+    template <typename W, int U, Reach R>
+    __device__ static void load(Raw<U>& r, const ExpertParams&, const Row& x, int s, int q, int end,
+                                int K) {
+        const int last = (K + 31) / 32 - 1;
+        // (places of an element in blocks that are not there: of the last one)
+        const auto in_row = [&](int k) { return R == kFull || k / 32 <= last ? k : 32 * last + k % 32; };
+        if (R == kFull) __builtin_memcpy(r.s, x.scales + 4 * s, 4 * U);
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) {
+            const int k0 = kStep * (s + u);
             if constexpr (kScaled<W>) {
                 // 8-bit codes k = 16 q .. + 15 and 64 + 16 q .. + 15
 #pragma unroll
-                for (int i = 0; i < 4; i += 2) {
-                    const int k = kStep * (s + u) + 32 * i + 16 * q;
-                    if (FULL || k / 32 < KB) __builtin_memcpy(r.c[u][i], x.codes + k, 16);
-                }
+                for (int i = 0; i < 4; i += 2)
+                    __builtin_memcpy(r.c[u][i], x.codes + in_row(k0 + 32 * i + 16 * q), 16);
+                if (R != kFull) r.s[u] = x.scales[in_row(k0 + 32 * q) / 32];
             } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int k = kStep * (s + u) + W::at(i, q);
-                    if (FULL || k / 32 < KB) __builtin_memcpy(r.c[u][i], x.codes + k, 8);
+                for (int i = 0; i < 4; ++i)
+                    __builtin_memcpy(r.c[u][i], x.codes + in_row(k0 + W::at(i, q)), 8);
+                if (R != kFull) {
+                    uint32_t b[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) b[i] = x.scales[in_row(k0 + 32 * i) / 32];
+                    r.s[u] = b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24;
                 }
             }
-        if (!FULL) {
-            for (int i = 0; i < 4; ++i)
-                if (4 * s + i < KB) r.s[0] |= (uint32_t)x.scales[4 * s + i] << (8 * i);
         }
     }
-    template <typename W, int U>
-    __device__ static void unpack(const Raw<U>& r, int u, int i, int q, bf16x8 (&v)[1]) {
-        const float f = scale_value((r.s[u] >> (W::at(i, q) / 32 * 8)) & 255);
+    template <typename W, int U, Reach R>
+    __device__ static void unpack(const Raw<U>& r, int u, int i, int s, int q, int end, int,
+                                  bf16x8 (&v)[1]) {
+        const int k = W::at(i, q);
+        const bool on = R == kFull || kStep * (s + u) + k < end;
+        const float f = scale_value(on ? (r.s[u] >> (k / 32 * 8)) & 255 : 0u);
+        const uint32_t c0 = on ? r.c[u][i][0] : 0u, c1 = on ? r.c[u][i][1] : 0u;
         bf16x2 t[4];
-        t[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.c[u][i][0], f, false);
-        t[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.c[u][i][0], f, true);
-        t[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.c[u][i][1], f, false);
-        t[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.c[u][i][1], f, true);
+        t[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c0, f, false);
+        t[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c0, f, true);
+        t[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c1, f, false);
+        t[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c1, f, true);
         __builtin_memcpy(&v[0], t, 16);
     }
 };
@@ -396,25 +470,34 @@ struct RowsOfH {
     static constexpr bool kScaled = false;
     template <int U>
     struct Raw {
-        bf16x8 v[U][TERMS][4];
+        uint32_t v[U][TERMS][4][4];
     };
     typedef const uint16_t* Row;
-    template <typename W, int U, bool FULL>
-    __device__ static void load(Raw<U>& r, const ExpertParams& p, Row x, int s, int q, int) {
+    template <typename W, int U, Reach R>
+    __device__ static void load(Raw<U>& r, const ExpertParams& p, Row x, int s, int q, int, int) {
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) {
+            // (steps that are not there: the last one, dropped)
+            const int at = R == kFull || kStep * (s + u) < p.Hp ? s + u : p.Hp / kStep - 1;
 #pragma unroll
             for (int m = 0; m < TERMS; ++m)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    __builtin_memcpy(&r.v[u][m][i],
-                                     x + (int64_t)m * p.P * p.Hp + kStep * (s + u) + W::at(i, q),
-                                     16);
+                    __builtin_memcpy(r.v[u][m][i],
+                                     x + (int64_t)m * p.P * p.Hp + kStep * at + W::at(i, q), 16);
+        }
     }
-    template <typename W, int U>
-    __device__ static void unpack(const Raw<U>& r, int u, int i, int, bf16x8 (&v)[TERMS]) {
+    template <typename W, int U, Reach R>
+    __device__ static void unpack(const Raw<U>& r, int u, int i, int s, int q, int end, int,
+                                  bf16x8 (&v)[TERMS]) {
+        const bool on = R == kFull || kStep * (s + u) + W::at(i, q) < end;
 #pragma unroll
-        for (int m = 0; m < TERMS; ++m) v[m] = r.v[u][m][i];
+        for (int m = 0; m < TERMS; ++m) {
+            uint32_t t[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) t[j] = on ? r.v[u][m][i][j] : 0u;
+            v[m] = __builtin_bit_cast(bf16x8, t);
+        }
     }
 };
 
@@ -427,47 +510,63 @@ constexpr int steps_at_once() {
 }
 
 // acc[t][m] += weight rows w[t] (this lane's of each 16) times rows x[m] (this lane's
-// of each 16): U steps from s on.
-template <typename W, typename X, int M, int U, bool FULL>
+// of each 16): U steps from s on, without elements from `end` on.
+template <typename W, typename X, int M, int U, Reach R>
 __device__ inline void multiply_steps(const ExpertParams& p, const typename W::Row (&w)[2],
-                                      const typename X::Row (&x)[M], int K, int s,
+                                      const typename X::Row (&x)[M], int K, int s, int end,
                                       f32x4 (&acc)[2][M]) {
     const int q = (threadIdx.x & 63) >> 4;
     typename W::template Raw<U> rw[2];
     typename X::template Raw<U> rx[M];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) W::template load<U, FULL>(rw[t], w[t], s, q, K);
+    for (int t = 0; t < 2; ++t) W::template load<U, R>(rw[t], w[t], s, q, end, K);
 #pragma unroll
-    for (int m = 0; m < M; ++m) X::template load<W, U, FULL>(rx[m], p, x[m], s, q, K);
+    for (int m = 0; m < M; ++m) X::template load<W, U, R>(rx[m], p, x[m], s, q, end, K);
     __builtin_amdgcn_sched_barrier(0);  // (the compiler would spread them to save registers)
     if constexpr (X::template kScaled<W>) {
         // lane quarter q has the scales of block q
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) {
+            i32x8 a[2];
+            int sa[2];
 #pragma unroll
-            for (int m = 0; m < M; ++m)
+            for (int t = 0; t < 2; ++t) {
+                uint32_t c[4];
+                W::template codes<U, R>(rw[t], u, s, q, end, c);
+                a[t] = i32x8{(int)c[0], (int)c[1], (int)c[2], (int)c[3], 0, 0, 0, 0};
+                sa[t] = (int)W::template scale<U, R>(rw[t], u, s, q, end);
+            }
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const uint32_t* c = rw[t].c[u];
-                    i32x8 a = {(int)c[0], (int)c[1], (int)c[2], (int)c[3], 0, 0, 0, 0}, b;
-                    __builtin_memcpy(&b, rx[m].c[u], 32);
-                    acc[t][m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-                        a, b, acc[t][m], kE2M1, kE4M3, 0, (int)(rw[t].s[u] >> (8 * q)), 0,
-                        (int)(rx[m].s[u] >> (8 * q)));
+            for (int m = 0; m < M; ++m) {
+                // (codes of the other half of a dropped block lie in other lanes)
+                i32x8 b;
+                __builtin_memcpy(&b, rx[m].c[u], 32);
+                int sb = (int)(R == kFull ? rx[m].s[u] >> (8 * q) : rx[m].s[u]);
+                if (R != kFull) {
+                    const int k = kStep * (s + u);
+                    sb = k + 32 * q < end ? sb : 0;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) b[i] = k + 64 * (i / 4) + 16 * q < end ? b[i] : 0;
                 }
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+                    acc[t][m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                        a[t], b, acc[t][m], kE2M1, kE4M3, 0, sa[t], 0, sb);
+            }
+        }
         return;
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         bf16x8 a[2][4];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) W::template unpack<U>(rw[t], u, q, a[t]);
+        for (int t = 0; t < 2; ++t) W::template unpack<U, R>(rw[t], u, s, q, end, K, a[t]);
 #pragma unroll
         for (int m = 0; m < M; ++m)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 bf16x8 b[X::kTerms];
-                X::template unpack<W, U>(rx[m], u, i, q, b);
+                X::template unpack<W, U, R>(rx[m], u, i, s, q, end, K, b);
 #pragma unroll
                 for (int c = X::kTerms - 1; c >= 0; --c)
 #pragma unroll
@@ -484,16 +583,14 @@ __device__ inline void multiply(const ExpertParams& p, const typename W::Row (&w
                                 const typename X::Row (&x)[M], int K, int s, int s1,
                                 f32x4 (&acc)[2][M]) {
     constexpr int U = steps_at_once<W, X, M>();
-    const int full = K / kStep < s1 ? K / kStep : s1;
-    for (; s + U <= full; s += U) multiply_steps<W, X, M, U, true>(p, w, x, K, s, acc);
-    if constexpr (U > 2) {
-        if (s + 2 <= full) {
-            multiply_steps<W, X, M, 2, true>(p, w, x, K, s, acc);
-            s += 2;
-        }
+    const int end = s1 * kStep < K ? s1 * kStep : K;
+    for (; (s + U) * kStep <= end; s += U) multiply_steps<W, X, M, U, kFull>(p, w, x, K, s, end, acc);
+    if (K >= 8) {
+        constexpr int E = U < 2 ? U : 2;
+        for (; s * kStep < end; s += E) multiply_steps<W, X, M, E, kEnd>(p, w, x, K, s, end, acc);
+    } else if (s * kStep < end) {
+        multiply_steps<W, X, M, 1, kShort>(p, w, x, K, s, end, acc);
     }
-    if (U > 1 && s < full) multiply_steps<W, X, M, 1, true>(p, w, x, K, s++, acc);
-    if (s < s1) multiply_steps<W, X, M, 1, false>(p, w, x, K, s, acc);
 }
 
 // ---- up ---------------------------------------------------------------------------------
