@@ -29,7 +29,7 @@ constexpr int kWaves = kBlock / kWave;
 constexpr int kStep = 128;    // elements of K of a step, 32 for a quarter of the lanes
 constexpr int kE4M3 = 0, kE2M1 = 4;  // operand formats of the scaled products
 constexpr int kCols = 32;     // weight rows of a workgroup
-constexpr int64_t kUpGrid = 1024;  // workgroups of the first launch, at most
+constexpr int64_t kUpGrid = 512;  // workgroups of the first launch, at most
 constexpr int kLine = 36;     // floats of a row's sums in LDS
 
 // 2^(s - 127) (s = 0 is subnormal); NaN for 255.
@@ -585,12 +585,21 @@ __device__ inline void multiply(const ExpertParams& p, const typename W::Row (&w
     constexpr int U = steps_at_once<W, X, M>();
     const int end = s1 * kStep < K ? s1 * kStep : K;
     for (; (s + U) * kStep <= end; s += U) multiply_steps<W, X, M, U, kFull>(p, w, x, K, s, end, acc);
-    if (K >= 8) {
-        constexpr int E = U < 2 ? U : 2;
-        for (; s * kStep < end; s += E) multiply_steps<W, X, M, E, kEnd>(p, w, x, K, s, end, acc);
-    } else if (s * kStep < end) {
-        multiply_steps<W, X, M, 1, kShort>(p, w, x, K, s, end, acc);
+    if constexpr (U > 2) {
+        if ((s + 2) * kStep <= end) {
+            multiply_steps<W, X, M, 2, kFull>(p, w, x, K, s, end, acc);
+            s += 2;
+        }
     }
+    if constexpr (U > 1) {
+        if ((s + 1) * kStep <= end) {
+            multiply_steps<W, X, M, 1, kFull>(p, w, x, K, s, end, acc);
+            ++s;
+        }
+    }
+    if (s * kStep >= end) return;
+    if (K >= 8) multiply_steps<W, X, M, 1, kEnd>(p, w, x, K, s, end, acc);
+    else multiply_steps<W, X, M, 1, kShort>(p, w, x, K, s, end, acc);
 }
 
 // ---- up ---------------------------------------------------------------------------------
@@ -640,7 +649,7 @@ __device__ inline void up_rows(const ExpertParams& p, const Lists& l, int e, int
 #pragma unroll
     for (int m = 0; m < M; ++m) {
         const int at = n0 + 16 * m + (lane & 15);
-        if (at >= n) continue;
+        if (at >= n || i >= 4) continue;
         const int pair = l.pairs[begin + at];
         float z[2] = {0.f, 0.f};
 #pragma unroll
