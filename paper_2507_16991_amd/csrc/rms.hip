@@ -553,7 +553,9 @@ int64_t rms_parts(int64_t N, int64_t F, int dtype) {
     const RmsShape h = rms_shape(F, dtype, false);
     if (wide(h)) return N < 1 ? 1 : ceil_div(N, wide_rows(N));
     const int64_t groups = ceil_div(N, h.block / h.L);
-    const int64_t most = h.block == 1024 ? 512 : 2048;
+    // (2.4M rows of 100 fp32 with 768, 1,024 and 2,048 workgroups: 564, 580 and 643 us;
+    // 169,343 of 256 bf16 53, 49 and 43, and the lines' sum 5, 5 and 10)
+    const int64_t most = h.block == 1024 ? 512 : 1024;
     return groups < 1 ? 1 : (groups < most ? groups : most);
 }
 

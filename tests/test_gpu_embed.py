@@ -160,3 +160,44 @@ def test_replayed_from_a_graph():
         torch.cuda.synchronize()
         assert torch.equal(out, mp.embed(ids, table))
         assert torch.equal(grad, mp.embed_backward(ids, dout, 3000))
+
+
+def test_tables_past_32_bits():
+    v, f = 2 ** 25 + 77, 70
+    table = torch.zeros(v, f, dtype=BF16, device=DEV)
+    assert table.numel() > 2 ** 31
+    rows = torch.randn(500, f, generator=torch.Generator().manual_seed(1)).to(BF16).to(DEV)
+    at = torch.randperm(v, generator=torch.Generator().manual_seed(2))[:500]
+    at[:3] = torch.tensor([v - 1, 0, 2 ** 31 // f + 1])
+    table[at.to(DEV)] = rows
+    ids = at.to(DEV)
+    assert torch.equal(mp.embed(ids, table), table[ids])
+    grad = mp.embed_backward(ids, rows, v)
+    assert torch.equal(grad[ids], mp.embed_backward(ids.argsort().argsort(), rows, 500)[ids.argsort().argsort()])
+    assert int((grad != 0).any(1).sum()) == len(at.unique())
+
+
+def test_a_training_step_of_the_entrance():
+    """Embedding, residual and norm, and their gradients together, against torch's in 64 bits."""
+    n, v, f = 3000, 170, 48
+    ids, table, dout = make(n, v, f, F32, torch.int64)
+    res = torch.randn(n, f, generator=torch.Generator().manual_seed(3)).to(DEV)
+    w = 1 + 0.1 * torch.randn(f, generator=torch.Generator().manual_seed(4)).to(DEV)
+    x = mp.embed(ids, table, scale=2.0)
+    out, total, rstd = mp.rms_norm(x, w, residual=res)
+    dx, dw = mp.rms_norm_backward(total, dout, rstd, w, dtotal=res)
+    dtable = mp.embed_backward(ids, dx, v, scale=2.0)
+
+    t64, w64 = table.cpu().double().requires_grad_(), w.cpu().double().requires_grad_()
+    i = ids.cpu()
+    ok = ((i >= 0) & (i < v))[:, None]
+    x64 = torch.where(ok, t64[torch.where(ok[:, 0], i, 0)] * 2.0, 0.0) + res.cpu().double()
+    y = x64 / torch.sqrt((x64 ** 2).mean(1, keepdim=True) + float(np.float32(1e-5))) * w64
+    ((y * dout.cpu().double()).sum() + (x64 * res.cpu().double()).sum()).backward()
+    # dx is off by 237 half steps of its terms (as tested by itself) and, for the two roundings of total
+    # (its own and the embedding's), by six times their change; dtable by its additions besides
+    _, size, _, sdw = ref.rms_norm_backward(f64(total), f64(dout), f64(w), 1e-5, f64(res))
+    _, part, count = ref.embed_backward(i.numpy(), size, v, 2.0)
+    tol = part * (237 + 12 + count[:, None] + 1) * ref.U
+    assert (np.abs(f64(dtable) - t64.grad.numpy()) <= tol).all()
+    assert (np.abs(f64(dw) - w64.grad.numpy()) <= sdw * (n + 50 + 6) * ref.U).all()

@@ -269,6 +269,18 @@ def test_a_layer_for_few_rows():
     out = mp.expert_mlp((codes, scales), idx, weight, w1, w2, residual=x)
     check(out, f64(values), idx, weight, v1, v2, "silu", True, x)
     assert torch.equal(out[3], x[3])
-    # the same experts through the sorted rows of a batch, whose rows are cut to 4 bits on the way
-    pairs = torch.arange(n * k, device=DEV, dtype=torch.int32)
-    assert int(counts[-1]) == n - 1 and pairs.numel() == idx.numel()
+    # rows of no choice come back as they were, and the router counted the others
+    assert int(counts[-1]) == n - 1 and (idx[3] == -1).all()
+
+
+def test_weights_past_32_bits():
+    """The last of experts whose weights take more than 2^32 bytes, against the same expert alone."""
+    e, f, h, fo = 5, 16384, 32768, 16000
+    w1 = (torch.randint(-8, 9, (e, h, f), device=DEV, dtype=torch.int8)).to(BF16)
+    w2 = (torch.randint(-8, 9, (e, fo, h), device=DEV, dtype=torch.int8)).to(BF16)
+    assert w1.numel() * 2 > 2 ** 32 and w2.numel() * 2 > 2 ** 32
+    x = randn(1, 3, f).to(BF16)
+    idx, weight = torch.full((3, 1), e - 1, dtype=torch.int32, device=DEV), torch.ones(3, 1, device=DEV)
+    out = mp.expert_mlp(x, idx, weight, w1, w2, act="relu", gated=False)
+    alone = mp.expert_mlp(x, idx - (e - 1), weight, w1[e - 1:], w2[e - 1:], act="relu", gated=False)
+    assert torch.equal(out, alone) and out.abs().sum() > 0

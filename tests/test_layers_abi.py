@@ -256,3 +256,137 @@ def test_products_of_more_tiles_than_a_launch_holds_are_refused():
                 ws_bytes=2 ** 62)
     for t, n, k, fo in ((1, 2 ** 31 - 1, 32, 1), (4096, 2 ** 31 - 1, 64, 256), (3, 2 ** 31 - 1, 128, 128)):
         assert query(t, n, k, fo) > 0
+
+
+EMBED = dict(ids=FAKE, ids_itype=0, N=10, table=FAKE, dtype=0, V=20, F=8, ldt=8, padding=-1, scale=1.0,
+             out=FAKE, out_dtype=0, stream=None)
+
+
+@pytest.mark.parametrize("status,change", [
+    (-3, dict(ids_itype=2)), (-3, dict(dtype=2)), (-3, dict(out_dtype=5)), (-2, dict(N=-1)),
+    (-2, dict(N=2 ** 31)), (-2, dict(V=0)), (-2, dict(V=2 ** 31 - 1)), (-2, dict(F=0)),
+    (-2, dict(F=65537, ldt=65537)), (-2, dict(ldt=7)), (-1, dict(ids=None)), (-1, dict(table=None)),
+    (-1, dict(out=None)), (-8, dict(ids=FAKE + 2)), (-8, dict(ids_itype=1, ids=FAKE + 4)),
+    (-8, dict(table=FAKE + 2)), (-8, dict(out=FAKE + 1))])
+def test_embed_refusals(status, change):
+    refused("mp_embed", EMBED, status, **change)
+
+
+EMBED_BACKWARD = dict(ids=FAKE, ids_itype=0, N=10, dout=FAKE, dtype=0, V=20, F=8, ldd=8, padding=-1,
+                      scale=1.0, dtable=FAKE, dtable_dtype=0, ws=FAKE, ws_bytes=1 << 30, stream=None)
+
+
+@pytest.mark.parametrize("status,change", [
+    (-3, dict(ids_itype=2)), (-3, dict(dtype=2)), (-3, dict(dtable_dtype=5)), (-2, dict(N=-1)),
+    (-2, dict(N=2 ** 31)), (-2, dict(V=0)), (-2, dict(V=2 ** 31 - 1)), (-2, dict(F=0)),
+    (-2, dict(F=65537, ldd=65537)), (-2, dict(ldd=7)), (-1, dict(ids=None)), (-1, dict(dout=None)),
+    (-1, dict(dtable=None)), (-1, dict(ws=None)), (-8, dict(ids_itype=1, ids=FAKE + 4)),
+    (-8, dict(dout=FAKE + 2)), (-8, dict(dtable=FAKE + 1)), (-8, dict(ws=FAKE + 8)),
+    (-5, dict(ws_bytes=64))])
+def test_embed_backward_refusals(status, change):
+    refused("mp_embed_backward", EMBED_BACKWARD, status, **change)
+
+
+RMS = dict(x=FAKE, dtype=0, N=10, F=8, ldx=8, residual=None, ldr=8, weight=None, eps=1e-5, total=None,
+           out=FAKE, out_dtype=0, rstd=None, stream=None)
+
+
+@pytest.mark.parametrize("status,change", [
+    (-3, dict(dtype=2)), (-3, dict(out_dtype=2)), (-2, dict(N=-1)), (-2, dict(N=2 ** 31)), (-2, dict(F=0)),
+    (-2, dict(F=65537, ldx=65537)), (-2, dict(ldx=7)), (-2, dict(residual=FAKE, ldr=7)), (-2, dict(eps=0.0)),
+    (-2, dict(eps=-1e-5)), (-2, dict(eps=float("nan"))), (-2, dict(eps=float("inf"))),
+    (-2, dict(total=FAKE, ldx=9)), (-2, dict(x=FAKE + 4096, residual=FAKE, total=FAKE, ldr=9)),
+    (-1, dict(x=None)), (-1, dict(out=None)), (-8, dict(x=FAKE + 2)), (-8, dict(residual=FAKE + 2)),
+    (-8, dict(weight=FAKE + 2)), (-8, dict(total=FAKE + 2)), (-8, dict(out=FAKE + 2)),
+    (-8, dict(rstd=FAKE + 2))])
+def test_rms_norm_refusals(status, change):
+    refused("mp_rms_norm", RMS, status, **change)
+
+
+RMS8 = dict(x=FAKE, dtype=1, N=10, F=8, ldx=8, residual=None, ldr=8, weight=None, eps=1e-5, total=None,
+            codes=FAKE, scales=FAKE, values=None, rstd=None, stream=None)
+
+
+@pytest.mark.parametrize("status,change", [
+    (-3, dict(dtype=2)), (-2, dict(F=0)), (-2, dict(ldx=7)), (-2, dict(eps=1e-39)), (-1, dict(x=None)),
+    (-1, dict(codes=None)), (-1, dict(scales=None)), (-8, dict(codes=FAKE + 8)), (-8, dict(values=FAKE + 1))])
+def test_rms_norm_mx8_refusals(status, change):
+    refused("mp_rms_norm_mx8", RMS8, status, **change)
+
+
+MX8 = dict(codes=FAKE, scales=FAKE, N=10, K=8, out=FAKE, dtype=0, stream=None)
+
+
+@pytest.mark.parametrize("status,change", [
+    (-3, dict(dtype=2)), (-2, dict(N=-1)), (-2, dict(K=0)), (-2, dict(K=65537)), (-1, dict(codes=None)),
+    (-1, dict(scales=None)), (-1, dict(out=None)), (-8, dict(codes=FAKE + 8)), (-8, dict(out=FAKE + 2))])
+def test_mx8_dequantize_refusals(status, change):
+    refused("mp_mx8_dequantize", MX8, status, **change)
+
+
+RMS_BACKWARD = dict(total=FAKE, dtype=0, N=10, F=8, ldt=8, dout=FAKE, rstd=FAKE, weight=None, dtotal=None,
+                    dx=FAKE, dx_dtype=0, dweight=None, ws=None, ws_bytes=0, stream=None)
+
+
+@pytest.mark.parametrize("status,change", [
+    (-3, dict(dtype=2)), (-3, dict(dx_dtype=2)), (-2, dict(N=-1)), (-2, dict(F=0)), (-2, dict(ldt=7)),
+    (-1, dict(total=None)), (-1, dict(dout=None)), (-1, dict(rstd=None)), (-1, dict(dx=None)),
+    (-1, dict(N=10000, dweight=FAKE)), (-5, dict(N=10000, dweight=FAKE, ws=FAKE, ws_bytes=16)),
+    (-8, dict(dout=FAKE + 2)), (-8, dict(rstd=FAKE + 2)), (-8, dict(dtotal=FAKE + 2)), (-8, dict(dx=FAKE + 2)),
+    (-8, dict(dweight=FAKE + 2)), (-8, dict(N=10000, dweight=FAKE, ws=FAKE + 8, ws_bytes=1 << 30))])
+def test_rms_norm_backward_refusals(status, change):
+    refused("mp_rms_norm_backward", RMS_BACKWARD, status, **change)
+
+
+EXPERTS = dict(x=FAKE, x_dtype=1, x_scales=None, N=8, K=64, ldx=64, idx=FAKE, weight=FAKE, k=2, E=4, H=32, Fo=64,
+               w1=FAKE, w1_scales=None, w2=FAKE, w2_scales=None, act=2, gated=1, residual=None, ldr=64, out=FAKE,
+               out_dtype=1, ws=FAKE, ws_bytes=1 << 30, stream=None)
+
+
+@pytest.mark.parametrize("status,change", [
+    (-3, dict(x_dtype=2)), (-3, dict(out_dtype=2)), (-2, dict(N=-1)), (-2, dict(N=65)), (-2, dict(k=0)),
+    (-2, dict(k=5)), (-2, dict(E=1025)), (-2, dict(N=64, k=17, E=20)), (-2, dict(H=0)), (-2, dict(H=65537)),
+    (-2, dict(Fo=0)), (-2, dict(Fo=65537)), (-2, dict(K=0)), (-2, dict(K=65537, ldx=65537)), (-2, dict(ldx=63)),
+    (-2, dict(residual=FAKE, ldr=63)), (-2, dict(residual=FAKE, ldr=65)), (-2, dict(act=4)), (-2, dict(act=-1)),
+    (-1, dict(x=None)), (-1, dict(idx=None)), (-1, dict(weight=None)), (-1, dict(w1=None)), (-1, dict(w2=None)),
+    (-1, dict(out=None)), (-1, dict(ws=None)), (-1, dict(w1_scales=FAKE)), (-1, dict(w2_scales=FAKE)),
+    (-8, dict(x=FAKE + 1)), (-8, dict(x_scales=FAKE, x=FAKE + 8)), (-8, dict(idx=FAKE + 2)),
+    (-8, dict(weight=FAKE + 2)), (-8, dict(w1=FAKE + 1)), (-8, dict(w1=FAKE + 8, w1_scales=FAKE, w2_scales=FAKE)),
+    (-8, dict(residual=FAKE + 1)), (-8, dict(out=FAKE + 1)), (-8, dict(ws=FAKE + 8)), (-5, dict(ws_bytes=1000))])
+def test_expert_mlp_refusals(status, change):
+    refused("mp_expert_mlp", EXPERTS, status, **change)
+
+
+def test_workspace_queries_refuse_too():
+    for call in (lambda: mp.mp_embed_backward_workspace(-1, 4, 4), lambda: mp.mp_embed_backward_workspace(1, 0, 4),
+                 lambda: mp.mp_rms_norm_backward_workspace(1, 0, 0), lambda: mp.mp_rms_norm_backward_workspace(1, 4, 9),
+                 lambda: mp.mp_expert_mlp_workspace(65, 1, 4, 8, 8, 0), lambda: mp.mp_expert_mlp_workspace(4, 5, 4, 8, 8, 0)):
+        with pytest.raises(mp.MPError):
+            call()
+    assert mp.mp_rms_norm_backward_workspace(0, 4, 0) == 0
+    # small calls have sizes that do not overflow, large ones either
+    assert mp.mp_embed_backward_workspace(2 ** 31 - 1, 2 ** 31 - 2, 65536) > 2 ** 40
+
+
+def test_wrappers_refuse_what_does_not_fit():
+    x, w1, w2 = torch.zeros(4, 64), torch.zeros(2, 64, 64, dtype=torch.bfloat16), torch.zeros(2, 64, 32, dtype=torch.bfloat16)
+    idx, weight = torch.zeros(4, 2, dtype=torch.int32), torch.zeros(4, 2)
+    ids = torch.zeros(4, dtype=torch.int64)
+    bad = [lambda: mp.expert_mlp(x, idx, weight, w1, w2),                      # not on a GPU
+           lambda: mp.expert_mlp(x, idx, weight, w1.float(), w2),
+           lambda: mp.expert_mlp(x, idx, weight, w1[:, :, :60], w2),
+           lambda: mp.expert_mlp(x, idx, weight, w1[:, :63], w2),
+           lambda: mp.expert_mlp(x, idx, weight, w1, w2[:1]),
+           lambda: mp.expert_mlp(x, idx, weight, w1, w2[:, :, :16]),
+           lambda: mp.expert_mlp(x, idx.long(), weight, w1, w2),
+           lambda: mp.expert_mlp(x, idx[:3], weight, w1, w2),
+           lambda: mp.expert_mlp(x, idx, weight, w1, w2, act="tanh"),
+           lambda: mp.expert_mlp(x, idx, weight, w1, w2, residual=x.bfloat16()),  # beside an fp32 result
+           lambda: mp.embed(ids, x), lambda: mp.embed(ids[:, None], x), lambda: mp.embed(ids, x, padding=-3),
+           lambda: mp.embed_backward(ids, x[:3], 9), lambda: mp.rms_norm(x), lambda: mp.rms_norm(x, x[0, :9]),
+           lambda: mp.rms_norm(x, residual=x[:3]), lambda: mp.rms_norm_mx8(x, residual=x.bfloat16()),
+           lambda: mp.rms_norm_backward(x, x, x[:, 0], dtotal=x[:2]), lambda: mp.rms_norm_backward(x, x, x[:3, 0]),
+           lambda: mp.mx8_dequantize(torch.zeros(4, 32, dtype=torch.uint8), torch.zeros(4, 2, dtype=torch.uint8), 32)]
+    for call in bad:
+        with pytest.raises(ValueError):
+            call()
