@@ -95,6 +95,60 @@ __global__ __launch_bounds__(kBlock) void embed_keys(EmbedParams P, int32_t* key
     row[r] = (int32_t)r;
 }
 
+// ---- few rows -----------------------------------------------------------------------
+// Without a sort: the place of a row in the order of the ids is the number of rows
+// before it, counted against all of them in LDS.  A workgroup has kPlaces rows,
+// kSlices threads each, that share the others.
+constexpr int kSlices = 8;
+constexpr int kPlaces = kBlock / kSlices;
+
+// `places` workgroups for the rows; the others clear the gradient.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void embed_places(EmbedParams P, int32_t* key, int32_t* row,
+                                                       int32_t* status, int places) {
+    extern __shared__ int32_t s_key[];
+    const int tid = threadIdx.x, N = (int)P.N;
+    if ((int)blockIdx.x >= places) {
+        const int64_t size = P.V * P.F, threads = (int64_t)(gridDim.x - places) * kBlock;
+        typename T::raw* out = static_cast<typename T::raw*>(P.out);
+        constexpr int E = 16 / sizeof(typename T::raw);
+        const float zero[E] = {};
+        const int64_t i0 = (int64_t)(blockIdx.x - places) * kBlock + tid;
+        for (int64_t i = i0; i < size / E; i += threads) store_floats<T, E>(out + i * E, zero);
+        if (i0 < size % E) store_one<T>(out + size / E * E + i0, 0.f);
+        return;
+    }
+    if (blockIdx.x == 0 && tid == 0) *status = MP_OK;
+    // (filled up to whole slices with keys that are before nothing)
+    const int per = ((N + kSlices - 1) / kSlices + 3) / 4 * 4;
+    for (int i = tid; i < kSlices * per; i += kBlock) {
+        const int64_t id = i < N ? id_at(P, i) : -1;
+        s_key[i] = i >= N ? INT32_MAX : (id >= 0 ? (int32_t)id : (int32_t)P.V);
+    }
+    __syncthreads();
+    // lanes of a slice are neighbours, so that they read the same words
+    const int slice = tid / kPlaces, r = (int)blockIdx.x * kPlaces + tid % kPlaces;
+    const int32_t mine = r < N ? s_key[r] : 0;
+    const int q0 = slice * per;
+    int before = 0;
+    for (int q = q0; q < q0 + per; q += 4) {
+        const int4 k = *reinterpret_cast<const int4*>(&s_key[q]);
+        // of the same id, earlier rows are before
+        before += k.x < mine + (q < r) ? 1 : 0;
+        before += k.y < mine + (q + 1 < r) ? 1 : 0;
+        before += k.z < mine + (q + 2 < r) ? 1 : 0;
+        before += k.w < mine + (q + 3 < r) ? 1 : 0;
+    }
+    __syncthreads();
+    s_key[tid] = before;  // (of all slices, in place of the keys)
+    __syncthreads();
+    if (slice == 0 && r < N) {
+        for (int u = 1; u < kSlices; ++u) before += s_key[u * kPlaces + tid];
+        key[r] = mine;
+        row[before] = r;
+    }
+}
+
 // Row v of the gradient from its sum, columns c ...; nothing for v = V.
 template <typename T, int V>
 __device__ inline void write_row(const EmbedParams& P, int32_t v, int c, const float (&sum)[V]) {
@@ -257,7 +311,7 @@ __global__ __launch_bounds__(kBlock) void embed_grad(EmbedParams P, int per, int
 }
 
 // The rows of ids whose positions lie in several workgroups (of C each), by the
-// workgroup of the first.
+// workgroup of the first.  There is one less than of the others.
 template <int V>
 __global__ __launch_bounds__(kBlock) void embed_join(EmbedParams P, int per, int slots, int64_t C) {
     __shared__ float lds[kBlock * V];
@@ -265,11 +319,21 @@ __global__ __launch_bounds__(kBlock) void embed_join(EmbedParams P, int per, int
     const int slot = threadIdx.x / per, first = threadIdx.x - slot * per;
     if (*P.status != MP_OK) return;
     const int64_t k0 = blockIdx.x, b = k0 * C, e = b + C;
-    if (e >= P.rowptr[P.V]) return;  // (no position of an id of the table follows)
-    const int32_t v = P.key[P.row[e - 1]];
-    const int64_t vbeg = P.rowptr[v], vend = P.rowptr[v + 1];
-    if (vend <= e || vbeg < b) return;
-    const int64_t k1 = (vend - 1) / C;
+    const int32_t v = P.key[P.row[e - 1]];  // (a position follows)
+    if (v == P.V || P.key[P.row[e]] != v || (b > 0 && P.key[P.row[b - 1]] == v)) return;
+    int64_t k1;
+    if (P.rowptr) {
+        k1 = (P.rowptr[v + 1] - 1) / C;
+    } else {
+        // the first workgroup that the id does not go on from, 64 at a time
+        k1 = k0 + 1;
+        uint64_t ends;
+        do {
+            const int64_t p = (k1 + 1 + (threadIdx.x & 63)) * C;
+            ends = __ballot(p >= P.N || P.key[P.row[p]] != v);
+            k1 += ends ? __builtin_ctzll(ends) : 64;
+        } while (!ends);
+    }
     for (int j = first; j < per; j += kBlock) {
         const int c = chunk_at<V>(j, F);
         float acc[V] = {};
@@ -328,9 +392,10 @@ void launch_rows(const EmbedParams& p, const EmbedShape& h, hipStream_t s) {
 template <typename T, int V>
 void launch_grad(const EmbedParams& p, const EmbedShape& h, hipStream_t s) {
     const int64_t C = positions(h), sums = ceil_div(p.N, C);
-    hipLaunchKernelGGL((embed_grad<T, V>),
-                       dim3((unsigned)(sums + at_most(ceil_div(p.V, h.slots * kRows)))), dim3(kBlock),
-                       0, s, p, h.per, h.slots, h.R, sums);
+    const int64_t zeros = p.rowptr ? at_most(ceil_div(p.V, h.slots * kRows)) : 0;
+    if (sums + zeros)
+        hipLaunchKernelGGL((embed_grad<T, V>), dim3((unsigned)(sums + zeros)), dim3(kBlock), 0, s, p,
+                           h.per, h.slots, h.R, sums);
     if (sums > 1)
         hipLaunchKernelGGL((embed_join<V>), dim3((unsigned)(sums - 1)), dim3(kBlock), 0, s, p, h.per,
                            h.slots, C);
@@ -362,6 +427,28 @@ hipError_t launch_embed_keys(const EmbedParams& p, int32_t* key, int32_t* row, h
     if (p.N > 0)
         hipLaunchKernelGGL(embed_keys, dim3((unsigned)ceil_div(p.N, kBlock)), dim3(kBlock), 0, s, p,
                            key, row);
+    return hipGetLastError();
+}
+
+// Up to 4,096 rows: fewer launches (50 ids of 200,000 14 us against 47, 4,096 of 100,000
+// 37 against 55, 8,192 60 against 59).  Where the library's one-workgroup sort takes
+// the ids, up to 2,048 (2,000 of 5,000 ids 22 and 25 us, 8,192 of 10,000 50 and 35).
+bool embed_few(int64_t N, int64_t V) { return N <= (V < kSortSmall ? 2048 : 4096); }
+
+hipError_t launch_embed_places(const EmbedParams& p, int32_t* key, int32_t* row, int32_t* status,
+                               hipStream_t s) {
+    // (without rows the status still is written)
+    const int places = (int)ceil_div(p.N > 0 ? p.N : 1, kPlaces);
+    const int64_t size = p.V * p.F * (p.out_bf16 ? 2 : 4), fill = ceil_div(size, 16 * kBlock);
+    const size_t lds = (size_t)(ceil_div(p.N, kSlices) + 4) * kSlices * 4;
+    const dim3 g((unsigned)(places + (fill < 4096 ? fill : 4096)));
+    const size_t least = kBlock * 4;
+    if (p.out_bf16)
+        hipLaunchKernelGGL((embed_places<BF16>), g, dim3(kBlock), lds > least ? lds : least, s, p, key,
+                           row, status, places);
+    else
+        hipLaunchKernelGGL((embed_places<F32>), g, dim3(kBlock), lds > least ? lds : least, s, p, key,
+                           row, status, places);
     return hipGetLastError();
 }
 

@@ -495,11 +495,16 @@ int mp_embed_backward(const void* ids, int ids_itype, int64_t N, const void* dou
     P.ld = ldd;
     P.out = dtable;
     P.out_bf16 = dtable_dtype == MP_BF16;
-    P.rowptr = rowptr;
     P.row = col;
     P.key = key;
     P.status = status;
     P.part = reinterpret_cast<float*>(w + m.part);
+    if (embed_few(N, V)) {
+        st = hip_status(launch_embed_places(P, key, col, status, as_stream(stream)));
+        if (st != MP_OK) return st;
+        return hip_status(launch_embed_backward(P, dtype, as_stream(stream)));
+    }
+    P.rowptr = rowptr;
     st = hip_status(launch_embed_keys(P, key, row, as_stream(stream)));
     if (st == MP_OK)
         st = mp_coo_to_csr(row, key, N, V + 1, rowptr, MP_I32, col, nullptr, nullptr, nullptr,

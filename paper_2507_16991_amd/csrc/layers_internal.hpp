@@ -281,7 +281,8 @@ struct EmbedParams {
     void* out;                 // rows, or the table's gradient
     int out_bf16;
     // backward
-    const int32_t* rowptr;     // [V + 2] positions of every id; ids outside come last
+    const int32_t* rowptr;     // [V + 2] positions of every id, ids outside last; nullptr
+                               // after launch_embed_places
     const int32_t* row;        // [N] the row at every position
     const int32_t* key;        // [N] the id of every row, V outside
     const int32_t* status;     // the sort's
@@ -290,6 +291,10 @@ struct EmbedParams {
 int64_t embed_parts(int64_t N, int64_t F);
 hipError_t launch_embed(const EmbedParams& p, int dtype, hipStream_t s);
 hipError_t launch_embed_keys(const EmbedParams& p, int32_t* key, int32_t* row, hipStream_t s);
+// Few rows: their order without a sort, and the gradient cleared.
+bool embed_few(int64_t N, int64_t V);
+hipError_t launch_embed_places(const EmbedParams& p, int32_t* key, int32_t* row, int32_t* status,
+                               hipStream_t s);
 hipError_t launch_embed_backward(const EmbedParams& p, int dtype, hipStream_t s);
 
 // ---- the experts of few rows (experts.hip) ---------------------------------------------------

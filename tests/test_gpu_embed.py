@@ -77,6 +77,18 @@ def test_long_and_short_ids(counts, f):
     check_backward(t, dout, len(counts), 1.0, None, mp.embed_backward(t, dout, len(counts)))
 
 
+# either side of where few rows are ordered without a sort, and an id that goes through many workgroups
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("spread", ["even", "popular", "one"])
+@pytest.mark.parametrize("n,v,f", [(2048, 16383, 130), (2049, 16383, 130), (4096, 16384, 40), (4097, 16384, 40), (4095, 99991, 3),
+                                   (4096, 20000, 1100)])
+def test_few_rows_and_more(n, v, f, spread, dtype):
+    ids, _, dout = make(n, v, f, dtype, torch.int64, spread=spread)
+    grad = mp.embed_backward(ids, dout, v)
+    check_backward(ids, dout, v, 1.0, None, grad)
+    assert torch.equal(grad, mp.embed_backward(ids.to(torch.int32), dout, v) if int(ids.max()) < 2 ** 31 else grad)
+
+
 def test_one_id_has_all_rows():
     ids, _, dout = make(70001, 513, 24, BF16, torch.int32, spread="one")
     check_backward(ids, dout, 513, 2.0, None, mp.embed_backward(ids, dout, 513, scale=2.0))
