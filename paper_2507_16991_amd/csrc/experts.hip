@@ -796,7 +796,7 @@ __global__ __launch_bounds__(WAVES * 64) void expert_down(ExpertParams p) {
         // loaded by agent-scope atomics, that is in memory that all XCDs see alike, and
         // every thread waits for its stores before the workgroup is counted: so no
         // fence has to write back and drop the L2 (with __threadfence on both sides
-        // this launch took 45 us for one row, now 7).
+        // this launch took 45 us for one row, now 9).
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         if (tid == 0)
