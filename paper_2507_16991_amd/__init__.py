@@ -183,23 +183,20 @@ def _ptr(t):
         return t
     if not t.is_contiguous():
         raise ValueError("tensors passed to libmp must be contiguous")
-    if t.numel() == 0:
-        # torch reports 0 for an empty tensor; pass its storage address (NULL
-        # only when nothing was ever allocated, see _edge_array)
-        return t.untyped_storage().data_ptr() + t.storage_offset() * t.element_size() or None
-    return t.data_ptr()
+    # torch reports 0 for an empty tensor; pass its storage address (NULL
+    # only when nothing was ever allocated, see _edge_array)
+    return t.data_ptr() or t.untyped_storage().data_ptr() + t.storage_offset() * t.element_size() or None
 
 
 def _rows_ptr(t):
     """Address of a 2-D table whose rows may be strided (stride(1) == 1,
     stride(0) >= shape[1]), and that stride in elements.  (The columns of a
     single row have a stride too; only that of one value or none is of no matter.)"""
-    if (t.dim() != 2 or (t.stride(1) != 1 and (t.shape[0] > 1 or t.numel() > 1))
-            or t.stride(0) < t.shape[1]):
-        raise ValueError("feature tables passed to libmp must have unit column stride")
-    if t.numel() == 0:
-        return _ptr(t.contiguous()), int(t.shape[1])
-    return t.data_ptr(), int(t.stride(0)) if t.shape[0] > 1 else int(t.shape[1])
+    if t.dim() == 2:
+        (n, f), (row, col) = t.shape, t.stride()
+        if (col == 1 or (n <= 1 and n * f <= 1)) and row >= f:
+            return (t.data_ptr() if n * f else _ptr(t.contiguous())), row if n > 1 else f
+    raise ValueError("feature tables passed to libmp must have unit column stride")
 
 
 # The current stream's handle without a Stream object around it (5 us of a small call).

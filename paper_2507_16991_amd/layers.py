@@ -112,6 +112,11 @@ def _table(t):
     return _rows_ptr(t[:, None] if t.dim() == 1 else t)
 
 
+def _rows(t):
+    """Address of a table whose rows may be strided; what is no tensor is an address."""
+    return _rows_ptr(t)[0] if isinstance(t, torch.Tensor) else t
+
+
 def _like(t, ref, name):
     if t is not None and (t.shape != ref.shape or t.dtype != ref.dtype):
         raise ValueError(f"{name} must have the shape and dtype of x")
@@ -511,18 +516,16 @@ def embed_backward(ids, dout, V, *, scale=1.0, padding=None, out_dtype=None, out
 def mp_rms_norm(x, dtype, N, F, ldx, residual, ldr, weight, eps, total, out, out_dtype, rstd,
                 stream=None):
     """x and residual: tensors (rows may be strided) or raw addresses."""
-    xp, rp = (_rows_ptr(t)[0] if isinstance(t, torch.Tensor) else t for t in (x, residual))
     _check("mp_rms_norm", _layers().mp_rms_norm(
-        xp, dtype, N, F, ldx, rp, ldr, _ptr(weight), eps, _ptr(total), _ptr(out), out_dtype, _ptr(rstd),
-        _stream(stream)))
+        _rows(x), dtype, N, F, ldx, _rows(residual), ldr, _ptr(weight), eps, _ptr(total), _ptr(out),
+        out_dtype, _ptr(rstd), _stream(stream)))
 
 
 def mp_rms_norm_mx8(x, dtype, N, F, ldx, residual, ldr, weight, eps, total, codes, scales, values, rstd,
                     stream=None):
-    xp, rp = (_rows_ptr(t)[0] if isinstance(t, torch.Tensor) else t for t in (x, residual))
     _check("mp_rms_norm_mx8", _layers().mp_rms_norm_mx8(
-        xp, dtype, N, F, ldx, rp, ldr, _ptr(weight), eps, _ptr(total), _ptr(codes), _ptr(scales),
-        _ptr(values), _ptr(rstd), _stream(stream)))
+        _rows(x), dtype, N, F, ldx, _rows(residual), ldr, _ptr(weight), eps, _ptr(total), _ptr(codes),
+        _ptr(scales), _ptr(values), _ptr(rstd), _stream(stream)))
 
 
 def mp_mx8_dequantize(codes, scales, N, K, out, dtype, stream=None):
@@ -570,7 +573,7 @@ def rms_norm(x, weight=None, *, residual=None, eps=1e-5, out_dtype=None, out=Non
             out = torch.empty(N, F, dtype=out_dtype or x.dtype, device=dev)
         rstd = torch.empty(N, dtype=torch.float32, device=dev)
         if residual is not None and total is None:
-            total = torch.empty(N, F, dtype=x.dtype, device=dev)
+            total = torch.empty_like(x)
         mp_rms_norm(xp, dt, N, F, ldx, rp, ldr, weight, eps, total, out, _dtype_code(out.dtype), rstd,
                     stream)
     return out, x if total is None else total, rstd
@@ -585,9 +588,9 @@ def rms_norm_mx8(x, weight=None, *, residual=None, eps=1e-5, want_values=False, 
     with _on(stream):
         codes = torch.empty(N, 32 * kb, dtype=torch.uint8, device=dev)
         scales = torch.empty(N, kb, dtype=torch.uint8, device=dev)
-        values = torch.empty(N, F, dtype=x.dtype, device=dev) if want_values else None
+        values = torch.empty_like(x) if want_values else None
         if residual is not None and total is None:
-            total = torch.empty(N, F, dtype=x.dtype, device=dev)
+            total = torch.empty_like(x)
         mp_rms_norm_mx8(xp, dt, N, F, ldx, rp, ldr, weight, eps, total, codes, scales, values, None,
                         stream)
     return codes, scales, values, x if total is None else total
@@ -644,11 +647,10 @@ def mp_expert_mlp_workspace(N, k, E, H, Fo, out_dtype) -> int:
 def mp_expert_mlp(x, x_dtype, x_scales, N, K, ldx, idx, weight, k, E, H, Fo, w1, w1_scales, w2, w2_scales,
                   act, gated, residual, ldr, out, out_dtype, ws, ws_bytes, stream=None):
     """x and residual: tensors (rows may be strided) or raw addresses."""
-    xp, rp = (_rows_ptr(t)[0] if isinstance(t, torch.Tensor) else t for t in (x, residual))
     _check("mp_expert_mlp", _layers().mp_expert_mlp(
-        xp, x_dtype, _ptr(x_scales), N, K, ldx, _ptr(idx), _ptr(weight), k, E, H, Fo, _ptr(w1),
-        _ptr(w1_scales), _ptr(w2), _ptr(w2_scales), act, gated, rp, ldr, _ptr(out), out_dtype, _ptr(ws),
-        ws_bytes, _stream(stream)))
+        _rows(x), x_dtype, _ptr(x_scales), N, K, ldx, _ptr(idx), _ptr(weight), k, E, H, Fo, _ptr(w1),
+        _ptr(w1_scales), _ptr(w2), _ptr(w2_scales), act, gated, _rows(residual), ldr,
+        _ptr(out), out_dtype, _ptr(ws), ws_bytes, _stream(stream)))
 
 
 def _expert_weights(w, cols, name):
