@@ -3,7 +3,7 @@
 //
 // The sort is one-sweep: radix_ghist counts the digits of every pass in one
 // read of the keys; then each pass is ONE kernel, radix_onesweep, in which a
-// tile of kSortTile keys (tile ids taken from an atomic counter in launch
+// tile of sort_tile(n) keys (tile ids taken from an atomic counter in launch
 // order) ranks its keys stably (wave-level multisplit: one ballot per digit
 // bit, per-wavefront LDS counters), publishes its per-digit counts, obtains
 // the running totals of all earlier tiles by decoupled look-back over their
@@ -35,7 +35,6 @@ namespace mp {
 namespace {
 
 constexpr int kSortWaves = kSortBlock / kWave;
-constexpr int kWaveKeys = kWave * kSortItems;  // keys per wavefront per tile
 constexpr int kMaxBuckets = 1 << kSortMaxBits;
 
 constexpr int kGhistBlock = 1024;
@@ -201,7 +200,7 @@ struct WordBits {
 // order, which is element order, and tiles are numbered in the order they
 // start, so the pass is stable.  Staging before the look-back frees the
 // registers of the keys while the tile waits on its predecessors, so the
-// look-back can keep kLookWindow descriptor loads in flight.  Descriptors of
+// look-back can keep many descriptor loads in flight.  Descriptors of
 // a pass over R = 2^bits digits lie R apart per tile.
 //   HAS_B: the COO-id payload b is carried (b = the element index on FIRST).
 //   WIDE:  digits of up to 9 bits (512 buckets: twice the per-wave counters).
@@ -214,16 +213,16 @@ struct WordBits {
 // with b, the keys, a and b go through one staging buffer in turn, the keys
 // before the look-back and the others after the previous array is written.
 // In kDrop, as a staged word has no digit, a byte per slot keeps it.
-constexpr int kLookWindow = 4;
-
-template <bool HAS_B, bool WIDE, bool FIRST, bool LAST>
+template <int ITEMS, bool HAS_B, bool WIDE, bool FIRST, bool LAST>
 __global__ __launch_bounds__(kSortBlock) void radix_onesweep(RadixPass p) {
-    static_assert(kSortTile <= 65536, "16-bit counters and staged slots");
+    constexpr int TILE = kSortBlock * ITEMS, WAVE_KEYS = kWave * ITEMS;
+    constexpr int WINDOW = ITEMS < kSortItems ? 16 : 4;  // descriptors of a look-back round
+    static_assert(TILE <= 65536, "16-bit counters and staged slots");
     constexpr int NB = WIDE ? kMaxBuckets : kMaxBuckets / 2;  // buckets this variant handles
     // per-wave digit counts, then each wave's run start inside its digit
     using cnt_t = uint16_t;
-    __shared__ uint32_t s_stage[2][kSortTile];
-    __shared__ uint8_t s_dig[HAS_B && !WIDE ? kSortTile : 1];  // kDrop: digit of every slot
+    __shared__ uint32_t s_stage[2][TILE];
+    __shared__ uint8_t s_dig[HAS_B && !WIDE ? TILE : 1];  // kDrop: digit of every slot
     __shared__ cnt_t s_cnt[kSortWaves][NB];
     __shared__ uint32_t s_tcnt[NB];   // the tile's count of each digit
     __shared__ uint32_t s_start[NB];  // ... and its exclusive scan
@@ -251,15 +250,15 @@ __global__ __launch_bounds__(kSortBlock) void radix_onesweep(RadixPass p) {
     const int64_t tile = s_tile;
     uint64_t* const desc = p.sc.desc + tile * R;
 
-    const int64_t tbase = tile * kSortTile;
-    const int64_t wbase = tbase + (int64_t)wv * kWaveKeys;
+    const int64_t tbase = tile * TILE;
+    const int64_t wbase = tbase + (int64_t)wv * WAVE_KEYS;
 
-    uint32_t key[kSortItems];
-    int32_t va[kSortItems], vb[HAS_B ? kSortItems : 1];
-    uint32_t rank[kSortItems];
+    uint32_t key[ITEMS];
+    int32_t va[ITEMS], vb[HAS_B ? ITEMS : 1];
+    uint32_t rank[ITEMS];
     if constexpr (FIRST) {
 #pragma unroll
-        for (int k = 0; k < kSortItems; ++k) {
+        for (int k = 0; k < ITEMS; ++k) {
             const int64_t i = wbase + (int64_t)k * kWave + lane;
             const bool ok = i < p.n;
             key[k] = ok ? __builtin_nontemporal_load(p.keys_in + i) : 0u;
@@ -267,15 +266,15 @@ __global__ __launch_bounds__(kSortBlock) void radix_onesweep(RadixPass p) {
             if constexpr (HAS_B) vb[k] = (int32_t)i;
         }
     } else {
-        uint64_t w[kSortItems];
+        uint64_t w[ITEMS];
 #pragma unroll
-        for (int k = 0; k < kSortItems; ++k) {
+        for (int k = 0; k < ITEMS; ++k) {
             const int64_t i = wbase + (int64_t)k * kWave + lane;
             w[k] = i < p.n ? __builtin_nontemporal_load(p.kv_in + i) : 0ull;
         }
         if (!HAS_B || fmt == kWide) {
 #pragma unroll
-            for (int k = 0; k < kSortItems; ++k) {
+            for (int k = 0; k < ITEMS; ++k) {
                 key[k] = (uint32_t)(w[k] >> 32);
                 va[k] = (int32_t)(uint32_t)w[k];
                 if constexpr (HAS_B) {
@@ -285,7 +284,7 @@ __global__ __launch_bounds__(kSortBlock) void radix_onesweep(RadixPass p) {
             }
         } else if constexpr (HAS_B) {
 #pragma unroll
-            for (int k = 0; k < kSortItems; ++k) {
+            for (int k = 0; k < ITEMS; ++k) {
                 const uint32_t hi = (uint32_t)(w[k] >> 32), lo = (uint32_t)w[k];
                 key[k] = word.key(hi, lo);
                 va[k] = word.a(hi, lo);
@@ -303,11 +302,11 @@ __global__ __launch_bounds__(kSortBlock) void radix_onesweep(RadixPass p) {
                             c += __popcll(__ballot(d + lane < PR && (int64_t)s_prev[d + lane] <= pos));
                         return c;
                     };
-                    const int64_t last = wbase + kWaveKeys - 1 < p.n ? wbase + kWaveKeys - 1 : p.n - 1;
+                    const int64_t last = wbase + WAVE_KEYS - 1 < p.n ? wbase + WAVE_KEYS - 1 : p.n - 1;
                     const int dA = count_le(wbase) - 1;
                     const int dB = last > wbase ? count_le(last) - 1 : dA;
 #pragma unroll
-                    for (int k = 0; k < kSortItems; ++k) {
+                    for (int k = 0; k < ITEMS; ++k) {
                         const int64_t i = wbase + (int64_t)k * kWave + lane;
                         int lo = dA, hi = dB;
                         while (lo < hi) {
@@ -321,7 +320,7 @@ __global__ __launch_bounds__(kSortBlock) void radix_onesweep(RadixPass p) {
         }
     }
 #pragma unroll
-    for (int k = 0; k < kSortItems; ++k) {
+    for (int k = 0; k < ITEMS; ++k) {
         const bool ok = wbase + (int64_t)k * kWave + lane < p.n;
         const uint32_t d = (key[k] >> p.shift) & (uint32_t)(R - 1);
         const uint64_t peers = digit_peers<kSortMaxBits>(ok, d, p.bits);
@@ -360,7 +359,7 @@ __global__ __launch_bounds__(kSortBlock) void radix_onesweep(RadixPass p) {
     // stage the tile in LDS in digit order (tile-local positions only)
     uint16_t* const s_lp = reinterpret_cast<uint16_t*>(s_stage[1]);  // kWide with b: slot of every key
 #pragma unroll
-    for (int k = 0; k < kSortItems; ++k) {
+    for (int k = 0; k < ITEMS; ++k) {
         const int64_t i = wbase + (int64_t)k * kWave + lane;
         const uint32_t d = (key[k] >> p.shift) & (uint32_t)(R - 1);
         const uint32_t lp = s_start[d] + s_cnt[wv][d] + rank[k];
@@ -384,7 +383,7 @@ __global__ __launch_bounds__(kSortBlock) void radix_onesweep(RadixPass p) {
     }
 
     // decoupled look-back, one thread per digit: add up earlier tiles'
-    // counts until one that carries an inclusive prefix, kLookWindow
+    // counts until one that carries an inclusive prefix, WINDOW
     // descriptors per round (a descriptor not yet published ends the round;
     // the wait on it is bounded)
     if (threadIdx.x < R) {
@@ -396,16 +395,16 @@ __global__ __launch_bounds__(kSortBlock) void radix_onesweep(RadixPass p) {
             uint32_t spins = 0;
             bool done = false;
             while (!done) {
-                uint64_t v[kLookWindow];
+                uint64_t v[WINDOW];
 #pragma unroll
-                for (int w = 0; w < kLookWindow; ++w)
+                for (int w = 0; w < WINDOW; ++w)
                     v[w] = look - w >= 0
                                ? __hip_atomic_load(col + (look - w) * R, __ATOMIC_RELAXED,
                                                    __HIP_MEMORY_SCOPE_AGENT)
                                : 0ull;
                 int used = 0;
 #pragma unroll
-                for (int w = 0; w < kLookWindow; ++w) {
+                for (int w = 0; w < WINDOW; ++w) {
                     if (done || used < w) continue;  // stopped earlier in this round
                     const bool ready = (uint32_t)((v[w] >> 56) & 63u) == tag && (v[w] >> 62) != 0;
                     if (!ready) continue;
@@ -433,11 +432,11 @@ __global__ __launch_bounds__(kSortBlock) void radix_onesweep(RadixPass p) {
     // write the digit runs: thread t takes staged slots t, t + kSortBlock, ...
     // (a staged row start also gives rowptr: the first slot of a run, whose
     // row an earlier tile may have seen too, or a slot after another row's)
-    const int nvalid = (int)(p.n - tbase < kSortTile ? p.n - tbase : kSortTile);
+    const int nvalid = (int)(p.n - tbase < TILE ? p.n - tbase : TILE);
     if (!HAS_B || fmt == kWide) {
-        int32_t pos[HAS_B ? kSortItems : 1];
+        int32_t pos[HAS_B ? ITEMS : 1];
 #pragma unroll
-        for (int k = 0; k < kSortItems; ++k) {
+        for (int k = 0; k < ITEMS; ++k) {
             const int i = (int)threadIdx.x + k * kSortBlock;
             if constexpr (HAS_B) pos[k] = -1;
             if (i < nvalid) {
@@ -472,7 +471,7 @@ __global__ __launch_bounds__(kSortBlock) void radix_onesweep(RadixPass p) {
                                     : (which == 0 ? p.a_out : p.b_out);
                 __syncthreads();  // every read of the buffer's previous contents is done
 #pragma unroll
-                for (int k = 0; k < kSortItems; ++k) {
+                for (int k = 0; k < ITEMS; ++k) {
                     const int64_t i = wbase + (int64_t)k * kWave + lane;
                     if (i < p.n)
                         s_stage[0][s_lp[k * kSortBlock + threadIdx.x]] =
@@ -480,7 +479,7 @@ __global__ __launch_bounds__(kSortBlock) void radix_onesweep(RadixPass p) {
                 }
                 __syncthreads();
 #pragma unroll
-                for (int k = 0; k < kSortItems; ++k)
+                for (int k = 0; k < ITEMS; ++k)
                     if (pos[k] >= 0)
                         out[half ? 2 * (int64_t)pos[k] : (int64_t)pos[k]] =
                             (int32_t)s_stage[0][threadIdx.x + k * kSortBlock];
@@ -489,7 +488,7 @@ __global__ __launch_bounds__(kSortBlock) void radix_onesweep(RadixPass p) {
     } else if constexpr (HAS_B) {
         const bool key_hi = abits + p.b_bits >= 32;  // the key lies in a word's high half alone
 #pragma unroll
-        for (int k = 0; k < kSortItems; ++k) {
+        for (int k = 0; k < ITEMS; ++k) {
             const int i = (int)threadIdx.x + k * kSortBlock;
             if (i < nvalid) {
                 const uint32_t hi = s_stage[0][i], lo = s_stage[1][i];
@@ -943,6 +942,14 @@ __global__ __launch_bounds__(256) void validate_csr(const RP* __restrict__ rowpt
     if (bad) atomicAdd(count, (unsigned long long)bad);
 }
 
+// Keys of a tile.  Few keys are shared out to more workgroups, whose longer look-back
+// takes more descriptors a round: CSR of 20,000 edges and 169,343 rows 46 -> 28 us,
+// 190,001 edges 52 -> 43 (with ids 58 -> 44), 400,000 56 -> 51; from 700,000 on there
+// is no difference (66 and 66; with ids 72 and 67).
+constexpr int kFewItems = 4;
+constexpr int64_t kFewKeys = 1 << 20;
+int64_t sort_tile(int64_t n) { return kSortBlock * (n <= kFewKeys ? kFewItems : kSortItems); }
+
 inline unsigned grid_for(int64_t n, int per_block) {
     return (unsigned)ceil_div(n > 0 ? n : 1, per_block);
 }
@@ -954,7 +961,7 @@ size_t radix_scratch_bytes(int64_t n, int64_t N) {
 }
 
 RadixScratch radix_scratch(void* base, int64_t n, int64_t N) {
-    const int64_t tiles = ceil_div(n > 0 ? n : 1, kSortTile);
+    const int64_t tiles = ceil_div(n > 0 ? n : 1, sort_tile(n));
     char* b = static_cast<char*>(base);
     size_t off = 0;
     auto take = [&](size_t bytes) {
@@ -992,7 +999,7 @@ hipError_t radix_sort_begin(const uint32_t* keys, const int32_t* a, int64_t n, i
         shifts |= (uint32_t)dp.shift[p] << (8 * p);
         widths |= (uint32_t)dp.width[p] << (8 * p);
     }
-    const int64_t tiles = ceil_div(n, kSortTile);
+    const int64_t tiles = ceil_div(n, sort_tile(n));
     // a pass over R = 2^width digits uses R descriptors per tile
     const int64_t ndesc = tiles * ((int64_t)1 << dp.max_width);
     const int64_t nstarts = sc.starts ? N : 0;
@@ -1008,23 +1015,29 @@ hipError_t radix_sort_begin(const uint32_t* keys, const int32_t* a, int64_t n, i
     return hipGetLastError();
 }
 
-template <bool HAS_B, bool WIDE>
-void launch_onesweep(const RadixPass& p, int64_t tiles, hipStream_t s) {
+template <int ITEMS, bool HAS_B, bool WIDE>
+void launch_items(const RadixPass& p, int64_t tiles, hipStream_t s) {
     const dim3 g((unsigned)tiles), b(kSortBlock);
     const bool first = p.keys_in != nullptr, last = p.a_out != nullptr;
     if (first && last)
-        hipLaunchKernelGGL((radix_onesweep<HAS_B, WIDE, true, true>), g, b, 0, s, p);
+        hipLaunchKernelGGL((radix_onesweep<ITEMS, HAS_B, WIDE, true, true>), g, b, 0, s, p);
     else if (first)
-        hipLaunchKernelGGL((radix_onesweep<HAS_B, WIDE, true, false>), g, b, 0, s, p);
+        hipLaunchKernelGGL((radix_onesweep<ITEMS, HAS_B, WIDE, true, false>), g, b, 0, s, p);
     else if (last)
-        hipLaunchKernelGGL((radix_onesweep<HAS_B, WIDE, false, true>), g, b, 0, s, p);
+        hipLaunchKernelGGL((radix_onesweep<ITEMS, HAS_B, WIDE, false, true>), g, b, 0, s, p);
     else
-        hipLaunchKernelGGL((radix_onesweep<HAS_B, WIDE, false, false>), g, b, 0, s, p);
+        hipLaunchKernelGGL((radix_onesweep<ITEMS, HAS_B, WIDE, false, false>), g, b, 0, s, p);
+}
+
+template <bool HAS_B, bool WIDE>
+void launch_onesweep(const RadixPass& p, int64_t tiles, hipStream_t s) {
+    if (sort_tile(p.n) == kSortTile) launch_items<kSortItems, HAS_B, WIDE>(p, tiles, s);
+    else launch_items<kFewItems, HAS_B, WIDE>(p, tiles, s);
 }
 
 hipError_t radix_sort_pass(const RadixPass& p, hipStream_t s) {
     if (p.n <= 0) return hipSuccess;
-    const int64_t tiles = ceil_div(p.n, kSortTile);
+    const int64_t tiles = ceil_div(p.n, sort_tile(p.n));
     const bool wide = p.bits > kSortMaxBits - 1;
     if (p.b_out) {
         if (wide) launch_onesweep<true, true>(p, tiles, s);

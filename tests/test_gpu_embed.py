@@ -213,3 +213,32 @@ def test_a_training_step_of_the_entrance():
     tol = part * (237 + 12 + count[:, None] + 1) * ref.U
     assert (np.abs(f64(dtable) - t64.grad.numpy()) <= tol).all()
     assert (np.abs(f64(dw) - w64.grad.numpy()) <= sdw * (n + 50 + 6) * ref.U).all()
+
+
+@pytest.mark.parametrize("n", [16385, 20480, 20481, 2 ** 20, 2 ** 20 + 1])
+@pytest.mark.parametrize("rows", [300, 70001])
+def test_order_of_the_sort_on_either_side_of_its_tiles(n, rows):
+    """Keys of many and of few equal ones, with and without their numbers carried along."""
+    g = torch.Generator().manual_seed(n)
+    dst = (torch.rand(n, generator=g) ** 3 * rows).int().clamp(max=rows - 1).to(DEV)
+    src = torch.randint(0, 2 ** 20, (n,), generator=g, dtype=torch.int32).to(DEV)
+    order = torch.from_numpy(np.argsort(dst.cpu().numpy(), kind="stable")).to(DEV)
+    ends = torch.cumsum(torch.bincount(dst, minlength=rows), 0).int()
+    for ids in (False, True):
+        rowptr, col, perm, _ = mp.coo_to_csr(src, dst, rows, want_perm=ids)
+        assert torch.equal(rowptr[1:], ends) and int(rowptr[0]) == 0
+        assert torch.equal(col, src[order])
+        assert perm is None or torch.equal(perm.long(), order)
+
+
+@pytest.mark.parametrize("f", [1, 3, 8])
+def test_an_id_over_many_short_runs(f):
+    """Sums of narrow rows lie in LDS by team; one id begins, fills and ends any number of teams."""
+    n, v = 20000, 5000
+    for first, length in ((0, n), (3, 8 * 70), (17, 8 * 9 + 5), (2043, 10), (2047, 4098), (5, 2043)):
+        ids = torch.arange(n) % 4
+        ids[first:first + length] = 4
+        ids[first + length:] += 5
+        dout = torch.randn(n, f, generator=torch.Generator().manual_seed(length))
+        check_backward(ids.sort()[0].to(DEV), dout.to(DEV), v, 1.0, None,
+                       mp.embed_backward(ids.sort()[0].to(DEV), dout.to(DEV), v))
