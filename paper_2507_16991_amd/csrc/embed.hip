@@ -253,9 +253,16 @@ __device__ inline void sum_runs(const EmbedParams& P, int64_t block, int j, int 
         // the end of a segment that began in an earlier run; what goes on past the workgroup
         if (part_of == 0 ? !(flag & kEnds) : !(last && flag & kGoesOn)) continue;
         int t = part_of == 0 ? slot - 1 : slot;
-        while (t >= 0 && s_flag[t] & kMiddle) --t;
+        // (eight flags, and eight teams' sums, on their way together: one by one the gradient
+        // of 190,001 rows of 1 or 4 fp32, many of one id, took 95 and 103 us for 82 and 91)
+        for (int n = 8; n == 8; t -= n) {
+            n = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) n += n == i && t >= i && s_flag[t >= i ? t - i : 0] & kMiddle;
+        }
         const bool began = t >= 0;  // in this workgroup
         float v[V] = {};
+#pragma unroll 8
         for (int u = t < 0 ? 0 : t; u <= (part_of == 0 ? slot - 1 : slot); ++u)
 #pragma unroll
             for (int i = 0; i < V; ++i) v[i] += s_b[i * kBlock + u * per + j];
@@ -352,6 +359,7 @@ __global__ __launch_bounds__(kBlock) void embed_join(EmbedParams P, int per, int
             for (int i = 0; i < V; ++i) lds[i * kBlock + threadIdx.x] = acc[i];
             __syncthreads();
             if (slot == 0) {
+#pragma unroll 8
                 for (int q = 1; q < slots; ++q)
 #pragma unroll
                     for (int i = 0; i < V; ++i) acc[i] += lds[i * kBlock + q * per + threadIdx.x];
@@ -431,7 +439,7 @@ hipError_t launch_embed_keys(const EmbedParams& p, int32_t* key, int32_t* row, h
 }
 
 // Up to 4,096 rows: fewer launches (50 ids of 200,000 14 us against 47, 4,096 of 100,000
-// 37 against 55, 8,192 60 against 59).  Where the library's one-workgroup sort takes
+// 34 against 43, but 8,192 60 and 47).  Where the library's one-workgroup sort takes
 // the ids, up to 2,048 (2,000 of 5,000 ids 22 and 25 us, 8,192 of 10,000 50 and 35).
 bool embed_few(int64_t N, int64_t V) { return N <= (V < kSortSmall ? 2048 : 4096); }
 
