@@ -316,6 +316,7 @@ int mp_rms_norm_backward(const void* total, int dtype, int64_t N, int64_t F, int
  *   residual   [N, Fo] of out_dtype, row stride ldr, or NULL.
  *   out        [N, Fo] contiguous of out_dtype; may be residual itself (ldr = Fo),
  *              must not overlap the inputs otherwise.
+ * An infinite weight makes the sums that it reaches infinite or NaN.
  * Products of fp32 or bf16 values with bf16 or 4-bit ones are exact but for fp32
  * values under a bf16 result, and h, which are taken to 16 bits of their mantissa (to
  * all of them where out is fp32); 8-bit values and weights below 2^-126 are rounded

@@ -961,7 +961,9 @@ size_t radix_scratch_bytes(int64_t n, int64_t N) {
 }
 
 RadixScratch radix_scratch(void* base, int64_t n, int64_t N) {
-    const int64_t tiles = ceil_div(n > 0 ? n : 1, sort_tile(n));
+    int64_t tiles = ceil_div(n > 0 ? n : 1, sort_tile(n));
+    // (a workspace of more keys is enough for fewer, too)
+    if (n > kFewKeys && tiles < kFewKeys / sort_tile(kFewKeys)) tiles = kFewKeys / sort_tile(kFewKeys);
     char* b = static_cast<char*>(base);
     size_t off = 0;
     auto take = [&](size_t bytes) {

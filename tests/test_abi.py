@@ -80,6 +80,16 @@ def test_coo_to_csr_workspace_sizes():
         mp.mp_coo_to_csr_workspace(10**6, 200, mp.MP_I32, 0)
 
 
+@pytest.mark.parametrize("payload", [0, 1])
+@pytest.mark.parametrize("rows", [100, 2 ** 24])
+def test_a_workspace_of_more_edges_is_enough_for_fewer(rows, payload):
+    """Tiles of the sort are larger from some size on, and so fewer.  (All of these edges are many
+    next to the rows, or all few: the sorted keys are kept only where they are few.)"""
+    edges = [1, 16384, 16385, 2 ** 20 - 1, 2 ** 20, 2 ** 20 + 1, 2 ** 20 + 4096, 2 ** 21, 2 ** 22, 2 ** 22 + 1, 2 ** 23]
+    sizes = [mp.mp_coo_to_csr_workspace(e, rows, mp.MP_I32, payload) for e in edges]
+    assert sizes == sorted(sizes)
+
+
 @pytest.mark.parametrize("E,N", [(-1, 5), (5, 0), (2**31, 5), (5, 2**31)])
 def test_coo_to_csr_size_errors(E, N):
     with pytest.raises(mp.MPError) as e:

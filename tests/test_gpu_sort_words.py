@@ -102,3 +102,21 @@ def test_rowptr_of_rows_beyond_the_last_edge(E, N, where):
     want = torch.zeros(N + 1, dtype=torch.int64, device=DEV)
     want[1:] = torch.bincount(dst, minlength=N).cumsum(0)
     assert torch.equal(rowptr.long(), want)
+
+
+# The same words where tiles have 16,384 keys (above 2^20 edges), and just below.
+LARGER = [
+    (1 << 20, 20_000, BIG), ((1 << 20) + 1, 20_000, BIG),  # one digit left out (15 + 31 + 21)
+    (1_100_000, 1_000, BIG),          # two passes, packed whole (10 + 31 + 21)
+    (1_100_000, 1 << 22, 1 << 28),    # three passes, one digit left out (15 + 28 + 21 = 64)
+    (1_100_000, 1 << 22, 1 << 29),    # too wide by one bit
+    (1_100_000, 200_000, 1 << 25),    # digits of 9 bits, whole (18 + 25 + 21 = 64)
+    (1_100_000, 20_000_000, 7),       # digits of 9 bits, three passes
+    (1_100_000, 300, 9),              # one pass
+]
+
+
+@pytest.mark.parametrize("E,N,src_max", LARGER)
+@pytest.mark.parametrize("kind", ["uniform", "hub", "few"])
+def test_csr_and_transpose_in_larger_tiles(E, N, src_max, kind):
+    test_csr_and_transpose(E, N, src_max, kind)
