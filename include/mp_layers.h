@@ -317,10 +317,10 @@ int mp_rms_norm_backward(const void* total, int dtype, int64_t N, int64_t F, int
  *   out        [N, Fo] contiguous of out_dtype; may be residual itself (ldr = Fo),
  *              must not overlap the inputs otherwise.
  * An infinite weight makes the sums that it reaches infinite or NaN.
- * Products of fp32 or bf16 values with bf16 or 4-bit ones are exact but for fp32
- * values under a bf16 result, and h, which are taken to 16 bits of their mantissa (to
- * all of them where out is fp32); 8-bit values and weights below 2^-126 are rounded
- * to steps of 2^-133 (bf16's); sums are in fp32.
+ * Products are exact, of fp32 rows and of h (fp32) too, and sums are in fp32: with the
+ * same operands a bf16 out is the fp32 one rounded once (after the residual).
+ * Values of rows and weights, and parts of h, are rounded to steps of 2^-133 (bf16's
+ * least).
  * Sizes: 0 <= N <= 64, 1 <= k <= E <= 1024, N * k <= 1024, 1 <= K, H, Fo <= 65536.
  * ws 16-byte aligned; calls that may overlap need one each.
  * ------------------------------------------------------------------------- */

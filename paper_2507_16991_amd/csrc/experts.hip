@@ -12,9 +12,12 @@
 //          joined in LDS, and the shares by the workgroup that ends last.
 // Products run on v_mfma_f32_16x16x32_bf16, weights first, so that a lane's
 // accumulators are neighbouring columns of one row.  4-bit weights are exact in
-// bf16, and so are 8-bit rows; fp32 values are taken as sums of bf16 terms, three
-// of which are exact (two, off by 2^-16, where the result is bf16).  8-bit rows
-// times 4-bit weights are v_mfma_scale_f32_16x16x128_f8f6f4's, as they are.
+// bf16, and so are 8-bit rows; fp32 values (rows, and h) are taken as sums of three
+// bf16 terms, which are exact.  (h with two terms, 16 bits, is a third less to load:
+// 2 of 8 experts for one row 15.9 us for 16.2, 8 of 64 for 16 8-bit rows 47.9 for 51.9, 4
+// of 64 for 64 rows 165 for 170; h in fp32, taken apart by the second launch, 17.4, 56.5
+// and 167.)
+// 8-bit rows times 4-bit weights are v_mfma_scale_f32_16x16x128_f8f6f4's, as they are.
 #include "layers_internal.hpp"
 
 namespace mp {
@@ -301,29 +304,25 @@ struct WeightsBf16 {
     }
 };
 
-// An fp32 value as a sum of bf16 terms: its upper 16 bits, and so on of what is
-// left; of two terms the second is rounded.  Three are exact.  An infinity or NaN
-// is its first term.
-template <int T>
-__device__ inline void split(float x, uint16_t (&t)[T]) {
+// An fp32 value as a sum of three bf16 terms: its upper 16 bits, and so on of what is
+// left.  They are exact, but for bits below 2^-133, the least that bf16 holds.  An
+// infinity or NaN is its first term.
+constexpr int kTermsF32 = 3;
+__device__ inline void split(float x, uint16_t (&t)[kTermsF32]) {
     const uint32_t u = __float_as_uint(x);
     float r = x - __uint_as_float(u & 0xFFFF0000u);
     const bool finite = (u & 0x7F800000u) != 0x7F800000u;
     // (the bits of a NaN may all lie in the lower half)
     t[0] = (uint16_t)((u >> 16) | (!finite && (u & 0xFFFF) ? 0x40u : 0u));
     r = finite ? r : 0.f;
-    if constexpr (T == 3) {
-        const uint32_t m = __float_as_uint(r);
-        t[1] = (uint16_t)(m >> 16);
-        r -= __uint_as_float(m & 0xFFFF0000u);
-    }
-    t[T - 1] = (uint16_t)pack_bf16(r, 0.f);
+    const uint32_t m = __float_as_uint(r);
+    t[1] = (uint16_t)(m >> 16);
+    t[2] = (uint16_t)pack_bf16(r - __uint_as_float(m & 0xFFFF0000u), 0.f);
 }
 
 // Rows: kTerms bf16 terms of every element.
-template <int TERMS>
 struct RowsF32 {
-    static constexpr int kTerms = TERMS;
+    static constexpr int kTerms = kTermsF32;
     template <typename W>
     static constexpr bool kScaled = false;
     template <int U>
@@ -352,22 +351,22 @@ struct RowsF32 {
     }
     template <typename W, int U, Reach R>
     __device__ static void unpack(const Raw<U>& r, int u, int i, int s, int q, int end, int K,
-                                  bf16x8 (&v)[TERMS]) {
+                                  bf16x8 (&v)[kTerms]) {
         uint32_t f[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) f[j] = r.v[u][i][j];
         if (R == kEnd)
             shift_words(f, place(kStep * (s + u) + W::at(i, q), end, K).skip);
-        uint16_t t[TERMS][8];
+        uint16_t t[kTerms][8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            uint16_t w[TERMS];
-            split<TERMS>(__uint_as_float(f[j]), w);
+            uint16_t w[kTerms];
+            split(__uint_as_float(f[j]), w);
 #pragma unroll
-            for (int m = 0; m < TERMS; ++m) t[m][j] = w[m];
+            for (int m = 0; m < kTerms; ++m) t[m][j] = w[m];
         }
 #pragma unroll
-        for (int m = 0; m < TERMS; ++m) __builtin_memcpy(&v[m], t[m], 16);
+        for (int m = 0; m < kTerms; ++m) __builtin_memcpy(&v[m], t[m], 16);
     }
 };
 
@@ -462,15 +461,14 @@ struct RowsMx8 {
     }
 };
 
-// Rows of h: TERMS planes, filled up with zeros to whole steps.
-template <int TERMS>
+// Rows of h: a plane for each term, filled up with zeros to whole steps.
 struct RowsOfH {
-    static constexpr int kTerms = TERMS;
+    static constexpr int kTerms = kTermsF32;
     template <typename W>
     static constexpr bool kScaled = false;
     template <int U>
     struct Raw {
-        uint32_t v[U][TERMS][4][4];
+        uint32_t v[U][kTermsF32][4][4];
     };
     typedef const uint16_t* Row;
     template <typename W, int U, Reach R>
@@ -480,7 +478,7 @@ struct RowsOfH {
             // (steps that are not there: the last one, dropped)
             const int at = R == kFull || kStep * (s + u) < p.Hp ? s + u : p.Hp / kStep - 1;
 #pragma unroll
-            for (int m = 0; m < TERMS; ++m)
+            for (int m = 0; m < kTerms; ++m)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     __builtin_memcpy(r.v[u][m][i],
@@ -489,10 +487,10 @@ struct RowsOfH {
     }
     template <typename W, int U, Reach R>
     __device__ static void unpack(const Raw<U>& r, int u, int i, int s, int q, int end, int,
-                                  bf16x8 (&v)[TERMS]) {
+                                  bf16x8 (&v)[kTerms]) {
         const bool on = R == kFull || kStep * (s + u) + W::at(i, q) < end;
 #pragma unroll
-        for (int m = 0; m < TERMS; ++m) {
+        for (int m = 0; m < kTerms; ++m) {
             uint32_t t[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) t[j] = on ? r.v[u][m][i][j] : 0u;
@@ -501,12 +499,13 @@ struct RowsOfH {
     }
 };
 
-// Steps whose loads are under way together: as many as about 104 registers hold.
+// Steps whose loads are under way together: as many as about 120 registers hold (of 104
+// h with 4-bit weights would have one: 8 of 64 experts for 16 8-bit rows 56.8 us for 52.5).
 template <typename W, typename X, int M>
 constexpr int steps_at_once() {
     constexpr int bytes = (int)(2 * sizeof(typename W::template Raw<1>) +
                                 M * sizeof(typename X::template Raw<1>));
-    return 4 * bytes <= 416 ? 4 : (2 * bytes <= 416 ? 2 : 1);
+    return 4 * bytes <= 480 ? 4 : (2 * bytes <= 480 ? 2 : 1);
 }
 
 // acc[t][m] += weight rows w[t] (this lane's of each 16) times rows x[m] (this lane's
@@ -665,17 +664,10 @@ __device__ inline void up_rows(const ExpertParams& p, const Lists& l, int e, int
             h *= weight;
             const int col = tile * COLS + 16 * t + c;
             if (col >= p.H) continue;
-            uint16_t term[3];
-            if (p.planes == 3) {
-                split<3>(h, term);
-            } else {
-                uint16_t two[2];
-                split<2>(h, two);
-                term[0] = two[0];
-                term[1] = two[1];
-                term[2] = 0;
-            }
-            for (int v = 0; v < p.planes; ++v)
+            uint16_t term[kTermsF32];
+            split(h, term);
+#pragma unroll
+            for (int v = 0; v < kTermsF32; ++v)
                 p.h[((int64_t)v * p.P + pair) * p.Hp + col] = term[v];
         }
     }
@@ -705,7 +697,7 @@ __global__ __launch_bounds__(kBlock) void expert_up(ExpertParams p, int tiles) {
         if (tile == tiles - 1) {  // zeros fill the last step of the rows of h
             const int more = p.Hp - p.H;
             for (int i = threadIdx.x; i < n * more; i += kBlock)
-                for (int v = 0; v < p.planes; ++v)
+                for (int v = 0; v < kTermsF32; ++v)
                     p.h[((int64_t)v * p.P + l.pairs[l.first[e] + i / more]) * p.Hp + p.H +
                         i % more] = 0;
         }
@@ -863,15 +855,11 @@ template <typename W, int M>
 hipError_t launch(const ExpertParams& p, int rows, hipStream_t s) {
     if (rows == kRowsMx8) launch_up<W, RowsMx8, M>(p, s);
     else if (rows == kRowsBf16) launch_up<W, RowsBf16, M>(p, s);
-    else if (p.planes == 3) launch_up<W, RowsF32<3>, M>(p, s);
-    else launch_up<W, RowsF32<2>, M>(p, s);
+    else launch_up<W, RowsF32, M>(p, s);
     const dim3 g((unsigned)(ceil_div(p.Fo, kCols) * p.splits));
     constexpr int D = M == 1 ? 8 : 4;  // wavefronts of a workgroup: their sums fit into LDS
     const size_t lds = in_16(kept_words(p.E, p.P)) + (size_t)D * p.N * kLine * 4;
-    if (p.planes == 3)
-        hipLaunchKernelGGL((expert_down<W, RowsOfH<3>, M, D>), g, dim3(D * 64), lds, s, p);
-    else
-        hipLaunchKernelGGL((expert_down<W, RowsOfH<2>, M, D>), g, dim3(D * 64), lds, s, p);
+    hipLaunchKernelGGL((expert_down<W, RowsOfH, M, D>), g, dim3(D * 64), lds, s, p);
     return hipGetLastError();
 }
 
@@ -890,5 +878,6 @@ hipError_t launch_experts(const ExpertParams& p, int rows, int mx4, hipStream_t 
 }
 
 size_t expert_list_bytes(int64_t E, int64_t P) { return (size_t)kept_words((int)E, (int)P) * 4; }
+size_t expert_h_bytes(int64_t P, int64_t Hp) { return (size_t)kTermsF32 * (size_t)P * (size_t)Hp * 2; }
 
 }  // namespace mp

@@ -138,10 +138,9 @@ int expert_space(int64_t N, int64_t k, int64_t E, int64_t H, int64_t Fo, int out
     if (N < 0 || N > 64 || k < 1 || k > E || E > 1024 || N * k > 1024 || H < 1 || H > kMaxF || Fo < 1 ||
         Fo > kMaxF)
         return MP_ERR_SIZE;
-    const size_t planes = out_dtype == MP_BF16 ? 2 : 3, tiles = (size_t)ceil_div(Fo, 32);
-    const size_t splits = (size_t)expert_splits(Fo);
+    const size_t tiles = (size_t)ceil_div(Fo, 32), splits = (size_t)expert_splits(Fo);
     m.h = 0;
-    m.part = align_up(planes * (size_t)(N * k) * align_up((size_t)H, 128) * 2, 256);
+    m.part = align_up(expert_h_bytes(N * k, (int64_t)align_up((size_t)H, 128)), 256);
     m.arrived = m.part + (splits > 1 ? align_up(tiles * splits * (size_t)N * 32 * 4, 256) : 0);
     m.lists = m.arrived + align_up(tiles * 4, 256);
     m.bytes = m.lists + align_up(expert_list_bytes(E, N * k), 256);
@@ -649,7 +648,6 @@ int mp_expert_mlp(const void* x, int x_dtype, const uint8_t* x_scales, int64_t N
     P.out = out;
     P.out_bf16 = out_dtype == MP_BF16;
     P.splits = expert_splits(Fo);
-    P.planes = out_dtype == MP_BF16 ? 2 : 3;
     P.h = reinterpret_cast<uint16_t*>(w + m.h);
     P.Hp = (int)align_up((size_t)H, 128);
     P.part = reinterpret_cast<float*>(w + m.part);

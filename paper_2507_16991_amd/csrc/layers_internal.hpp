@@ -315,8 +315,7 @@ struct ExpertParams {
     void* out;
     int out_bf16;
     int splits;                // of the second product's work
-    int planes;                // bf16 terms of an element of h
-    uint16_t* h;               // workspace [planes][P][Hp]
+    uint16_t* h;               // workspace [terms of an element][P][Hp]
     int Hp;                    // H in whole steps
     float* part;               // workspace [column tiles][splits][N][32]
     int* arrived;              // workspace [column tiles]
@@ -325,6 +324,7 @@ struct ExpertParams {
 enum { kRowsF32 = 0, kRowsBf16 = 1, kRowsMx8 = 2 };
 int expert_splits(int64_t Fo);
 size_t expert_list_bytes(int64_t E, int64_t P);
+size_t expert_h_bytes(int64_t P, int64_t Hp);
 hipError_t launch_experts(const ExpertParams& p, int rows, int mx4, hipStream_t s);
 
 }  // namespace mp
