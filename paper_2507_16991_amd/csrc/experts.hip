@@ -17,7 +17,10 @@
 // 2 of 8 experts for one row 15.9 us for 16.2, 8 of 64 for 16 8-bit rows 47.9 for 51.9, 4
 // of 64 for 64 rows 165 for 170; h in fp32, taken apart by the second launch, 17.4, 56.5
 // and 167.)
-// 8-bit rows times 4-bit weights are v_mfma_scale_f32_16x16x128_f8f6f4's, as they are.
+// 8-bit rows times 4-bit weights go the same way.  v_mfma_scale_f32_16x16x128_f8f6f4
+// takes them as they are, but adds each 8 neighbouring products of a lane to some 15 bits
+// below the largest (448 * 6 + 0.125 * 0.5 is 448 * 6): sums off by 2^-17 of their size, in
+// 52 us for 59 (8 of 64 experts for 16 rows, both launches).
 #include "layers_internal.hpp"
 
 namespace mp {
@@ -25,12 +28,10 @@ namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kBlock = 256;
 constexpr int kWaves = kBlock / kWave;
 constexpr int kStep = 128;    // elements of K of a step, 32 for a quarter of the lanes
-constexpr int kE4M3 = 0, kE2M1 = 4;  // operand formats of the scaled products
 constexpr int kCols = 32;     // weight rows of a workgroup
 constexpr int64_t kUpGrid = 512;  // workgroups of the first launch, at most
 constexpr int kLine = 36;     // floats of a row's sums in LDS
@@ -217,7 +218,6 @@ __device__ inline bf16x8 take_bf16(const uint32_t (&w)[4], int k, int end, int K
 }
 
 struct WeightsMx4 {
-    static constexpr bool kMx4 = true;
     template <int U>
     struct Raw {
         uint32_t c[U][4];
@@ -277,7 +277,6 @@ struct WeightsMx4 {
 };
 
 struct WeightsBf16 {
-    static constexpr bool kMx4 = false;
     template <int U>
     struct Raw {
         uint32_t v[U][4][4];
@@ -323,8 +322,6 @@ __device__ inline void split(float x, uint16_t (&t)[kTermsF32]) {
 // Rows: kTerms bf16 terms of every element.
 struct RowsF32 {
     static constexpr int kTerms = kTermsF32;
-    template <typename W>
-    static constexpr bool kScaled = false;
     template <int U>
     struct Raw {
         uint32_t v[U][4][8];
@@ -372,8 +369,6 @@ struct RowsF32 {
 
 struct RowsBf16 {
     static constexpr int kTerms = 1;
-    template <typename W>
-    static constexpr bool kScaled = false;
     template <int U>
     struct Raw {
         uint32_t v[U][4][4];
@@ -400,9 +395,6 @@ struct RowsBf16 {
 
 struct RowsMx8 {
     static constexpr int kTerms = 1;
-    // Whether products with these weights take codes and scales as they are.
-    template <typename W>
-    static constexpr bool kScaled = W::kMx4;
     template <int U>
     struct Raw {
         uint32_t c[U][4][2];
@@ -426,22 +418,14 @@ struct RowsMx8 {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int k0 = kStep * (s + u);
-            if constexpr (kScaled<W>) {
-                // 8-bit codes k = 16 q .. + 15 and 64 + 16 q .. + 15
 #pragma unroll
-                for (int i = 0; i < 4; i += 2)
-                    __builtin_memcpy(r.c[u][i], x.codes + in_row(k0 + 32 * i + 16 * q), 16);
-                if (R != kFull) r.s[u] = x.scales[in_row(k0 + 32 * q) / 32];
-            } else {
+            for (int i = 0; i < 4; ++i)
+                __builtin_memcpy(r.c[u][i], x.codes + in_row(k0 + W::at(i, q)), 8);
+            if (R != kFull) {
+                uint32_t b[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    __builtin_memcpy(r.c[u][i], x.codes + in_row(k0 + W::at(i, q)), 8);
-                if (R != kFull) {
-                    uint32_t b[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) b[i] = x.scales[in_row(k0 + 32 * i) / 32];
-                    r.s[u] = b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24;
-                }
+                for (int i = 0; i < 4; ++i) b[i] = x.scales[in_row(k0 + 32 * i) / 32];
+                r.s[u] = b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24;
             }
         }
     }
@@ -464,8 +448,6 @@ struct RowsMx8 {
 // Rows of h: a plane for each term, filled up with zeros to whole steps.
 struct RowsOfH {
     static constexpr int kTerms = kTermsF32;
-    template <typename W>
-    static constexpr bool kScaled = false;
     template <int U>
     struct Raw {
         uint32_t v[U][kTermsF32][4][4];
@@ -522,39 +504,6 @@ __device__ inline void multiply_steps(const ExpertParams& p, const typename W::R
 #pragma unroll
     for (int m = 0; m < M; ++m) X::template load<W, U, R>(rx[m], p, x[m], s, q, end, K);
     __builtin_amdgcn_sched_barrier(0);  // (the compiler would spread them to save registers)
-    if constexpr (X::template kScaled<W>) {
-        // lane quarter q has the scales of block q
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            i32x8 a[2];
-            int sa[2];
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                uint32_t c[4];
-                W::template codes<U, R>(rw[t], u, s, q, end, c);
-                a[t] = i32x8{(int)c[0], (int)c[1], (int)c[2], (int)c[3], 0, 0, 0, 0};
-                sa[t] = (int)W::template scale<U, R>(rw[t], u, s, q, end);
-            }
-#pragma unroll
-            for (int m = 0; m < M; ++m) {
-                // (codes of the other half of a dropped block lie in other lanes)
-                i32x8 b;
-                __builtin_memcpy(&b, rx[m].c[u], 32);
-                int sb = (int)(R == kFull ? rx[m].s[u] >> (8 * q) : rx[m].s[u]);
-                if (R != kFull) {
-                    const int k = kStep * (s + u);
-                    sb = k + 32 * q < end ? sb : 0;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) b[i] = k + 64 * (i / 4) + 16 * q < end ? b[i] : 0;
-                }
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-                    acc[t][m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-                        a[t], b, acc[t][m], kE2M1, kE4M3, 0, sa[t], 0, sb);
-            }
-        }
-        return;
-    }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         bf16x8 a[2][4];

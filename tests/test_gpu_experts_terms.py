@@ -73,3 +73,27 @@ def test_a_bf16_result_is_the_fp32_one_rounded(n, x, w):
     idx, weight = choices(n, 6, 3, 4)
     whole = mp.expert_mlp(rows, idx, weight, w1, w2, out_dtype=F32)
     assert torch.equal(mp.expert_mlp(rows, idx, weight, w1, w2, out_dtype=BF16), whole.to(BF16))
+
+
+@pytest.mark.parametrize("out", [F32, BF16])
+@pytest.mark.parametrize("w", ["bf16", "mx4"])
+@pytest.mark.parametrize("x", ["f32", "bf16", "mx8"])
+@pytest.mark.parametrize("at", [0, 64, 130])
+@pytest.mark.parametrize("n", [1, 20])
+def test_small_products_beside_large_ones(n, at, x, w, out):
+    """448 * 6 + 2^-6 / 2 + 448 * -6 of neighbouring places: the sums have at most 20 bits, and the small
+    product is left of the large ones."""
+    k = 192
+    rows = torch.zeros(n, k, device=DEV)
+    rows[:, at], rows[:, at + 1], rows[:, at + 2] = 448.0, 2.0 ** -6, 448.0
+    if x == "mx8":
+        codes = rows.to(torch.float8_e4m3fn).view(torch.uint8)
+        rows = codes, torch.full((n, k // 32), 127, dtype=torch.uint8, device=DEV)
+    elif x == "bf16":
+        rows = rows.to(BF16)
+    w1 = torch.zeros(1, 32, k, dtype=BF16, device=DEV)
+    w1[0, :, at], w1[0, :, at + 1], w1[0, :, at + 2] = 6.0, 0.5, -6.0
+    w2 = torch.eye(32, device=DEV).to(BF16)[None]
+    idx, weight = torch.zeros(n, 1, dtype=torch.int32, device=DEV), torch.ones(n, 1, device=DEV)
+    got = mp.expert_mlp(rows, idx, weight, as_kind(w1, w), as_kind(w2, w), act="none", gated=False, out_dtype=out)
+    assert (f64(got) == 2.0 ** -7).all()
