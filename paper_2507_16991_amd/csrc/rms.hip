@@ -206,6 +206,10 @@ __device__ inline void norm_row(const RmsParams& P, int64_t r, float* lds) {
             for (int i = 0; i < V; ++i) v[i] *= w[i];
         }
         if constexpr (Q8) {
+            if (at[k] + V > F) {  // (zeros past the row also where rstd is NaN)
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[i] = at[k] + i < F ? v[i] : 0.f;
+            }
             uint32_t c[2], sc;
             quantize8(v, c, sc);
             const int KB = (F + 31) / 32, b = at[k] / 32;
