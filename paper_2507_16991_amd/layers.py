@@ -707,6 +707,8 @@ def expert_mlp(x, idx, weight, w1, w2, *, act="silu", gated=True, residual=None,
     k = int(idx.shape[1])
     _vector(idx, N * k, torch.int32, "idx")
     _vector(weight, N * k, torch.float32, "weight")
+    if weight.shape != idx.shape:
+        raise ValueError("weight must have the shape of idx")
     if out is not None and tuple(out.shape) != (N, Fo):
         raise ValueError("out must be [N, Fo]")
     kind = out.dtype if out is not None else out_dtype or default
