@@ -227,8 +227,9 @@ int mp_embed_backward_workspace(int64_t N, int64_t V, int64_t F, size_t* bytes);
 
 /* dL/dtable given dout = dL/dout [N, F] of dtype, row stride ldd:
  *   dtable[v] = scale * sum over the rows r of id v of dout[r]
- * summed in fp32 in the order of the rows, over rows sorted by id; the sums of
- * an id of many rows are joined from chunks of it.
+ * summed in fp32 in an order that ids and sizes alone set, over rows sorted by id:
+ * runs of an id's rows in their order, and what several runs and workgroups have of
+ * it joined after that.
  *   dtable  [V, F] contiguous of dtable_dtype, written in full (0 for an id of
  *           no row); must not overlap dout.  All of it is NaN if the sort gave
  *           up (MP_ERR_SORT, as for mp_coo_to_csr).

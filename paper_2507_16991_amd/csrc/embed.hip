@@ -2,15 +2,17 @@
 // (include/mp_layers.h).
 //
 // Forward: bound by memory; a thread has 16 bytes of a row.
-// Backward: the rows' numbers lie sorted by id (the library's radix sort), so that
-// every row of the gradient is the sum of consecutive positions, in the order of
-// the rows: no atomics.  The positions, not the ids, are shared out: a team of lanes
+// Backward: the rows' numbers lie sorted by id (the library's radix sort), and those
+// of an id in order, so that every row of the gradient is the sum of consecutive
+// positions: no atomics.  The positions, not the ids, are shared out: a team of lanes
 // walks over a run of them and writes the rows of the ids that begin and end
 // there, so that popular and rare ids cost the same (a team an id instead: 103 us
 // for 169,343 ids of 256 fp32, 350 for 2.4M of 100 bf16; now 95 and 280).  What
 // an id has in several runs is joined in LDS by the team of its last run, what it
-// has in several workgroups by a second launch, each in order.  Rows of ids without
-// positions are zeroed by workgroups of their own.
+// has in several workgroups by a second launch, whose teams take every so many
+// of them and are then added up: an order that the positions alone set.  (That launch has
+// one workgroup an id: one with most rows of a large batch leaves the rest of the chip
+// idle.)  Rows of ids without positions are zeroed by workgroups of their own.
 #include "layers_internal.hpp"
 
 namespace mp {
@@ -76,7 +78,7 @@ __device__ inline void copy_rows(const EmbedParams& P, int64_t r0, int first, in
 }
 
 // A workgroup has kRows * slots rows, slots = 256 / per of `per` chunks (1 of
-// longer ones). 
+// longer ones).
 template <typename T, int V>
 __global__ __launch_bounds__(kBlock) void embed_rows(EmbedParams P, int per, int slots) {
     const int slot = threadIdx.x / per, first = threadIdx.x - slot * per;
@@ -165,10 +167,10 @@ __device__ inline void write_row(const EmbedParams& P, int32_t v, int c, const f
 enum { kEnds = 1, kGoesOn = 2, kMiddle = 4 };  // A there, B there, all of the run is B
 
 // The workgroup's runs of R * kRun positions, columns of chunk j.  Flags and what lies
-// in A and B go through LDS where there are several teams.
+// in B go through LDS where there are several teams (A is its own team's).
 template <typename T, int V>
 __device__ inline void sum_runs(const EmbedParams& P, int64_t block, int j, int per, int slots, int slot, int R,
-                                float* s_a, float* s_b, int* s_flag) {
+                                float* s_b, int* s_flag) {
     const int F = (int)P.F, c = chunk_at<V>(j, F);
     const int tid = threadIdx.x;
     const int64_t p0 = (block * slots + slot) * R * kRun;
@@ -241,10 +243,7 @@ __device__ inline void sum_runs(const EmbedParams& P, int64_t block, int j, int 
         return;
     }
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        s_a[i * kBlock + tid] = a[i];
-        s_b[i * kBlock + tid] = acc[i];
-    }
+    for (int i = 0; i < V; ++i) s_b[i * kBlock + tid] = acc[i];
     if (j == 0) s_flag[slot] = flag;
     __syncthreads();
     if (slot >= slots) return;
@@ -283,7 +282,7 @@ __device__ inline void sum_runs(const EmbedParams& P, int64_t block, int j, int 
 template <typename T, int V>
 __global__ __launch_bounds__(kBlock) void embed_grad(EmbedParams P, int per, int slots, int R,
                                                      int64_t sums) {
-    __shared__ float s_a[kBlock * V], s_b[kBlock * V];
+    __shared__ float s_b[kBlock * V];
     __shared__ int s_flag[kBlock + 1];  // (one for the threads beside the teams)
     const int F = (int)P.F;
     const int slot = threadIdx.x / per, first = threadIdx.x - slot * per;
@@ -293,7 +292,7 @@ __global__ __launch_bounds__(kBlock) void embed_grad(EmbedParams P, int per, int
         if (failed) return;
         // (several teams: all threads make one pass)
         for (int j = first; j < per; j += kBlock)
-            sum_runs<T, V>(P, before, j, per, slots, slot, R, s_a, s_b, s_flag);
+            sum_runs<T, V>(P, before, j, per, slots, slot, R, s_b, s_flag);
         return;
     }
     if (slot >= slots) return;

@@ -491,7 +491,8 @@ def embed(ids, table, *, scale=1.0, padding=None, out_dtype=None, out=None, stre
 
 def embed_backward(ids, dout, V, *, scale=1.0, padding=None, out_dtype=None, out=None, stream=None):
     """dL/dtable [V, F] of out_dtype (default dout's) of embed given dout = dL/dout [N, F], in full: 0 for
-    ids of no row.  Sums are in fp32 and in the rows' order, whatever runs beside."""
+    ids of no row.  Sums are in fp32 and in a fixed order (ids and sizes alone set it), so the same bits
+    every time."""
     V, N, F = int(V), int(dout.shape[0]), int(dout.shape[1])
     if ids.dim() != 1 or int(ids.shape[0]) != N:
         raise ValueError("ids [N] and dout [N, F] expected")
