@@ -208,7 +208,10 @@ struct WordBits {
 //   LAST:  a (and b) are written alone, and for rowptr the key too, or where
 //          the tile first sees a row, starts[row] takes the place (the least
 //          over all tiles: a row's edges lie together, in tile order);
-//          otherwise words are written.
+//          otherwise words are written.  Of a sort of one pass a digit is a row,
+//          and only the tile that no edge of it precedes names its place: from
+//          all 256 tiles the rows' few words take an atomic after the other (2^20
+//          edges of 64 rows 95 us in tiles of 4,096 keys, now 34).
 // A tile's words are staged in LDS as two halves at once (128 KB); in kWide
 // with b, the keys, a and b go through one staging buffer in turn, the keys
 // before the look-back and the others after the previous array is written.
@@ -426,6 +429,7 @@ __global__ __launch_bounds__(kSortBlock) void radix_onesweep(RadixPass p) {
                                __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
         s_gbase[d] += (uint32_t)excl;
+        if constexpr (FIRST && LAST) s_tcnt[d] = excl == 0;  // (the count is published)
     }
     __syncthreads();
 
@@ -450,7 +454,7 @@ __global__ __launch_bounds__(kSortBlock) void radix_onesweep(RadixPass p) {
                         if (p.sc.keys)
                             p.sc.keys[q] = kk;
                         else if ((i == (int)run || kk != s_stage[0][i > 0 ? i - 1 : 0]) &&
-                                 (int64_t)kk < p.rows)
+                                 (int64_t)kk < p.rows && (!(FIRST && LAST) || s_tcnt[d]))
                             atomicMin(p.sc.starts + kk, (uint32_t)q);
                         if constexpr (!HAS_B) p.a_out[q] = (int32_t)s_stage[1][i];
                     } else if constexpr (HAS_B) {
@@ -507,7 +511,8 @@ __global__ __launch_bounds__(kSortBlock) void radix_onesweep(RadixPass p) {
                             // within a run the keys differ exactly where the words' do
                             const int j = i > 0 ? i - 1 : 0;
                             const uint32_t kb = word.key(s_stage[0][j], key_hi ? 0u : s_stage[1][j]);
-                            if ((i == (int)run || kk != kb) && (int64_t)v < p.rows)
+                            if ((i == (int)run || kk != kb) && (int64_t)v < p.rows &&
+                                (!(FIRST && LAST) || s_tcnt[d]))
                                 atomicMin(p.sc.starts + v, (uint32_t)q);
                         }
                         p.a_out[q] = word.a(hi, lo);
@@ -944,11 +949,20 @@ __global__ __launch_bounds__(256) void validate_csr(const RP* __restrict__ rowpt
 
 // Keys of a tile.  Few keys are shared out to more workgroups, whose longer look-back
 // takes more descriptors a round: CSR of 20,000 edges and 169,343 rows 46 -> 28 us,
-// 190,001 edges 52 -> 43 (with ids 58 -> 44), 400,000 56 -> 51; from 700,000 on there
-// is no difference (66 and 66; with ids 72 and 67).
+// 190,001 edges 52 -> 43 (with ids 58 -> 44), 400,000 56 -> 51.  With ids it still is
+// less at 2^20 (300,000 rows 88 -> 81); without, 2^20 edges of 170,000 rows 72 -> 74, of
+// 1,000 51 -> 53, of one 33 -> 37, and 600,000 of 300,000 rows 73 -> 69, of one 30 -> 32.
 constexpr int kFewItems = 4;
-constexpr int64_t kFewKeys = 1 << 20;
-int64_t sort_tile(int64_t n) { return kSortBlock * (n <= kFewKeys ? kFewItems : kSortItems); }
+constexpr int64_t kFewKeys = 1 << 20, kFewWithoutIds = 3 << 18;
+int64_t sort_tile(int64_t n, bool ids) {
+    return kSortBlock * (n <= (ids ? kFewKeys : kFewWithoutIds) ? kFewItems : kSortItems);
+}
+// Most tiles that n keys make.  (A workspace of more keys is enough for fewer, too.)
+int64_t sort_tiles_most(int64_t n) {
+    const int64_t tiles = ceil_div(n > 0 ? n : 1, sort_tile(n, true));
+    const int64_t few = kFewKeys / (kSortBlock * kFewItems);
+    return n > kFewKeys && tiles < few ? few : tiles;
+}
 
 inline unsigned grid_for(int64_t n, int per_block) {
     return (unsigned)ceil_div(n > 0 ? n : 1, per_block);
@@ -961,9 +975,7 @@ size_t radix_scratch_bytes(int64_t n, int64_t N) {
 }
 
 RadixScratch radix_scratch(void* base, int64_t n, int64_t N) {
-    int64_t tiles = ceil_div(n > 0 ? n : 1, sort_tile(n));
-    // (a workspace of more keys is enough for fewer, too)
-    if (n > kFewKeys && tiles < kFewKeys / sort_tile(kFewKeys)) tiles = kFewKeys / sort_tile(kFewKeys);
+    const int64_t tiles = sort_tiles_most(n);
     char* b = static_cast<char*>(base);
     size_t off = 0;
     auto take = [&](size_t bytes) {
@@ -1001,7 +1013,7 @@ hipError_t radix_sort_begin(const uint32_t* keys, const int32_t* a, int64_t n, i
         shifts |= (uint32_t)dp.shift[p] << (8 * p);
         widths |= (uint32_t)dp.width[p] << (8 * p);
     }
-    const int64_t tiles = ceil_div(n, sort_tile(n));
+    const int64_t tiles = ceil_div(n, sort_tile(n, true));  // (no fewer than without ids)
     // a pass over R = 2^width digits uses R descriptors per tile
     const int64_t ndesc = tiles * ((int64_t)1 << dp.max_width);
     const int64_t nstarts = sc.starts ? N : 0;
@@ -1033,13 +1045,13 @@ void launch_items(const RadixPass& p, int64_t tiles, hipStream_t s) {
 
 template <bool HAS_B, bool WIDE>
 void launch_onesweep(const RadixPass& p, int64_t tiles, hipStream_t s) {
-    if (sort_tile(p.n) == kSortTile) launch_items<kSortItems, HAS_B, WIDE>(p, tiles, s);
+    if (sort_tile(p.n, HAS_B) == kSortTile) launch_items<kSortItems, HAS_B, WIDE>(p, tiles, s);
     else launch_items<kFewItems, HAS_B, WIDE>(p, tiles, s);
 }
 
 hipError_t radix_sort_pass(const RadixPass& p, hipStream_t s) {
     if (p.n <= 0) return hipSuccess;
-    const int64_t tiles = ceil_div(p.n, sort_tile(p.n));
+    const int64_t tiles = ceil_div(p.n, sort_tile(p.n, p.b_out != nullptr));
     const bool wide = p.bits > kSortMaxBits - 1;
     if (p.b_out) {
         if (wide) launch_onesweep<true, true>(p, tiles, s);
