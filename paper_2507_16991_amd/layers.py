@@ -583,7 +583,8 @@ def rms_norm(x, weight=None, *, residual=None, eps=1e-5, out_dtype=None, out=Non
 def rms_norm_mx8(x, weight=None, *, residual=None, eps=1e-5, want_values=False, total=None, stream=None):
     """rms_norm in microscaled 8 bits: (codes [N, 32 KB] uint8, scales [N, KB] uint8, values, total),
     KB = ceil(F / 32).  values: what they stand for, [N, F] of x's dtype, or None without want_values;
-    total as rms_norm's.  (codes, scales) are rows of expert_mlp."""
+    total as rms_norm's.  (codes, scales) are rows of expert_mlp.  The gradient is rms_norm_backward's, with
+    the rstd that rms_norm gives of the same rows (mp_rms_norm_mx8 writes it too)."""
     N, F, dt, xp, ldx, rp, ldr = _rms_operands(x, weight, residual, total)
     dev, kb = x.device, _blocks(F)
     with _on(stream):
@@ -677,7 +678,9 @@ def expert_mlp(x, idx, weight, w1, w2, *, act="silu", gated=True, residual=None,
     are route's (idx -1: no choice).  w1 [E, (2 if gated else 1) * H, K] and w2 [E, Fo, H]: bf16 both, or
     both as (codes, scales) of mx_quantize.  out_dtype: default x's, bf16 for rows in 8 bits.
 
-    For the many rows of a batch sort them by expert (coo_to_csr) and take mx_segment_matmul."""
+    For the many rows of a batch sort them by expert (coo_to_csr) and take mx_segment_matmul, or segment_matmul
+    (rows and W.transpose(1, 2) in bf16).  The former takes the rows in 4 bits, which this call does not, so
+    that its results differ by that rounding."""
     a = _act(act)
     if isinstance(x, torch.Tensor):
         xs, K, dt = None, int(x.shape[1]), _dtype_code(x.dtype)
